@@ -438,8 +438,8 @@ def _plain_copy(st):
 def _run_compact(st):
     if own:
         from paper_2510_26475_amd import binding
-        binding.respec_pages_compact(st["page_indptr"], st["page_table"], st["page_count"], st["page_refs"], st["new_table"],
-                                     st["new_refs"], st["copy_src"], st["copy_dst"], st["num_live"], st["ws"])
+        binding.respec_pages_compact(st["page_table"], st["page_refs"], st["new_table"], st["new_refs"], st["copy_src"],
+                                     st["copy_dst"], st["num_live"], st["ws"])
         for k, v in st["pools"]:
             binding.respec_pages_copy(k, v, st["copy_src"], st["copy_dst"])
     else:
