@@ -16,6 +16,9 @@
  * respec_tree_rejection_sample, the paged-cache forms respec_verify_attention_paged and
  * respec_commit_accepted_paged, respec_kd_rows, the drafter's distillation loss over the
  * same logits rows (Section 5.3), and respec_solver_pick, the Solver's table look-up (host code).
+ * Around the verify step: respec_prompt_attention and respec_append_paged fill the cache before drafting
+ * begins, respec_pages_* share, grow, free and move its pages, and respec_token_logprobs records
+ * the log-probabilities of the emitted tokens (Algorithm 1), with their gradient.
  *
  * General rules
  *   - Every data pointer is a DEVICE pointer (HIP global memory) unless it says "host".
@@ -255,6 +258,142 @@ respec_status_t respec_commit_accepted_paged(void *k_pages, void *v_pages, const
                                              int32_t D, respec_dtype_t dt, void *hip_stream);
 
 /*
+ * Attention over whole prompts (the forward that fills a sequence's cache before drafting begins
+ * and rebuilds it where a sequence moves from plain to speculative decoding through the
+ * prefill interface, Section 5.2).  The result is that of respec_verify_attention, for any
+ * number of rows:
+ *     out[q_indptr[b]+i, h, :] = sum_j softmax_j(sm_scale * <q[row,h,:], K_b[j,h/G,:]>) V_b[j,h/G,:]
+ * over the keys j = 0 .. L_b-R_b+i of sequence b.  L_b = R_b is a prompt by itself; L_b > R_b is
+ * a prompt's next chunk, its earlier tokens being in the cache.  A row that sees no key (L_b < R_b)
+ * gets zeros and lse = -inf; a sequence may have no rows or no tokens; rows of `out` that belong to no
+ * sequence are left as they were.  Softmax and accumulation run in fp32; for RESPEC_BF16 the products
+ * run on bf16 MFMA, probabilities are rounded to bf16 for the second one, and the result to nearest even.
+ *
+ *   q         [total_q, Hq, D]    dt, token stride ld_q elements
+ *   k, v      [total_kv, Hkv, D]  dt, token strides ld_k, ld_v elements: a token's heads lie back to
+ *             back, so slices of one projection's output can be passed as they are
+ *   q_indptr  [B+1] int32; kv_indptr [B+1] int64
+ *   out       [total_q, Hq, D]    dt, contiguous (written)
+ *   lse       [total_q, Hq] f32 or NULL (written), as in respec_verify_attention
+ *   max_q_per_seq, max_kv_len   host-side upper bounds of R_b and L_b; rows or keys beyond them are
+ *             not processed
+ *   D in {64, 128}; Hq % Hkv == 0; strides multiples of 16 bytes; data pointers 16-byte aligned.
+ *   workspace respec_prompt_attention_workspace_bytes(...) bytes, 256-byte aligned, scratch (nothing
+ *             to prepare, nothing survives): calls that overlap need one each, captured ones too.
+ * A value of V that is not finite reaches only the rows that see its key.  Repeated calls give the same bits.
+ */
+size_t respec_prompt_attention_workspace_bytes(int32_t B, int32_t total_q, int64_t total_kv, int32_t max_q_per_seq,
+                                               int32_t max_kv_len, int32_t Hq, int32_t Hkv, int32_t D,
+                                               respec_dtype_t dt);
+respec_status_t respec_prompt_attention(const void *q, const void *k, const void *v, const int32_t *q_indptr,
+                                        const int64_t *kv_indptr, void *out, float *lse, int32_t B,
+                                        int32_t total_q, int64_t total_kv, int32_t max_q_per_seq,
+                                        int32_t max_kv_len, int32_t Hq, int32_t Hkv, int32_t D, int64_t ld_q,
+                                        int64_t ld_k, int64_t ld_v, float sm_scale, respec_dtype_t dt,
+                                        void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * The same over a paged cache: k_pages, v_pages, page_indptr, page_table, kv_len, num_pages,
+ * page_table_len and page_size as in respec_verify_attention_paged (kv_len includes the R_b new
+ * tokens, whose K/V are in the pages already: respec_append_paged).  Only slots below kv_len are read.
+ * The workspace is that of respec_prompt_attention with total_kv = num_pages * page_size.
+ */
+respec_status_t respec_prompt_attention_paged(const void *q, const void *k_pages, const void *v_pages,
+                                              const int32_t *q_indptr, const int32_t *page_indptr,
+                                              const int32_t *page_table, const int32_t *kv_len, void *out,
+                                              float *lse, int32_t B, int32_t total_q, int32_t num_pages,
+                                              int32_t page_table_len, int32_t page_size,
+                                              int32_t max_q_per_seq, int32_t max_kv_len, int32_t Hq,
+                                              int32_t Hkv, int32_t D, int64_t ld_q, float sm_scale,
+                                              respec_dtype_t dt, void *workspace, size_t workspace_bytes,
+                                              void *hip_stream);
+
+/*
+ * The K/V of new tokens into the pages that the paged attention reads: row i of sequence b
+ * (k_new, v_new [total_q, Hkv, D], token stride ld_new elements) goes to position kv_len[b]-R_b+i.
+ * Rows whose position is negative, past the sequence's pages, or in a page id outside
+ * [0, num_pages) are not written anywhere.  kv_len is not changed.  Pages that are written must
+ * belong to one sequence only (respec_pages_resize sees to that).
+ *   Hkv*D*sizeof(element) and the stride in bytes must be multiples of 16, data pointers 16-byte aligned.
+ */
+respec_status_t respec_append_paged(const void *k_new, const void *v_new, void *k_pages, void *v_pages,
+                                    const int32_t *q_indptr, const int32_t *page_indptr,
+                                    const int32_t *page_table, const int32_t *kv_len, int32_t B, int32_t total_q,
+                                    int32_t max_q_per_seq, int32_t num_pages, int32_t page_table_len,
+                                    int32_t page_size, int32_t Hkv, int32_t D, int64_t ld_new, respec_dtype_t dt,
+                                    void *hip_stream);
+
+/*
+ * Pages of the cache: who holds which.  A rollout group forks one prompt into its responses, which
+ * then grow apart and end at different times; these calls keep the page tables of the paged entry
+ * points while that happens (Sections 5.1 and 5.2: the cache stays in place).  The state is
+ *   page_indptr [B+1] int32   the entries of page_table that belong to sequence b: the most pages it
+ *               can hold
+ *   page_table  [page_table_len] int32; page_count [B] int32: the first page_count[b] of sequence b's
+ *               entries name the pages it holds, the others are -1
+ *   kv_len      [B] int32     tokens held (<= page_size * page_count[b])
+ *   page_refs   [num_pages] int32   how many entries of page_table name a page; 0 = free
+ * all in device memory, started by the caller as -1, zeros and zeros.  Nothing waits for the host:
+ * a sequence that cannot be served is left as it was and says so in out_missing.  A page is shared
+ * until one of its holders is about to write into it.  Copies of contents are only listed
+ * (copy_src[i] -> copy_dst[i], -1 = none): respec_pages_copy carries them out, once per layer.
+ * Ids in the arrays that lie outside their bounds are never followed.
+ *
+ * respec_pages_resize: sequence b shall hold the pages for want_tokens[b] tokens (negative: leave
+ * it alone; 0: give everything back).
+ *   - Pages past those are given back, their entries become -1, kv_len is cut to want_tokens[b].
+ *   - New pages are the lowest free ones, in the order of the sequences.  Free is what had no
+ *     reference before the call: what the call itself gives back is handed out by the next one.
+ *   - If want_tokens[b] > kv_len[b] and the page that position kv_len[b] lies in is shared, the sequence
+ *     gets a page of its own in its place (before its other new pages in the order) and entry b
+ *     of copy_src and copy_dst [B] names the two.  Whether it is shared is decided before the call: holders that all grow
+ *     in one call all get a page.  Do the copies before the next call that hands out pages.
+ *   - out_missing[b] [B] = 0, or the pages that sequence b needed and did not get: the free ones did not
+ *     suffice for it and the sequences before it, or its part of page_table is too short (such a
+ *     sequence takes no page from the others).
+ *   kv_len is not raised: the caller adds the new tokens when it has them.
+ */
+size_t respec_pages_workspace_bytes(int32_t B, int32_t num_pages);
+respec_status_t respec_pages_resize(const int32_t *want_tokens, const int32_t *page_indptr, int32_t *page_table,
+                                    int32_t *page_count, int32_t *kv_len, int32_t *page_refs, int32_t *copy_src,
+                                    int32_t *copy_dst, int32_t *out_missing, int32_t B, int32_t page_table_len,
+                                    int32_t num_pages, int32_t page_size, void *workspace, size_t workspace_bytes,
+                                    void *hip_stream);
+
+/*
+ * respec_pages_fork: sequence b becomes a copy of sequence parent[b] (parent [B] int32, negative: b is
+ * left alone): it names the same pages, and kv_len and page_count are its parent's.  out_missing[b] = 0,
+ * or -1 where b was left as it was: it held pages, its part of page_table is too short, or the parent
+ * is not a sequence or is itself a child of this call.
+ */
+respec_status_t respec_pages_fork(const int32_t *parent, const int32_t *page_indptr, int32_t *page_table,
+                                  int32_t *page_count, int32_t *kv_len, int32_t *page_refs, int32_t *out_missing,
+                                  int32_t B, int32_t page_table_len, int32_t num_pages, void *hip_stream);
+
+/*
+ * respec_pages_compact: moves the used pages to the front of the pools, so that these can be cut.
+ * With n pages used, those behind the first n go to the free ones among them, the highest to the
+ * lowest, at most max_moves of them.  The new table and the new counts of references go to
+ * new_page_table and new_page_refs, which may be the old ones; until the caller changes over, the old ones
+ * stay right for readers in flight, as only free pages are written.  copy_src, copy_dst
+ * [max_moves]: the moves, then -1.  *out_pages_end [1]: every used page lies below it afterwards.
+ * The workspace is respec_pages_workspace_bytes(1, num_pages) bytes at least.
+ */
+respec_status_t respec_pages_compact(const int32_t *page_table, const int32_t *page_refs, int32_t *new_page_table,
+                                     int32_t *new_page_refs, int32_t *copy_src, int32_t *copy_dst,
+                                     int32_t *out_pages_end, int32_t page_table_len, int32_t num_pages,
+                                     int32_t max_moves, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * respec_pages_copy: page copy_src[i] of both pools to page copy_dst[i], i < n, for the pools of
+ * one layer.  Entries with an id outside [0, num_pages) or with copy_src[i] == copy_dst[i] are skipped.
+ * The copies run at the same time: no page may be written twice, or be read by one and written by another.
+ */
+respec_status_t respec_pages_copy(void *k_pages, void *v_pages, const int32_t *copy_src, const int32_t *copy_dst,
+                                  int32_t n, int32_t num_pages, int32_t page_size, int32_t Hkv, int32_t D,
+                                  respec_dtype_t dt, void *hip_stream);
+
+/*
  * Profiling hook (benchmarks only; not for production callers).  One-shot: the calling
  * thread's NEXT attention call (any of the respec_verify_attention* entry points) records
  * `before_main` (if non-NULL) on that call's stream right before its main kernel and
@@ -466,6 +605,54 @@ respec_status_t respec_kd_rows(const void *target_logits, const void *draft_logi
                                double *total_loss, int32_t rows, int32_t V, int64_t ld_t, int64_t ld_d,
                                int64_t ld_g, respec_dtype_t logits_dt, void *workspace,
                                size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Log-probabilities of given tokens, with the entropy of their rows and the best alternatives: what
+ * a rollout records of the tokens it emits under the target and under the drafter (Algorithm 1 stores
+ * log p and log q), over the same logits rows that the samplers read.  For every row r, with
+ * z = logits[r, :] / T,
+ *     out_lse[r]     = log sum_x exp z(x)
+ *     out_logprob[r] = z(tokens[r]) - out_lse[r]
+ *     out_entropy[r] = -sum_x p(x) log p(x),   p = exp(z - out_lse[r])   (p(x) = 0 terms are 0)
+ *     out_top_tokens[r, i], out_top_logprobs[r, i]   the top_n largest logits, descending, the lowest
+ *                      token id first among equal ones (a row with fewer logits ends with -1 and -inf)
+ * A row whose token lies outside [0, V) (the samplers' fill, -1) is not read: its numbers are 0, its
+ * alternatives -1 and 0.  Logits of -inf are tokens without probability; a row of nothing else, or one
+ * with a NaN or +inf, gives NaN (and lse = -inf in the first case).
+ *
+ *   logits    [rows, V], row stride ld elements (>= V)  logits_dt.  Any alignment; rows that start
+ *             16-byte aligned are fastest
+ *   tokens    [rows] int32
+ *   row_temperature [rows] f32 or NULL: one temperature per row instead of `temperature`; one that is
+ *             not positive and finite gives NaN
+ *   out_entropy [rows] f32 or NULL; out_top_tokens, out_top_logprobs [rows, top_n] or NULL with top_n = 0
+ *   top_n <= 64 (RESPEC_ERR_UNSUPPORTED otherwise)
+ *   workspace respec_token_logprobs_workspace_bytes(...) bytes, 256-byte aligned, scratch (nothing to
+ *             prepare, nothing survives); it does not depend on the number of rows
+ * Sums are formed in a fixed order: repeated calls give the same bits.
+ */
+size_t respec_token_logprobs_workspace_bytes(int32_t rows, int32_t V, int32_t top_n, respec_dtype_t logits_dt);
+respec_status_t respec_token_logprobs(const void *logits, const int32_t *tokens, const float *row_temperature,
+                                      float *out_logprob, float *out_lse, float *out_entropy,
+                                      int32_t *out_top_tokens, float *out_top_logprobs, int32_t rows, int32_t V,
+                                      int64_t ld, int32_t top_n, float temperature, respec_dtype_t logits_dt,
+                                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * The gradient of a loss over them in the logits: with g = dloss/dlogprob[r] and h = dloss/dentropy[r]
+ *     grad_logits[r, x] = (g ([x = tokens[r]] - p(x)) - h p(x) (log p(x) + H_r)) / T
+ * from the lse and entropy that respec_token_logprobs wrote for the same logits, tokens and
+ * temperatures.  Rows without a token get zeros (and are not read).
+ *   grad_logprob  [rows] f32 or NULL (zeros); grad_entropy [rows] f32 or NULL (zeros; entropy may be
+ *                 NULL then); not both NULL
+ *   grad_logits   [rows, V] logits_dt, row stride ld_g (written; bf16: rounded to nearest even).  It may be
+ *                 `logits` itself with ld_g == ld; other overlaps are a caller error
+ */
+respec_status_t respec_token_logprobs_grad(const void *logits, const int32_t *tokens, const float *row_temperature,
+                                           const float *lse, const float *entropy, const float *grad_logprob,
+                                           const float *grad_entropy, void *grad_logits, int32_t rows, int32_t V,
+                                           int64_t ld, int64_t ld_g, float temperature, respec_dtype_t logits_dt,
+                                           void *hip_stream);
 
 /*
  * Debug check of the device-side data that the other entry points cannot report: they clamp

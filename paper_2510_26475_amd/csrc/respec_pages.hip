@@ -1,0 +1,577 @@
+// Pages of the KV cache for gfx950: sequences that grow, shrink, fork and give their pages back, pages moved together, and the
+// copies and appends that go with it (the cache that the serving side keeps under the rollouts, Sections 5.1 and 5.2).
+//
+// The state is four integer arrays: page_table with page_indptr (the paged attention's own), page_count (pages held by a
+// sequence) and page_refs (table entries that name a page; 0 = free).  There is no free list: the i-th page that a call hands out
+// is the i-th lowest free one, a prefix sum over page_refs, so equal states give equal tables whatever the device did before.
+// A call is index work on a few hundred kilobytes at most, bound by launches and by the latency of dependent loads; the copies
+// are bound by HBM.  Index work is done once per forward, copies once per layer: respec_pages_copy takes the lists that the
+// others leave.
+#include "respec_common.hpp"
+#include "respec_tiles.hpp"
+
+#include <algorithm>
+
+namespace respec {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+constexpr int kPagesPerBlock = 4 * kThreads;  // page_refs that a work-group ranks: four in a row per thread
+constexpr int32_t kKeep = INT32_MIN;          // a page that compaction neither moves nor fills
+
+struct PageState {
+    const int32_t *page_indptr;
+    int32_t *page_table;
+    int32_t *page_count;
+    int32_t *kv_len;
+    int32_t *page_refs;
+    int32_t B, table_len, num_pages, page_shift;
+};
+
+// What the table of sequence b may hold: its first entry, its entries, and the pages it holds of them (all inside the buffers
+// whatever the arrays hold).
+struct Seq {
+    int32_t e0, cap, count;
+};
+__device__ inline Seq seq_of(const PageState &p, int b) {
+    Seq s;
+    s.e0 = max(0, min(p.page_indptr[b], p.table_len));
+    s.cap = max(0, min(p.page_indptr[b + 1], p.table_len) - s.e0);
+    s.count = max(0, min(p.page_count[b], s.cap));
+    return s;
+}
+__device__ inline bool is_page(const PageState &p, int32_t id) { return (uint32_t)id < (uint32_t)p.num_pages; }
+
+// Inclusive sums over the threads of a work-group; `total` is everybody's.
+__device__ inline int block_scan(int x, int &total, int *lds /* [kThreads / 64] */) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int in_wave = wave_scan_add(x);
+    if (lane == 63) lds[wave] = in_wave;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+    for (int w = 0; w < kThreads / 64; ++w) {
+        before += w < wave ? lds[w] : 0;
+        total += lds[w];
+    }
+    __syncthreads();
+    return before + in_wave;
+}
+
+__device__ inline int block_sum_of(const int32_t *a, int n, int *lds) {
+    int s = 0, total;
+    for (int i = threadIdx.x; i < n; i += kThreads) s += a[i];
+    block_scan(s, total, lds);
+    return total;
+}
+
+// ------------------------------------------------------------------------------------------ resize
+struct ResizeParams {
+    PageState s;
+    const int32_t *want;
+    int32_t *copy_src, *copy_dst, *missing;
+    int32_t blocks;
+    int32_t *block_free;  // [blocks] free pages of each block of page_refs
+    int32_t *begin;       // [B] where a sequence's part of `fresh` begins
+    int32_t *need;        // [B] how many it takes; bit 30: the first of them replaces a shared page; bit 31: too many for its table
+    int32_t *total_need;  // [1]
+    int32_t *fresh;       // [num_pages] the free pages in order
+};
+constexpr int32_t kSplitBit = 1 << 30, kRefusedBit = INT32_MIN, kNeedMask = kSplitBit - 1;
+
+// The last work-group: what every sequence needs, by the state before the call.  The others: how many pages of a block are free.
+__global__ __launch_bounds__(kThreads) void resize_plan_kernel(ResizeParams p) {
+    __shared__ int lds[kThreads / 64];
+    const PageState &s = p.s;
+    int total;
+    if ((int)blockIdx.x < p.blocks) {
+        int n = 0;
+        for (int i = 0; i < 4; ++i) {
+            const int page = blockIdx.x * kPagesPerBlock + threadIdx.x * 4 + i;
+            n += page < s.num_pages && s.page_refs[page] == 0;
+        }
+        block_scan(n, total, lds);
+        if (threadIdx.x == 0) p.block_free[blockIdx.x] = total;
+        return;
+    }
+    int base = 0;
+    for (int b0 = 0; b0 < s.B; b0 += kThreads) {
+        const int b = b0 + threadIdx.x;
+        int word = 0, take = 0;
+        if (b < s.B && p.want[b] >= 0) {
+            const Seq q = seq_of(s, b);
+            const int64_t pages = ((int64_t)p.want[b] + ((1 << s.page_shift) - 1)) >> s.page_shift;
+            const int len = max(0, s.kv_len[b]), at = len >> s.page_shift;
+            bool split = false;
+            if (p.want[b] > len && (len & ((1 << s.page_shift) - 1)) != 0 && at < q.count) {
+                const int32_t id = s.page_table[q.e0 + at];
+                split = is_page(s, id) && s.page_refs[id] > 1;
+            }
+            const int64_t need = max((int64_t)0, pages - q.count) + split;
+            word = (int)min(need, (int64_t)kNeedMask) | (split ? kSplitBit : 0);
+            if (pages > q.cap) word |= kRefusedBit;
+            else take = (int)need;
+        }
+        const int to = block_scan(take, total, lds);
+        if (b < s.B) {
+            p.begin[b] = base + to - take;
+            p.need[b] = word;
+        }
+        base += total;  // (at most the entries of page_table and one page for each sequence)
+    }
+    if (threadIdx.x == 0) *p.total_need = base;
+}
+
+// The free pages in order, as many as are needed.
+__global__ __launch_bounds__(kThreads) void resize_rank_kernel(ResizeParams p) {
+    __shared__ int lds[kThreads / 64];
+    const PageState &s = p.s;
+    const int wanted = *p.total_need;
+    if (wanted == 0) return;  // (uniform)
+    const int before = block_sum_of(p.block_free, blockIdx.x, lds);
+    if (before >= wanted) return;
+    int is_free[4], n = 0, total;
+    for (int i = 0; i < 4; ++i) {
+        const int page = blockIdx.x * kPagesPerBlock + threadIdx.x * 4 + i;
+        is_free[i] = page < s.num_pages && s.page_refs[page] == 0;
+        n += is_free[i];
+    }
+    int rank = before + block_scan(n, total, lds) - n;
+    for (int i = 0; i < 4; ++i)
+        if (is_free[i]) p.fresh[rank++] = blockIdx.x * kPagesPerBlock + threadIdx.x * 4 + i;
+}
+
+// One work-group per sequence.  A page named by several sequences that let go of it in one call is counted down by each; a page
+// handed out was free before the call, so no other sequence of the call names it.
+__global__ __launch_bounds__(kThreads) void resize_apply_kernel(ResizeParams p) {
+    __shared__ int lds[kThreads / 64];
+    const PageState &s = p.s;
+    const int b = blockIdx.x;
+    const int want = p.want[b];
+    const int word = p.need[b], need = word & kNeedMask;
+    const bool split = (word & kSplitBit) != 0;
+    bool ok = (word & kRefusedBit) == 0;
+    if (ok && need > 0) {  // (uniform)
+        const int n_free = block_sum_of(p.block_free, p.blocks, lds);
+        ok = p.begin[b] + need <= n_free;
+    }
+    const Seq q = seq_of(s, b);
+    const int len = s.kv_len[b];
+    __syncthreads();  // (count and length are read by everybody before one thread writes them)
+    if (threadIdx.x == 0) {
+        p.missing[b] = want >= 0 && !ok ? need : 0;
+        p.copy_src[b] = p.copy_dst[b] = -1;
+    }
+    if (want < 0 || !ok) return;
+    const int pages = (int)(((int64_t)want + ((1 << s.page_shift) - 1)) >> s.page_shift);
+    const int32_t *fresh = p.fresh + p.begin[b];
+    for (int e = pages + threadIdx.x; e < q.count; e += kThreads) {
+        const int32_t id = s.page_table[q.e0 + e];
+        if (is_page(s, id)) atomicSub(&s.page_refs[id], 1);
+        s.page_table[q.e0 + e] = -1;
+    }
+    for (int e = q.count + threadIdx.x; e < pages; e += kThreads) {
+        const int32_t id = fresh[split + e - q.count];
+        s.page_table[q.e0 + e] = id;
+        s.page_refs[id] = 1;
+    }
+    if (threadIdx.x == 0) {
+        if (split) {
+            int32_t *entry = &s.page_table[q.e0 + (len >> s.page_shift)];
+            atomicSub(&s.page_refs[*entry], 1);
+            p.copy_src[b] = *entry;
+            p.copy_dst[b] = *entry = fresh[0];
+            s.page_refs[fresh[0]] = 1;
+        }
+        s.page_count[b] = pages;
+        s.kv_len[b] = min(len, want);
+    }
+}
+
+// ------------------------------------------------------------------------------------------ fork
+struct ForkParams {
+    PageState s;
+    const int32_t *parent;
+    int32_t *missing;
+};
+
+// One work-group per sequence.  Only sequences with a parent are written, and a parent has none itself, so no work-group reads
+// what another one writes (the counts of references aside, which are added to).
+__global__ __launch_bounds__(kThreads) void fork_kernel(ForkParams p) {
+    const PageState &s = p.s;
+    const int b = blockIdx.x, from = p.parent[b];
+    if (from < 0) {
+        if (threadIdx.x == 0) p.missing[b] = 0;
+        return;
+    }
+    bool ok = from < s.B && from != b && p.parent[from] < 0;
+    Seq q{}, f{};
+    if (ok) {
+        q = seq_of(s, b);
+        f = seq_of(s, from);
+        ok = q.count == 0 && f.count <= q.cap;
+    }
+    __syncthreads();  // (the count is read by everybody before one thread writes it)
+    if (threadIdx.x == 0) p.missing[b] = ok ? 0 : -1;
+    if (!ok) return;
+    for (int e = threadIdx.x; e < f.count; e += kThreads) {
+        const int32_t id = s.page_table[f.e0 + e];
+        s.page_table[q.e0 + e] = id;
+        if (is_page(s, id)) atomicAdd(&s.page_refs[id], 1);
+    }
+    if (threadIdx.x == 0) {
+        s.page_count[b] = f.count;
+        s.kv_len[b] = s.kv_len[from];
+    }
+}
+
+// ------------------------------------------------------------------------------------------ compact
+struct CompactParams {
+    const int32_t *page_table, *page_refs;
+    int32_t table_len, num_pages;
+    int32_t *new_table, *new_refs;
+    int32_t *copy_src, *copy_dst, *pages_end;
+    int32_t max_moves, blocks;
+    int32_t *block_live;  // [blocks]
+    int32_t *moves;       // [1] live pages behind the first num_live
+    int32_t *role;        // [num_pages] n >= 0: the n-th highest of those; -1-n: the n-th lowest free page before them; kKeep
+    int32_t *high, *hole; // [num_pages / 2 + 1] the pages with those roles
+};
+
+__global__ __launch_bounds__(kThreads) void compact_count_kernel(CompactParams p) {
+    __shared__ int lds[kThreads / 64];
+    int n = 0, total;
+    for (int i = 0; i < 4; ++i) {
+        const int page = blockIdx.x * kPagesPerBlock + threadIdx.x * 4 + i;
+        n += page < p.num_pages && p.page_refs[page] > 0;
+    }
+    block_scan(n, total, lds);
+    if (threadIdx.x == 0) p.block_live[blockIdx.x] = total;
+}
+
+// With n live pages in all, the m live ones behind the first n pages go to the m free ones among them.  Both numbers are the
+// same, so a page's partner is known by its rank: highest live to lowest free, so that a bounded number of moves frees the end.
+__global__ __launch_bounds__(kThreads) void compact_rank_kernel(CompactParams p) {
+    __shared__ int lds[kThreads / 64];
+    const int before = block_sum_of(p.block_live, blockIdx.x, lds);
+    const int n_live = block_sum_of(p.block_live, p.blocks, lds);
+    int live[4], n = 0, total;
+    for (int i = 0; i < 4; ++i) {
+        const int page = blockIdx.x * kPagesPerBlock + threadIdx.x * 4 + i;
+        live[i] = page < p.num_pages && p.page_refs[page] > 0;
+        n += live[i];
+    }
+    int rank = before + block_scan(n, total, lds) - n;  // live pages before this one
+    for (int i = 0; i < 4; ++i) {
+        const int page = blockIdx.x * kPagesPerBlock + threadIdx.x * 4 + i;
+        if (page >= p.num_pages) break;
+        int32_t role = kKeep;
+        if (live[i] && page >= n_live) {
+            role = n_live - 1 - rank;
+            p.high[role] = page;
+        } else if (!live[i] && page < n_live) {
+            p.hole[page - rank] = page;
+            role = -1 - (page - rank);
+        }
+        p.role[page] = role;
+        rank += live[i];
+        if (page == max(n_live, 1) - 1) *p.moves = n_live - (n_live > 0 ? rank : 0);
+    }
+}
+
+// A thread per page, per table entry and per place of the lists.
+__global__ __launch_bounds__(kThreads) void compact_apply_kernel(CompactParams p) {
+    __shared__ int lds[kThreads / 64];
+    const int moves = *p.moves, done = min(moves, p.max_moves);
+    const int stride = gridDim.x * kThreads, first = blockIdx.x * kThreads + threadIdx.x;
+    if (blockIdx.x == 0) {
+        const int n_live = block_sum_of(p.block_live, p.blocks, lds);
+        if (threadIdx.x == 0) *p.pages_end = moves <= p.max_moves ? n_live : p.high[p.max_moves] + 1;
+    }
+    for (int i = first; i < p.max_moves; i += stride) {
+        p.copy_src[i] = i < done ? p.high[i] : -1;
+        p.copy_dst[i] = i < done ? p.hole[i] : -1;
+    }
+    for (int page = first; page < p.num_pages; page += stride) {
+        const int32_t role = p.role[page];
+        if (role >= 0 && role < done) {
+            const int32_t refs = p.page_refs[page];
+            p.new_refs[p.hole[role]] = refs;
+            p.new_refs[page] = 0;
+        } else if (role >= 0 || role == kKeep || -1 - role >= done) {  // (a page that is filled is written by the one that goes there)
+            p.new_refs[page] = p.page_refs[page];
+        }
+    }
+    for (int e = first; e < p.table_len; e += stride) {
+        int32_t id = p.page_table[e];
+        if ((uint32_t)id < (uint32_t)p.num_pages) {
+            const int32_t role = p.role[id];
+            if (role >= 0 && role < done) id = p.hole[role];
+        }
+        p.new_table[e] = id;
+    }
+}
+
+// ------------------------------------------------------------------------------------------ copy, append
+struct CopyParams {
+    char *k, *v;
+    const int32_t *src, *dst;
+    int32_t n, num_pages;
+    int64_t page_bytes;
+    int32_t chunks;  // of kChunk bytes in a page
+};
+constexpr int kChunk = kThreads * 16 * 4;  // a work-group's piece of a page: four 16-byte loads in flight per thread
+
+__global__ __launch_bounds__(kThreads) void copy_pages_kernel(CopyParams p) {
+    const int64_t items = (int64_t)p.n * p.chunks * 2;
+    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+        const int i = (int)(it / (2 * p.chunks)), rest = (int)(it % (2 * p.chunks));
+        const int32_t src = p.src[i], dst = p.dst[i];
+        if ((uint32_t)src >= (uint32_t)p.num_pages || (uint32_t)dst >= (uint32_t)p.num_pages || src == dst) continue;
+        char *pool = rest & 1 ? p.v : p.k;
+        const int64_t at = (int64_t)(rest >> 1) * kChunk;
+        const char *from = pool + src * p.page_bytes + at;
+        char *to = pool + dst * p.page_bytes + at;
+        u32x4 x[4];
+        for (int j = 0; j < 4; ++j) {
+            const int64_t o = ((int64_t)j * kThreads + threadIdx.x) * 16;
+            if (at + o < p.page_bytes) x[j] = *reinterpret_cast<const u32x4 *>(from + o);
+        }
+        for (int j = 0; j < 4; ++j) {
+            const int64_t o = ((int64_t)j * kThreads + threadIdx.x) * 16;
+            if (at + o < p.page_bytes) *reinterpret_cast<u32x4 *>(to + o) = x[j];
+        }
+    }
+}
+
+struct AppendParams {
+    const char *k_new, *v_new;
+    char *k, *v;
+    const int32_t *q_indptr, *page_indptr, *page_table, *kv_len;
+    int64_t ld_bytes;  // between tokens of k_new, v_new
+    int32_t B, total_q, max_q, num_pages, table_len, page_shift, token_bytes;
+};
+constexpr int kAppendRows = 8;  // rows of a work-group
+
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendParams p) {
+    Tile t;
+    if (!find_tile(p.q_indptr, p.B, p.total_q, p.max_q, 1, kAppendRows, blockIdx.x, t)) return;
+    int e0 = max(0, min(p.page_indptr[t.b], p.table_len));
+    const int pages = max(0, min(p.page_indptr[t.b + 1], p.table_len) - e0);
+    const int64_t L = max((int64_t)0, min((int64_t)p.kv_len[t.b], (int64_t)pages << p.page_shift));
+    const int pieces = p.token_bytes / 16, rows = min(kAppendRows, t.R - t.index * kAppendRows);
+    for (int i = threadIdx.x; i < rows * pieces; i += kThreads) {
+        const int r = t.index * kAppendRows + i / pieces, piece = i % pieces;
+        const int64_t pos = L - t.R + r;
+        if (pos < 0) continue;
+        const int32_t id = p.page_table[e0 + (pos >> p.page_shift)];
+        if ((uint32_t)id >= (uint32_t)p.num_pages) continue;
+        const int64_t from = (t.q0 + r) * p.ld_bytes + (int64_t)piece * 16;
+        const int64_t to = (((int64_t)id << p.page_shift) + (pos & ((1 << p.page_shift) - 1))) * p.token_bytes + (int64_t)piece * 16;
+        const u32x4 a = *reinterpret_cast<const u32x4 *>(p.k_new + from), c = *reinterpret_cast<const u32x4 *>(p.v_new + from);
+        *reinterpret_cast<u32x4 *>(p.k + to) = a;
+        *reinterpret_cast<u32x4 *>(p.v + to) = c;
+    }
+}
+
+// ------------------------------------------------------------------------------------------ host side
+int page_blocks(int32_t num_pages) { return (int)(((int64_t)num_pages + kPagesPerBlock - 1) / kPagesPerBlock); }
+
+// 32-bit words: blocks, 64 single words, then for resize begin [B], need [B] and fresh [num_pages], for compact role
+// [num_pages], high and hole [num_pages / 2 + 1] each.
+size_t pages_words(int32_t B, int32_t num_pages) {
+    const size_t resize = (size_t)2 * B + num_pages, compact = (size_t)num_pages + 2 * ((size_t)num_pages / 2 + 1);
+    return (size_t)page_blocks(num_pages) + 64 + std::max(resize, compact);
+}
+
+respec_status_t check_state(const char *name, const void *a, const void *b, const void *c, const void *d, const void *e, int32_t B,
+                            int32_t table_len, int32_t num_pages) {
+    if (!a || !b || !c || !d || !e) return fail(RESPEC_ERR_INVALID_ARG, "%s: null pointer argument", name);
+    if (B <= 0 || table_len <= 0 || num_pages <= 0)
+        return fail(RESPEC_ERR_INVALID_ARG, "%s: sizes must be positive (B=%d page_table_len=%d num_pages=%d)", name, B, table_len, num_pages);
+    return RESPEC_OK;
+}
+
+int shift_of(int32_t page_size) {
+    if (page_size < 16 || page_size > 1024 || (page_size & (page_size - 1)) != 0) return -1;
+    return __builtin_ctz((unsigned)page_size);
+}
+
+respec_status_t check_workspace(const char *name, const void *workspace, size_t bytes, int32_t B, int32_t num_pages) {
+    const size_t need = respec_pages_workspace_bytes(B, num_pages);
+    if (!workspace || bytes < need || !aligned_to(workspace, 256))
+        return fail(RESPEC_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) needed, got %zu", name, need, workspace ? bytes : (size_t)0);
+    return RESPEC_OK;
+}
+
+respec_status_t launched(const char *name) {
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return fail(RESPEC_ERR_HIP, "%s: launch failed: %s", name, hipGetErrorString(err));
+    clear_error();
+    return RESPEC_OK;
+}
+
+}  // namespace
+}  // namespace respec
+
+extern "C" {
+
+size_t respec_pages_workspace_bytes(int32_t B, int32_t num_pages) {
+    using namespace respec;
+    if (B <= 0 || num_pages <= 0) return 0;
+    return round_up(pages_words(B, num_pages) * sizeof(int32_t), 256);
+}
+
+respec_status_t respec_pages_resize(const int32_t *want_tokens, const int32_t *page_indptr, int32_t *page_table, int32_t *page_count,
+                                    int32_t *kv_len, int32_t *page_refs, int32_t *copy_src, int32_t *copy_dst, int32_t *out_missing,
+                                    int32_t B, int32_t page_table_len, int32_t num_pages, int32_t page_size, void *workspace,
+                                    size_t workspace_bytes, void *hip_stream) {
+    using namespace respec;
+    respec_status_t st = check_state("pages_resize", page_indptr, page_table, page_count, kv_len, page_refs, B, page_table_len, num_pages);
+    if (st != RESPEC_OK) return st;
+    if (!want_tokens || !copy_src || !copy_dst || !out_missing) return fail(RESPEC_ERR_INVALID_ARG, "pages_resize: null pointer argument");
+    const int shift = shift_of(page_size);
+    if (shift < 0) return fail(RESPEC_ERR_UNSUPPORTED, "pages_resize: page size %d is not a power of two in [16, 1024]", page_size);
+    if ((int64_t)page_table_len + B >= kSplitBit)
+        return fail(RESPEC_ERR_UNSUPPORTED, "pages_resize: page_table_len + B must be below 2^30");
+    st = check_workspace("pages_resize", workspace, workspace_bytes, B, num_pages);
+    if (st != RESPEC_OK) return st;
+    ResizeParams p{};
+    p.s = {page_indptr, page_table, page_count, kv_len, page_refs, B, page_table_len, num_pages, shift};
+    p.want = want_tokens;
+    p.copy_src = copy_src;
+    p.copy_dst = copy_dst;
+    p.missing = out_missing;
+    p.blocks = page_blocks(num_pages);
+    p.total_need = static_cast<int32_t *>(workspace);
+    p.block_free = p.total_need + 64;
+    p.begin = p.block_free + p.blocks;
+    p.need = p.begin + B;
+    p.fresh = p.need + B;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    hipLaunchKernelGGL(resize_plan_kernel, dim3(p.blocks + 1), dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL(resize_rank_kernel, dim3(p.blocks), dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL(resize_apply_kernel, dim3(B), dim3(kThreads), 0, stream, p);
+    return launched("pages_resize");
+}
+
+respec_status_t respec_pages_fork(const int32_t *parent, const int32_t *page_indptr, int32_t *page_table, int32_t *page_count,
+                                  int32_t *kv_len, int32_t *page_refs, int32_t *out_missing, int32_t B, int32_t page_table_len,
+                                  int32_t num_pages, void *hip_stream) {
+    using namespace respec;
+    respec_status_t st = check_state("pages_fork", page_indptr, page_table, page_count, kv_len, page_refs, B, page_table_len, num_pages);
+    if (st != RESPEC_OK) return st;
+    if (!parent || !out_missing) return fail(RESPEC_ERR_INVALID_ARG, "pages_fork: null pointer argument");
+    ForkParams p{};
+    p.s = {page_indptr, page_table, page_count, kv_len, page_refs, B, page_table_len, num_pages, 0};
+    p.parent = parent;
+    p.missing = out_missing;
+    hipLaunchKernelGGL(fork_kernel, dim3(B), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), p);
+    return launched("pages_fork");
+}
+
+respec_status_t respec_pages_compact(const int32_t *page_table, const int32_t *page_refs, int32_t *new_page_table, int32_t *new_page_refs,
+                                     int32_t *copy_src, int32_t *copy_dst, int32_t *out_pages_end, int32_t page_table_len,
+                                     int32_t num_pages, int32_t max_moves, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    using namespace respec;
+    if (!page_table || !page_refs || !new_page_table || !new_page_refs || !copy_src || !copy_dst || !out_pages_end)
+        return fail(RESPEC_ERR_INVALID_ARG, "pages_compact: null pointer argument");
+    if (page_table_len <= 0 || num_pages <= 0 || max_moves <= 0)
+        return fail(RESPEC_ERR_INVALID_ARG, "pages_compact: sizes must be positive (page_table_len=%d num_pages=%d max_moves=%d)", page_table_len,
+                    num_pages, max_moves);
+    const respec_status_t st = check_workspace("pages_compact", workspace, workspace_bytes, 1, num_pages);
+    if (st != RESPEC_OK) return st;
+    CompactParams p{};
+    p.page_table = page_table;
+    p.page_refs = page_refs;
+    p.table_len = page_table_len;
+    p.num_pages = num_pages;
+    p.new_table = new_page_table;
+    p.new_refs = new_page_refs;
+    p.copy_src = copy_src;
+    p.copy_dst = copy_dst;
+    p.pages_end = out_pages_end;
+    p.max_moves = max_moves;
+    p.blocks = page_blocks(num_pages);
+    p.moves = static_cast<int32_t *>(workspace);
+    p.block_live = p.moves + 64;
+    p.role = p.block_live + p.blocks;
+    p.high = p.role + num_pages;
+    p.hole = p.high + num_pages / 2 + 1;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    hipLaunchKernelGGL(compact_count_kernel, dim3(p.blocks), dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL(compact_rank_kernel, dim3(p.blocks), dim3(kThreads), 0, stream, p);
+    const int64_t most = std::max({num_pages, page_table_len, max_moves});
+    hipLaunchKernelGGL(compact_apply_kernel, dim3((unsigned)std::min<int64_t>((most + kThreads - 1) / kThreads, 1024)), dim3(kThreads), 0, stream, p);
+    return launched("pages_compact");
+}
+
+respec_status_t respec_pages_copy(void *k_pages, void *v_pages, const int32_t *copy_src, const int32_t *copy_dst, int32_t n,
+                                  int32_t num_pages, int32_t page_size, int32_t Hkv, int32_t D, respec_dtype_t dt, void *hip_stream) {
+    using namespace respec;
+    if (!k_pages || !v_pages || !copy_src || !copy_dst) return fail(RESPEC_ERR_INVALID_ARG, "pages_copy: null pointer argument");
+    if (n <= 0 || num_pages <= 0 || page_size <= 0 || Hkv <= 0 || D <= 0)
+        return fail(RESPEC_ERR_INVALID_ARG, "pages_copy: sizes must be positive (n=%d num_pages=%d page_size=%d Hkv=%d D=%d)", n, num_pages, page_size, Hkv, D);
+    if (dt != RESPEC_F32 && dt != RESPEC_BF16) return fail(RESPEC_ERR_INVALID_ARG, "pages_copy: unknown dtype %d", (int)dt);
+    if (shift_of(page_size) < 0) return fail(RESPEC_ERR_UNSUPPORTED, "pages_copy: page size %d is not a power of two in [16, 1024]", page_size);
+    const int64_t token = (int64_t)Hkv * D * (dt == RESPEC_BF16 ? 2 : 4);
+    if (token % 16 != 0 || token > (1 << 24)) return fail(RESPEC_ERR_UNSUPPORTED, "pages_copy: Hkv*D*sizeof(element) must be a multiple of 16 up to 2^24");
+    if (!aligned_to(k_pages, 16) || !aligned_to(v_pages, 16)) return fail(RESPEC_ERR_INVALID_ARG, "pages_copy: k_pages and v_pages must be 16-byte aligned");
+    CopyParams p{};
+    p.k = static_cast<char *>(k_pages);
+    p.v = static_cast<char *>(v_pages);
+    p.src = copy_src;
+    p.dst = copy_dst;
+    p.n = n;
+    p.num_pages = num_pages;
+    p.page_bytes = token * page_size;
+    p.chunks = (int32_t)((p.page_bytes + kChunk - 1) / kChunk);
+    const int64_t items = (int64_t)n * p.chunks * 2;
+    hipLaunchKernelGGL(copy_pages_kernel, dim3((unsigned)std::min<int64_t>(items, 4096)), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), p);
+    return launched("pages_copy");
+}
+
+respec_status_t respec_append_paged(const void *k_new, const void *v_new, void *k_pages, void *v_pages, const int32_t *q_indptr,
+                                    const int32_t *page_indptr, const int32_t *page_table, const int32_t *kv_len, int32_t B, int32_t total_q,
+                                    int32_t max_q_per_seq, int32_t num_pages, int32_t page_table_len, int32_t page_size, int32_t Hkv,
+                                    int32_t D, int64_t ld_new, respec_dtype_t dt, void *hip_stream) {
+    using namespace respec;
+    if (!k_new || !v_new || !k_pages || !v_pages || !q_indptr || !page_indptr || !page_table || !kv_len)
+        return fail(RESPEC_ERR_INVALID_ARG, "append_paged: null pointer argument");
+    if (B <= 0 || total_q <= 0 || max_q_per_seq <= 0 || num_pages <= 0 || page_table_len <= 0 || Hkv <= 0 || D <= 0)
+        return fail(RESPEC_ERR_INVALID_ARG, "append_paged: sizes must be positive (B=%d total_q=%d)", B, total_q);
+    if (dt != RESPEC_F32 && dt != RESPEC_BF16) return fail(RESPEC_ERR_INVALID_ARG, "append_paged: unknown dtype %d", (int)dt);
+    const int shift = shift_of(page_size);
+    if (shift < 0) return fail(RESPEC_ERR_UNSUPPORTED, "append_paged: page size %d is not a power of two in [16, 1024]", page_size);
+    const int64_t esz = dt == RESPEC_BF16 ? 2 : 4, token = (int64_t)Hkv * D * esz;
+    if (ld_new < (int64_t)Hkv * D) return fail(RESPEC_ERR_INVALID_ARG, "append_paged: token stride smaller than Hkv*D");
+    if (token % 16 != 0 || token > (1 << 24) || (ld_new * esz) % 16 != 0)
+        return fail(RESPEC_ERR_UNSUPPORTED, "append_paged: tokens must be whole 16-byte pieces (Hkv*D up to 2^24 bytes, ld_new)");
+    if (!aligned_to(k_pages, 16) || !aligned_to(v_pages, 16) || !aligned_to(k_new, 16) || !aligned_to(v_new, 16))
+        return fail(RESPEC_ERR_INVALID_ARG, "append_paged: data pointers must be 16-byte aligned");
+    AppendParams p{};
+    p.k_new = static_cast<const char *>(k_new);
+    p.v_new = static_cast<const char *>(v_new);
+    p.k = static_cast<char *>(k_pages);
+    p.v = static_cast<char *>(v_pages);
+    p.q_indptr = q_indptr;
+    p.page_indptr = page_indptr;
+    p.page_table = page_table;
+    p.kv_len = kv_len;
+    p.ld_bytes = ld_new * esz;
+    p.B = B;
+    p.total_q = total_q;
+    p.max_q = max_q_per_seq;
+    p.num_pages = num_pages;
+    p.table_len = page_table_len;
+    p.page_shift = shift;
+    p.token_bytes = (int32_t)token;
+    const int64_t grid = tiles_bound(B, total_q, max_q_per_seq, 1, kAppendRows);
+    if (grid > 0x7fffffff) return fail(RESPEC_ERR_UNSUPPORTED, "append_paged: too many rows");
+    hipLaunchKernelGGL(append_kernel, dim3((unsigned)grid), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), p);
+    return launched("append_paged");
+}
+
+}  // extern "C"
