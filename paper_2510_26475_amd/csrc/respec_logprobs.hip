@@ -5,9 +5,10 @@
 // t = sum e^{(x-m)/T} (x-m)/T over its pieces, and
 //     lse = m/T + ln s,   H = ln s - t/s,   log p(x) = x/T - lse,
 // so that neither needs the row's maximum beforehand and the entropy is a difference of small numbers.  The reference is moved only
-// where a value lies 2^20 above it.  The N best logits are kept as 64-bit keys (the value in an order-preserving form, the
-// complement of the token id), sorted over the lanes of a wave: a piece whose largest value is below the N-th key costs one
-// comparison.  Bound by HBM (a row is read once); few rows are cut into parts that a second kernel joins in a fixed order.
+// where a value lies 2^20 above it.  For the N best logits a wave keeps the maxima of its groups of pieces (128 bytes each, in a
+// vocabulary of 151,936): the N groups with the largest ones hold its N best logits, so after the pass those few are read again,
+// and the waves' best are ranked by counting, as 64-bit keys of the value in an order-preserving form and the complement of the
+// token id.  Bound by HBM (a row is read once); few rows are cut into parts that a second kernel joins in a fixed order.
 //
 // Gradient.  Reads a row and writes its gradient once, from the lse and H of the forward pass; no statistics.  Bound by HBM.
 //
@@ -16,6 +17,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace respec {
 namespace {
@@ -26,6 +28,10 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kUnroll = 4;          // pieces in flight per thread
 constexpr int kMaxTop = 64;         // alternatives of a row: one per lane
 constexpr int kMaxParts = 64;       // parts of a row: one per lane of the wave that joins them
+constexpr int kGroups = 640;        // groups of pieces whose maxima a wave keeps
+constexpr int kChosen = 64;         // groups of them that are read again
+constexpr int kCandidates = 256;    // keys of a wave that are ranked
+constexpr int kJoin = 512;          // keys of a row's parts that are ranked
 constexpr int kFill = 1024;         // work-groups that a call is cut into where it has fewer rows
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kSlack = 20.f;      // log2 units that a value may lie above its thread's reference
@@ -93,35 +99,25 @@ template <bool BF16>
 struct Row {
     const void *base;
     int32_t off, V, pieces;
+    int32_t whole_from, whole_to;  // the pieces that lie in the row as a whole
     __device__ Row(const void *logits, int64_t row, int64_t ld, int32_t v) {
         using E = Elem<BF16>;
         base = static_cast<const char *>(logits) + row * ld * E::kSize;
         off = (int32_t)((reinterpret_cast<uintptr_t>(base) & 15) / E::kSize);
         V = v;
         pieces = (int32_t)(((int64_t)off + V + E::kPer - 1) / E::kPer);
+        whole_from = off != 0;
+        whole_to = (int32_t)(((int64_t)off + V) / E::kPer);
     }
     __device__ int64_t first(int i) const { return (int64_t)i * Elem<BF16>::kPer - off; }
-    __device__ bool whole(int i) const { return first(i) >= 0 && first(i) + Elem<BF16>::kPer <= V; }
+    __device__ bool whole(int i) const { return i >= whole_from && i < whole_to; }
     __device__ const u32x4 *at(int i) const {
         return reinterpret_cast<const u32x4 *>(static_cast<const char *>(base) + first(i) * Elem<BF16>::kSize);
     }
-    // The piece's bits; elements outside the row (at its ends) are -inf.
-    __device__ u32x4 load(int i) const {
-        using E = Elem<BF16>;
-        if (whole(i)) return *at(i);
-        u32x4 raw;
-        for (int w = 0; w < 4; ++w) raw[w] = BF16 ? 0xff80ff80u : 0xff800000u;
-        for (int j = 0; j < E::kPer; ++j) {
-            const int64_t e = first(i) + j;
-            if (e < 0 || e >= V) continue;
-            if constexpr (BF16) {
-                const uint32_t x = static_cast<const uint16_t *>(base)[e];
-                raw[j / 2] = j % 2 ? (raw[j / 2] & 0xffffu) | x << 16 : (raw[j / 2] & 0xffff0000u) | x;
-            } else {
-                raw[j] = static_cast<const uint32_t *>(base)[e];
-            }
-        }
-        return raw;
+    __device__ int edges() const { return V - max(0, whole_to - whole_from) * Elem<BF16>::kPer; }  // elements in no whole piece
+    __device__ int edge(int i) const {  // the i-th of them
+        const int head = whole_to > whole_from ? whole_from * Elem<BF16>::kPer - off * (whole_from != 0) : V;
+        return i < head ? i : V - edges() + i;
     }
 };
 
@@ -144,6 +140,33 @@ __device__ inline Sums join(Sums a, Sums b, float scale) {
     if (a.ref != ref) move_to(a, ref, scale);
     if (b.ref != ref) move_to(b, ref, scale);
     return {ref, a.s + b.s, a.t + b.t};
+}
+
+// Over the lanes of a wave, in a fixed tree; everybody's result.  `zero` is the operation's neutral value.
+template <typename T, typename OP>
+__device__ inline T wave_reduce(T x, T zero, OP op) {
+    auto from = [&](T y, auto ctrl, auto rows) __attribute__((always_inline)) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, zero), __builtin_bit_cast(int, y), decltype(ctrl)::value,
+                                                                 decltype(rows)::value, 0xf, false));
+    };
+    using std::integral_constant;
+    const integral_constant<int, 0xf> all{};
+    x = op(x, from(x, integral_constant<int, 0x111>{}, all));                          // row_shr:1
+    x = op(x, from(x, integral_constant<int, 0x112>{}, all));                          // row_shr:2
+    x = op(x, from(x, integral_constant<int, 0x114>{}, all));                          // row_shr:4
+    x = op(x, from(x, integral_constant<int, 0x118>{}, all));                          // row_shr:8
+    x = op(x, from(x, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{}));  // row_bcast:15
+    x = op(x, from(x, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{}));  // row_bcast:31
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+__device__ inline uint32_t wave_max(uint32_t x) {
+    return wave_reduce(x, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+__device__ inline Sums join_wave(Sums a, float scale) {
+    const float ref = wave_reduce(a.ref, (float)-INFINITY, [](float x, float y) { return fmaxf(x, y); });
+    if (a.ref != ref) move_to(a, ref, scale);
+    const auto add = [](float x, float y) { return x + y; };
+    return {ref, wave_reduce(a.s, 0.f, add), wave_reduce(a.t, 0.f, add)};
 }
 
 __device__ inline uint64_t make_key(float x, int32_t token) {
@@ -170,26 +193,12 @@ __device__ inline uint64_t from_lane_before(uint64_t x) {  // (lane 0 keeps its 
 // The best keys of a wave, descending over its lanes; 0 = none.
 struct Best {
     uint64_t list, floor;  // floor: the N-th (0 while there are fewer)
-    float floor_value;
-    int32_t floor_token;
-    __device__ void start() {
-        list = floor = 0;
-        floor_value = -INFINITY;
-        floor_token = INT32_MAX;
-    }
+    __device__ void start() { list = floor = 0; }
     __device__ void insert(uint64_t key, int top) {
         const int rank = __popcll(__ballot(list > key)), lane = threadIdx.x & 63;
         const uint64_t before = from_lane_before(list);
         list = lane < rank ? list : lane == rank ? key : before;
         floor = read_lane(list, top - 1);
-        if (floor != 0) {
-            floor_value = key_value(floor);
-            floor_token = key_token(floor);
-        }
-    }
-    // Whether a piece with this largest value, its first element being `first`, can hold a key above the floor.
-    __device__ bool may_hold(float largest, int32_t first) const {
-        return largest > floor_value || (largest == floor_value && first < floor_token) || floor == 0;
     }
 };
 
@@ -223,14 +232,146 @@ __device__ inline void write_unused(const LogprobParams &p, int row) {
     }
 }
 
+__device__ inline uint32_t order_of(float x) { return (uint32_t)(make_key(x, 0) >> 32); }
+__device__ inline int bits_below(uint64_t mask) {  // set bits of lanes before this one
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// How the pieces of a part are dealt out: chunks of 64 `deep` pieces, chunk c to wave c % kWaves; an octet of lanes (or a lane, `wide` =
+// 1) owns a run of wide * deep pieces of a chunk, its group.
+struct Deal {
+    int32_t begin, end, deep, wide;
+    int32_t chunks;  // of this wave
+    __device__ Deal(int b, int e, int wave) : begin(b), end(e) {
+        const int per_wave = (e - b + 64 * kWaves - 1) / (64 * kWaves);  // steps of a wave, one piece per lane each
+        wide = per_wave <= kGroups / 64 ? 1 : 8;
+        deep = wide == 1 ? 1 : (per_wave * 8 + kGroups - 1) / kGroups;
+        const int all = (e - b + 64 * deep - 1) / (64 * deep);
+        chunks = (all - wave + kWaves - 1) / kWaves;
+    }
+    __device__ int groups() const { return chunks * (64 / wide); }
+    __device__ int piece(int group, int wave, int within) const {  // of a group
+        const int chunk = group / (64 / wide), at = group % (64 / wide);
+        return begin + ((chunk * kWaves + wave) * 64 + at * wide) * deep + within;
+    }
+};
+
+// The best keys among a wave's groups: the `top` groups with the largest maxima hold them (of groups with equal maxima the first
+// ones), so only those, or a few more, are read again.  Leaves them, unsorted and with a few more, in `cand`; returns their number.
+template <bool BF16>
+__device__ inline int best_of_groups(const Row<BF16> &r, const Deal &deal, int wave, int top, const float *maxima, int32_t *chosen, uint64_t *cand,
+                                     int held, float &floor) {
+    using E = Elem<BF16>;
+    const int lane = threadIdx.x & 63, n = deal.groups();
+    uint32_t x[kGroups / 64];  // (0: no group)
+#pragma unroll
+    for (int j = 0; j < kGroups / 64; ++j) x[j] = j * 64 + lane < n ? order_of(maxima[j * 64 + lane]) : 0u;
+    // A value that `top` lanes' own maxima reach: bit by bit, by the upper half alone for bf16, which is all there is to its order.
+    constexpr int kLast = BF16 ? 16 : 0;
+    uint32_t mine = 0, least = 0;
+#pragma unroll
+    for (int j = 0; j < kGroups / 64; ++j) mine = max(mine, x[j]);
+    for (int bit = 31; bit >= kLast; --bit) {
+        const int c = (int)__popcll(__ballot(mine >= (least | 1u << bit)));
+        if (c < top) continue;
+        least |= 1u << bit;
+        if (c == top) break;
+    }
+    auto count = [&](uint32_t from) __attribute__((always_inline)) {
+        int c = 0;
+#pragma unroll
+        for (int j = 0; j < kGroups / 64; ++j)
+            if (j * 64 < n) c += (int)__popcll(__ballot(x[j] >= from));
+        return c;
+    };
+    least = max(least, 1u);
+    int ties = INT32_MAX, sel = 0;
+    if (count(least) > kChosen) {  // Too many groups reach it: the top-th largest maximum of all.
+        int found = 0;
+        least = 0;
+        for (int bit = 31; bit >= kLast; --bit) {
+            const int c = count(least | 1u << bit);
+            if (c < top) continue;
+            least |= 1u << bit;
+            found = c;
+            if (c == top) break;
+        }
+        least = max(least, 1u);
+        if (found != top) ties = top - count(least + (1u << kLast));
+    }
+#pragma unroll
+    for (int j = 0; j < kGroups / 64; ++j)
+        if (j * 64 < n) {
+            const bool at = (x[j] ^ least) >> kLast == 0;
+            const uint64_t equal = __ballot(at);
+            const bool take = x[j] >= least && (!at || bits_below(equal) < ties);
+            const uint64_t taken = __ballot(take);
+            if (take) chosen[sel + bits_below(taken)] = j * 64 + lane;
+            sel += (int)__popcll(taken);
+            if (ties != INT32_MAX) ties = max(0, ties - (int)__popcll(equal));
+        }
+    floor = key_value((uint64_t)least << 32);
+    const int run = deal.wide * deal.deep, pieces = sel * run;
+    int kept = held;
+    for (int q0 = 0; q0 < pieces; q0 += 64) {
+        const int q = q0 + lane;
+        const int i = q < pieces ? deal.piece(chosen[q / run], wave, q % run) : deal.end;
+        u32x4 raw{};
+        if (i < deal.end) raw = *r.at(i);
+        float v[E::kPer];
+        unpack<BF16>(raw, v);
+        const int32_t first = (int32_t)r.first(i);
+#pragma unroll
+        for (int j = 0; j < E::kPer; ++j) {
+            const int32_t e = first + j;
+            const bool take = i < deal.end && !(v[j] < floor);
+            const uint64_t taken = __ballot(take);
+            if (taken == 0) continue;
+            const int to = kept + bits_below(taken);
+            if (take && to < kCandidates) cand[to] = make_key(v[j], e);
+            kept += (int)__popcll(taken);
+        }
+    }
+    if (kept <= kCandidates) return kept;
+    // Too many equal ones: one at a time into a sorted list.
+    Best best;
+    best.start();
+    for (int i = 0; i < held; ++i) best.insert(cand[i], top);
+    for (int q0 = 0; q0 < pieces; q0 += 64) {
+        const int q = q0 + lane;
+        const int i = q < pieces ? deal.piece(chosen[q / run], wave, q % run) : deal.end;
+        u32x4 raw{};
+        if (i < deal.end) raw = *r.at(i);
+        float v[E::kPer];
+        unpack<BF16>(raw, v);
+        const int32_t first = (int32_t)r.first(i);
+        for (int j = 0; j < E::kPer; ++j) {
+            const int32_t e = first + j;
+            const uint64_t key = i < deal.end ? make_key(v[j], e) : 0;
+            uint64_t todo = __ballot(key > best.floor);
+            while (todo) {
+                best.insert(read_lane(key, __builtin_ctzll(todo)), top);
+                todo &= todo - 1;
+                todo &= __ballot(key > best.floor);
+            }
+        }
+    }
+    if (lane < top) cand[lane] = best.list;
+    return top;
+}
+
 // One work-group per part of a row.
 template <bool BF16, bool TOP>
 __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobParams p) {
     using E = Elem<BF16>;
     __shared__ Sums sh_sums[kWaves];
-    __shared__ uint64_t sh_top[TOP ? kWaves * kMaxTop : 1];
+    __shared__ float sh_maxima[TOP ? kWaves * kGroups : 1];
+    __shared__ int32_t sh_chosen[TOP ? kWaves * kChosen : 1];
+    __shared__ uint64_t sh_cand[TOP ? kWaves * kCandidates : 1];
+    __shared__ int sh_kept[kWaves], sh_left;
+    __shared__ float sh_floor[kWaves];
     const int row = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int32_t token = p.tokens[row];
     if ((uint32_t)token >= (uint32_t)p.V) {
         if (p.parts == 1) write_unused(p, row);
@@ -240,23 +381,42 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobParams p) {
     const float scale = row_scale_of<BF16>(p, row, inv_t);
     const Row<BF16> r(p.logits, row, p.ld, p.V);
     const float token_logit = load_one<BF16>(r.base, token);
-    const int begin = (int)((int64_t)r.pieces * part / p.parts), end = (int)((int64_t)r.pieces * (part + 1) / p.parts);
+    const int whole = max(0, r.whole_to - r.whole_from);
+    const Deal deal(r.whole_from + (int)((int64_t)whole * part / p.parts), r.whole_from + (int)((int64_t)whole * (part + 1) / p.parts), wave);
 
     Sums a{-INFINITY, 0.f, 0.f};
-    float used = 0.f;  // the reference, or 0 while there is none
-    Best best;
-    if constexpr (TOP) best.start();
-    const float slack = kSlack / scale;
-    for (int i0 = begin; i0 < end; i0 += kThreads * kUnroll) {
-        u32x4 raw[kUnroll];
-        for (int u = 0; u < kUnroll; ++u) {
-            const int i = i0 + u * kThreads + threadIdx.x;
-            if (i < end) raw[u] = r.load(i);
-            else
-                for (int w = 0; w < 4; ++w) raw[u][w] = BF16 ? 0xff80ff80u : 0xff800000u;
+    int held = 0;
+    if (part == 0 && wave == 0) {  // the elements before and behind the whole pieces, one per lane
+        held = r.edges();
+        if (lane < held) {
+            const int e = r.edge(lane);
+            const float x = load_one<BF16>(r.base, e);
+            if (x > -INFINITY) a = {x, 1.f, 0.f};
+            if (!(x < INFINITY)) a.s = NAN;
+            if constexpr (TOP) sh_cand[lane] = make_key(x, e);
         }
+    }
+    float used = a.ref > -INFINITY ? a.ref : 0.f, used_log2 = used * scale;  // the reference, or 0 while there is none; in log2 units
+    float group_max = -INFINITY;
+    const float slack = kSlack / scale;
+    const int steps = deal.chunks * deal.deep, lane_at = (lane / deal.wide) * deal.wide * deal.deep + lane % deal.wide;
+    // (a load in a branch would have to be waited for with all that are on their way, so all lanes load, the last piece if need be)
+    int chunk = 0, within = 0;      // of the next step to be requested
+    int chunk_at = 0, within_at = 0, done = 0;  // of the next one to be worked on; groups done
+    auto request = [&](u32x4(&raw)[kUnroll]) __attribute__((always_inline)) {
         for (int u = 0; u < kUnroll; ++u) {
-            const int i = i0 + u * kThreads + threadIdx.x;
+            const int i = deal.begin + (chunk * kWaves + wave) * 64 * deal.deep + within * deal.wide + lane_at;
+            raw[u] = *r.at(min(i, deal.end - 1));
+            if (++within == deal.deep) within = 0, chunk = min(chunk + 1, deal.chunks);
+        }
+    };
+    auto work = [&](u32x4(&raw)[kUnroll], int f0) __attribute__((always_inline)) {
+        for (int u = 0; u < kUnroll; ++u) {
+            if (f0 + u >= steps) break;  // (uniform)
+            const int first = deal.begin + (chunk_at * kWaves + wave) * 64 * deal.deep;
+            if (first + 64 * deal.deep > deal.end)  // (uniform: the last chunk)
+                if (first + within_at * deal.wide + lane_at >= deal.end)
+                    for (int w = 0; w < 4; ++w) raw[u][w] = BF16 ? 0xff80ff80u : 0xff800000u;
             float v[E::kPer];
             unpack<BF16>(raw[u], v);
             float largest = v[0];
@@ -264,40 +424,66 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobParams p) {
             if (largest > a.ref + slack || (a.ref == -INFINITY && largest > -INFINITY)) {
                 move_to(a, largest, scale);
                 used = largest;
+                used_log2 = used * scale;
             }
             float s = 0.f, t = 0.f;
-            for (int j = 0; j < E::kPer; ++j) {
-                const float d = (v[j] - used) * scale, e = __builtin_amdgcn_exp2f(d);
-                s += e;
-                t += e * fmaxf(d, kFar);
+            if (__ballot(!(fabsf(used_log2) < 1e30f)) == 0) {
+                // (the reference's product with the scale is rounded: a step of lse, which is rounded itself)
+                for (int j = 0; j < E::kPer; ++j) {
+                    const float d = fmaf(v[j], scale, -used_log2), e = __builtin_amdgcn_exp2f(d);
+                    s += e;
+                    t += e * fmaxf(d, kFar);
+                }
+            } else {  // logits of the type's lowest value, or a temperature that takes them there
+                for (int j = 0; j < E::kPer; ++j) {
+                    const float d = (v[j] - used) * scale, e = __builtin_amdgcn_exp2f(d);
+                    s += e;
+                    t += e * fmaxf(d, kFar);
+                }
             }
             a.s += s;
             a.t += t;
             if constexpr (TOP) {
-                const int32_t first = (int32_t)r.first(i);
-                if (__ballot(i < end && best.may_hold(largest, first)) != 0) {
-                    for (int j = 0; j < E::kPer; ++j) {
-                        const int32_t e = first + j;
-                        const uint64_t key = make_key(v[j], e);
-                        uint64_t todo = __ballot(i < end && e >= 0 && e < p.V && key > best.floor);
-                        while (todo) {
-                            const int from = __builtin_ctzll(todo);
-                            best.insert(read_lane(key, from), p.top);
-                            todo &= todo - 1;
-                            todo &= __ballot(key > best.floor);
-                        }
+                if (deal.wide == 1) {
+                    sh_maxima[wave * kGroups + (f0 + u) * 64 + lane] = largest;
+                } else {
+                    group_max = fmaxf(group_max, largest);
+                    if (within_at + 1 == deal.deep) {
+                        float m = group_max;  // over the octet: lanes ^ 1, ^ 2, and the mirrored half row
+                        m = fmaxf(m, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(m), 0xb1, 0xf, 0xf, true)));
+                        m = fmaxf(m, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(m), 0x4e, 0xf, 0xf, true)));
+                        m = fmaxf(m, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(m), 0x141, 0xf, 0xf, true)));
+                        if ((lane & 7) == 0) sh_maxima[wave * kGroups + done * 8 + lane / 8] = m;
+                        ++done;
+                        group_max = -INFINITY;
                     }
                 }
             }
+            if (++within_at == deal.deep) within_at = 0, ++chunk_at;
+        }
+    };
+    u32x4 even[kUnroll], odd[kUnroll];  // a batch is worked on while the next one is on its way
+    if (steps > 0) request(even);
+    for (int f0 = 0; f0 < steps; f0 += 2 * kUnroll) {
+        request(odd);
+        work(even, f0);
+        if (f0 + kUnroll >= steps) break;
+        request(even);
+        work(odd, f0 + kUnroll);
+    }
+    a = join_wave(a, scale);
+    if (lane == 0) sh_sums[wave] = a;
+    if (threadIdx.x == 0) sh_left = 0;
+    float floor = -INFINITY;
+    if constexpr (TOP) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const int kept = best_of_groups<BF16>(r, deal, wave, p.top, sh_maxima + wave * kGroups, sh_chosen + wave * kChosen, sh_cand + wave * kCandidates, held, floor);
+        if (lane == 0) {
+            sh_kept[wave] = kept;
+            sh_floor[wave] = floor;
         }
     }
-    for (int step = 1; step < 64; step *= 2) {
-        const Sums b{__shfl_xor(a.ref, step), __shfl_xor(a.s, step), __shfl_xor(a.t, step)};
-        a = lane & step ? join(b, a, scale) : join(a, b, scale);
-    }
-    if (lane == 0) sh_sums[wave] = a;
-    if constexpr (TOP)
-        if (lane < p.top) sh_top[wave * p.top + lane] = best.list;
     __syncthreads();
     a = sh_sums[0];
     for (int w = 1; w < kWaves; ++w) a = join(a, sh_sums[w], scale);
@@ -311,35 +497,41 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobParams p) {
             p.part_sums[slot * 4 + 2] = a.t;
         }
     }
-    if constexpr (TOP) {  // a key's place is the number of keys above it
-        const int n = kWaves * p.top, tid = threadIdx.x;
-        int present = 0, rank = 0;
-        const uint64_t mine = tid < n ? sh_top[tid] : 0;
-        for (int i = 0; i < n; ++i) {
-            rank += sh_top[i] > mine;
-            present += sh_top[i] != 0;
+    if constexpr (TOP) {
+        // what the highest of the waves' floors leaves, together; then a key's place is the number of keys above it
+        for (int w = 0; w < kWaves; ++w) floor = fmaxf(floor, sh_floor[w]);
+        uint64_t *const left = reinterpret_cast<uint64_t *>(sh_maxima);
+        static_assert(!TOP || sizeof(sh_maxima) >= sizeof(sh_cand), "room for all");
+        for (int c = lane; c < sh_kept[wave]; c += 64) {
+            const uint64_t key = sh_cand[wave * kCandidates + c];
+            if (key != 0 && !(key_value(key) < floor)) left[atomicAdd(&sh_left, 1)] = key;  // (in any order)
         }
-        if (tid < n && mine != 0 && rank < p.top) {
-            if (p.parts == 1) write_top(p, row, rank, mine, a, inv_t);
-            else p.part_top[slot * p.top + rank] = mine;
+        __syncthreads();
+        const int n = sh_left;
+        for (int c = threadIdx.x; c < n; c += kThreads) {
+            const uint64_t mine = left[c];
+            int rank = 0;
+            for (int i = 0; i < n; ++i) rank += left[i] > mine;
+            if (rank < p.top) {
+                if (p.parts == 1) write_top(p, row, rank, mine, a, inv_t);
+                else p.part_top[slot * p.top + rank] = mine;
+            }
         }
-        if (tid < p.top && tid >= present) {
-            if (p.parts == 1) write_top(p, row, tid, 0, a, inv_t);
-            else p.part_top[slot * p.top + tid] = 0;
+        if ((int)threadIdx.x < p.top && (int)threadIdx.x >= n) {  // fewer elements than places
+            if (p.parts == 1) write_top(p, row, threadIdx.x, 0, a, inv_t);
+            else p.part_top[slot * p.top + threadIdx.x] = 0;
         }
     }
 }
 
-__device__ inline uint32_t wave_max(uint32_t x) {
-    for (int step = 1; step < 64; step *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, step));
-    return x;
-}
-
-// The parts of a row, one per lane: sums in a fixed tree, alternatives by taking the best head of the sorted lists N times.
+// Joins the parts of a row.  Sums: a part per lane, in a fixed tree.  Alternatives: the sorted lists' first entries give a value that
+// the top-th best is not below, the few keys from there on are ranked by counting.
 template <bool BF16>
-__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobParams p) {
-    __shared__ uint64_t sh_top[kMaxTop];
-    const int row = blockIdx.x, lane = threadIdx.x;
+__global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobParams p) {
+    extern __shared__ uint64_t keys[];  // [parts][top], then kJoin candidates
+    __shared__ int sh_kept;
+    __shared__ Sums sh_sums;
+    const int row = blockIdx.x, lane = threadIdx.x & 63, top = p.top;
     const int32_t token = p.tokens[row];
     if ((uint32_t)token >= (uint32_t)p.V) {
         write_unused(p, row);
@@ -347,27 +539,68 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobParams p) {
     }
     float inv_t;
     const float scale = row_scale_of<BF16>(p, row, inv_t);
-    const float token_logit = load_one<BF16>(static_cast<const char *>(p.logits) + (int64_t)row * p.ld * Elem<BF16>::kSize, token);
-    const int64_t slot = (int64_t)row * p.parts + lane;
-    Sums a{-INFINITY, 0.f, 0.f};
-    if (lane < p.parts) a = {p.part_sums[slot * 4], p.part_sums[slot * 4 + 1], p.part_sums[slot * 4 + 2]};
-    uint64_t head = 0;
-    int next = 1;
-    if (p.top > 0 && lane < p.parts) head = p.part_top[slot * p.top];
-    for (int step = 1; step < 64; step *= 2) {
-        const Sums b{__shfl_xor(a.ref, step), __shfl_xor(a.s, step), __shfl_xor(a.t, step)};
-        a = lane & step ? join(b, a, scale) : join(a, b, scale);
+    const int64_t slot = (int64_t)row * p.parts;
+    const int all = p.parts * top;
+    for (int i = threadIdx.x; i < all; i += kThreads) keys[i] = p.part_top[slot * top + i];
+    if (threadIdx.x < 64) {
+        const float token_logit = load_one<BF16>(static_cast<const char *>(p.logits) + (int64_t)row * p.ld * Elem<BF16>::kSize, token);
+        Sums a{-INFINITY, 0.f, 0.f};
+        if (lane < p.parts) a = {p.part_sums[(slot + lane) * 4], p.part_sums[(slot + lane) * 4 + 1], p.part_sums[(slot + lane) * 4 + 2]};
+        a = join_wave(a, scale);
+        if (lane == 0) {
+            write_row(p, row, a, token_logit, inv_t);
+            sh_sums = a;
+            sh_kept = 0;
+        }
     }
-    if (lane == 0) write_row(p, row, a, token_logit, inv_t);
-    for (int i = 0; i < p.top; ++i) {
+    if (top == 0) return;
+    __syncthreads();
+    uint64_t *cand = keys + all;
+    // the top-th best of the first `deep` entries of every list (at most 64 + 63 keys), by every wave
+    const int deep = (top + p.parts - 1) / p.parts, firsts = deep * p.parts;
+    uint32_t x[2];
+    for (int j = 0; j < 2; ++j) {
+        const int q = j * 64 + lane;
+        x[j] = q < firsts ? (uint32_t)(keys[q / deep * top + q % deep] >> 32) : 0;
+    }
+    uint32_t least = 0;
+    for (int bit = 31; bit >= (BF16 ? 16 : 0); --bit) {
+        const uint32_t c = least | 1u << bit;
+        const int n = (int)__popcll(__ballot(x[0] >= c)) + (int)__popcll(__ballot(x[1] >= c));
+        if (n < top) continue;
+        least = c;
+        if (n == top) break;
+    }
+    for (int i = threadIdx.x; i < all; i += kThreads)
+        if (keys[i] != 0 && (uint32_t)(keys[i] >> 32) >= least) {
+            const int to = atomicAdd(&sh_kept, 1);  // (any order: the ranks are the keys')
+            if (to < kJoin) cand[to] = keys[i];
+        }
+    __syncthreads();
+    const int kept = sh_kept;
+    const Sums a = sh_sums;
+    if (kept <= kJoin) {
+        for (int c = threadIdx.x; c < kept; c += kThreads) {
+            const uint64_t mine = cand[c];
+            int rank = 0;
+            for (int i = 0; i < kept; ++i) rank += cand[i] > mine;
+            if (rank < top) write_top(p, row, rank, mine, a, inv_t);
+        }
+        if ((int)threadIdx.x < top && (int)threadIdx.x >= kept) write_top(p, row, threadIdx.x, 0, a, inv_t);
+        return;
+    }
+    // The best keys lie in few lists: the best head of all lists, `top` times.
+    if (threadIdx.x >= 64) return;
+    uint64_t head = lane < p.parts ? keys[lane * top] : 0, kept_key = 0;
+    int next = 1;
+    for (int i = 0; i < top; ++i) {
         const uint32_t hi = wave_max((uint32_t)(head >> 32));
         const uint32_t lo = wave_max((uint32_t)(head >> 32) == hi ? (uint32_t)head : 0u);
         const uint64_t key = (uint64_t)hi << 32 | lo;
-        if (lane == 0) sh_top[i] = key;
-        if (key != 0 && head == key) head = next < p.top ? p.part_top[slot * p.top + next++] : 0;
+        if (lane == i) kept_key = key;
+        if (key != 0 && head == key) head = next < top ? keys[lane * top + next++] : 0;
     }
-    __syncthreads();
-    if (lane < p.top) write_top(p, row, lane, sh_top[lane], a, inv_t);
+    if (lane < top) write_top(p, row, lane, kept_key, a, inv_t);
 }
 
 // ------------------------------------------------------------------------------------------ gradient
@@ -405,26 +638,22 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradParams p) {
         u32x4 raw[kUnroll];
         if (!unused)
             for (int u = 0; u < kUnroll; ++u)
-                if (i0 + u * kThreads < r.pieces) raw[u] = r.load(i0 + u * kThreads);
+                if (r.whole(i0 + u * kThreads)) raw[u] = *r.at(i0 + u * kThreads);
         for (int u = 0; u < kUnroll; ++u) {
             const int i = i0 + u * kThreads;
             if (i >= r.pieces) break;
             const int64_t first = r.first(i);
-            float v[E::kPer];
-            if (unused)
-                for (int j = 0; j < E::kPer; ++j) v[j] = 0.f;
-            else {
-                unpack<BF16>(raw[u], v);
-                for (int j = 0; j < E::kPer; ++j) v[j] = g.at(v[j], first + j);
-            }
             if (r.whole(i)) {
+                float v[E::kPer];
+                unpack<BF16>(raw[u], v);
+                for (int j = 0; j < E::kPer; ++j) v[j] = unused ? 0.f : g.at(v[j], first + j);
                 u32x4 w;
                 for (int j = 0; j < 4; ++j)
                     w[j] = BF16 ? bf16_bits(v[2 * j]) | bf16_bits(v[(2 * j + 1) % E::kPer]) << 16 : __float_as_uint(v[j]);
                 *reinterpret_cast<u32x4 *>(out + first * E::kSize) = w;
             } else {
-                for (int j = 0; j < E::kPer; ++j)
-                    if (first + j >= 0 && first + j < p.V) store_one<BF16>(out, first + j, v[j]);
+                for (int64_t e = max(first, (int64_t)0); e < min(first + E::kPer, (int64_t)p.V); ++e)
+                    store_one<BF16>(out, e, unused ? 0.f : g.at(load_one<BF16>(r.base, e), e));
             }
         }
     } else {
@@ -450,7 +679,7 @@ void launch_forward(const LogprobParams &p, hipStream_t stream) {
     const dim3 grid((unsigned)((int64_t)p.rows * p.parts));
     if (p.top > 0) hipLaunchKernelGGL((logprob_kernel<BF16, true>), grid, dim3(kThreads), 0, stream, p);
     else hipLaunchKernelGGL((logprob_kernel<BF16, false>), grid, dim3(kThreads), 0, stream, p);
-    if (p.parts > 1) hipLaunchKernelGGL((logprob_join_kernel<BF16>), dim3(p.rows), dim3(64), 0, stream, p);
+    if (p.parts > 1) hipLaunchKernelGGL((logprob_join_kernel<BF16>), dim3(p.rows), dim3(kThreads), ((size_t)p.parts * p.top + (p.top ? kJoin : 0)) * sizeof(uint64_t), stream, p);
 }
 
 respec_status_t check_rows(const char *name, int32_t rows, int32_t V, int64_t ld, float temperature, bool per_row, respec_dtype_t dt,
