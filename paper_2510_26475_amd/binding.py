@@ -572,27 +572,39 @@ def respec_kd_rows(target_logits, draft_logits, row_weight, grad, row_loss, tota
         _stream_ptr(stream)))
 
 
-def _here(first, **tensors):
-    """Every tensor (None: absent) lives on the device of `first`, and that is the current one: the stream is its."""
-    if not first.is_cuda or first.device.index != torch.cuda.current_device():
+# (As above: torch.cuda.current_device() takes 0.5 us of a call's 6 to 10, this 0.1.)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _here(first, *others):
+    """The index of the current GPU, on which `first` and the others (None: absent) have to live: the stream is its."""
+    index = first.get_device()
+    if index < 0 or index != _current_device():
         raise ValueError(f"tensors must live on the current GPU (got {first.device})")
-    for name, t in tensors.items():
-        if t is not None and t.device != first.device:
-            raise ValueError(f"{name} must live on {first.device} (got {t.device})")
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"all tensors must live on {first.device} (got one on {t.device})")
+    return index
 
 
-def _ints(n, **tensors):
+def _stream_on(index, stream):
+    if stream is not None or _current_raw_stream is None:
+        return _stream_ptr(stream)
+    return _current_raw_stream(index)
+
+
+def _ints(n, names, *tensors):
     """Contiguous int32 tensors of n elements (None: any number)."""
-    for name, t in tensors.items():
-        if t.dtype != torch.int32 or (n is not None and t.numel() != n) or not t.is_contiguous():
-            raise TypeError(f"{name} must be contiguous int32" + ("" if n is None else f" [{n}]"))
+    for i, t in enumerate(tensors):
+        if t.dtype is not torch.int32 or (n is not None and t.numel() != n) or not t.is_contiguous():
+            raise TypeError(f"{names.split()[i]} must be contiguous int32" + ("" if n is None else f" [{n}]"))
 
 
-def _floats(n, **tensors):
+def _floats(n, names, *tensors):
     """Contiguous float32 tensors of n elements; None may stand for an absent one."""
-    for name, t in tensors.items():
-        if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
-            raise TypeError(f"{name} must be contiguous float32 [{n}]")
+    for i, t in enumerate(tensors):
+        if t is not None and (t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous()):
+            raise TypeError(f"{names.split()[i]} must be contiguous float32 [{n}]")
 
 
 def _ptr(t):
@@ -623,19 +635,19 @@ def respec_prompt_attention(q, k, v, q_indptr, kv_indptr, out, lse, max_q_per_se
     total_q, Hq, D = q.shape
     total_kv, Hkv, _ = k.shape
     B = q_indptr.numel() - 1
-    _here(q, k=k, v=v, q_indptr=q_indptr, kv_indptr=kv_indptr, out=out, lse=lse, workspace=workspace)
-    _ints(B + 1, q_indptr=q_indptr)
+    index = _here(q, k, v, q_indptr, kv_indptr, out, lse, workspace)
+    _ints(B + 1, "q_indptr", q_indptr)
     if kv_indptr.dtype != torch.int64 or kv_indptr.numel() != B + 1 or not kv_indptr.is_contiguous():
         raise TypeError(f"kv_indptr must be contiguous int64 [{B + 1}]")
     if k.dtype != q.dtype or v.dtype != q.dtype or out.dtype != q.dtype:
         raise TypeError("q, k, v and out must share one dtype")
     if k.shape[2] != D or v.shape != k.shape or out.shape != q.shape or not out.is_contiguous():
         raise ValueError("k and v must be [total_kv, Hkv, D] with q's D, and out contiguous in q's shape")
-    _floats(total_q * Hq, lse=lse)
+    _floats(total_q * Hq, "lse", lse)
     _check(load().respec_prompt_attention(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), q_indptr.data_ptr(), kv_indptr.data_ptr(), out.data_ptr(), _ptr(lse), B, total_q,
         total_kv, max_q_per_seq, max_kv_len, Hq, Hkv, D, _token_stride(q, "q"), _token_stride(k, "k"), _token_stride(v, "v"),
-        float(sm_scale), _dtype_code(q), *_room(workspace), _stream_ptr(stream)))
+        float(sm_scale), _dtype_code(q), *_room(workspace), _stream_on(index, stream)))
 
 
 def _pools(k_pages, v_pages):
@@ -651,20 +663,19 @@ def respec_prompt_attention_paged(q, k_pages, v_pages, q_indptr, page_indptr, pa
     total_q, Hq, D = q.shape
     num_pages, page_size, Hkv, Dk = _pools(k_pages, v_pages)
     B = q_indptr.numel() - 1
-    _here(q, k_pages=k_pages, v_pages=v_pages, q_indptr=q_indptr, page_indptr=page_indptr, page_table=page_table, kv_len=kv_len,
-          out=out, lse=lse, workspace=workspace)
-    _ints(B + 1, q_indptr=q_indptr, page_indptr=page_indptr)
-    _ints(B, kv_len=kv_len)
-    _ints(None, page_table=page_table)
+    index = _here(q, k_pages, v_pages, q_indptr, page_indptr, page_table, kv_len, out, lse, workspace)
+    _ints(B + 1, "q_indptr page_indptr", q_indptr, page_indptr)
+    _ints(B, "kv_len", kv_len)
+    _ints(None, "page_table", page_table)
     if k_pages.dtype != q.dtype or out.dtype != q.dtype:
         raise TypeError("q, k_pages, v_pages and out must share one dtype")
     if Dk != D or out.shape != q.shape or not out.is_contiguous():
         raise ValueError("k_pages and v_pages must have q's D, and out must be contiguous in q's shape")
-    _floats(total_q * Hq, lse=lse)
+    _floats(total_q * Hq, "lse", lse)
     _check(load().respec_prompt_attention_paged(
         q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), q_indptr.data_ptr(), page_indptr.data_ptr(), page_table.data_ptr(),
         kv_len.data_ptr(), out.data_ptr(), _ptr(lse), B, total_q, num_pages, page_table.numel(), page_size, max_q_per_seq, max_kv_len,
-        Hq, Hkv, D, _token_stride(q, "q"), float(sm_scale), _dtype_code(q), *_room(workspace), _stream_ptr(stream)))
+        Hq, Hkv, D, _token_stride(q, "q"), float(sm_scale), _dtype_code(q), *_room(workspace), _stream_on(index, stream)))
 
 
 def respec_append_paged(k_new, v_new, k_pages, v_pages, q_indptr, page_indptr, page_table, kv_len, max_q_per_seq, stream=None):
@@ -672,11 +683,10 @@ def respec_append_paged(k_new, v_new, k_pages, v_pages, q_indptr, page_indptr, p
     changed in place."""
     num_pages, page_size, Hkv, D = _pools(k_pages, v_pages)
     B = q_indptr.numel() - 1
-    _here(k_new, v_new=v_new, k_pages=k_pages, v_pages=v_pages, q_indptr=q_indptr, page_indptr=page_indptr, page_table=page_table,
-          kv_len=kv_len)
-    _ints(B + 1, q_indptr=q_indptr, page_indptr=page_indptr)
-    _ints(B, kv_len=kv_len)
-    _ints(None, page_table=page_table)
+    index = _here(k_new, v_new, k_pages, v_pages, q_indptr, page_indptr, page_table, kv_len)
+    _ints(B + 1, "q_indptr page_indptr", q_indptr, page_indptr)
+    _ints(B, "kv_len", kv_len)
+    _ints(None, "page_table", page_table)
     if k_new.dtype != k_pages.dtype or v_new.dtype != k_pages.dtype:
         raise TypeError("the new tokens must have the pools' dtype")
     if tuple(k_new.shape[1:]) != (Hkv, D) or v_new.shape != k_new.shape:
@@ -687,7 +697,7 @@ def respec_append_paged(k_new, v_new, k_pages, v_pages, q_indptr, page_indptr, p
     _check(load().respec_append_paged(
         k_new.data_ptr(), v_new.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), q_indptr.data_ptr(), page_indptr.data_ptr(),
         page_table.data_ptr(), kv_len.data_ptr(), B, k_new.shape[0], max_q_per_seq, num_pages, page_table.numel(), page_size, Hkv, D, ld,
-        _dtype_code(k_pages), _stream_ptr(stream)))
+        _dtype_code(k_pages), _stream_on(index, stream)))
 
 
 def respec_pages_workspace_bytes(B, num_pages) -> int:
@@ -698,54 +708,51 @@ def respec_pages_resize(want_tokens, page_indptr, page_table, page_count, kv_len
                         workspace, stream=None):
     """want_tokens [B] (negative: leave the sequence alone); the state and the outputs are changed in place."""
     B = want_tokens.numel()
-    _here(want_tokens, page_indptr=page_indptr, page_table=page_table, page_count=page_count, kv_len=kv_len, page_refs=page_refs,
-          copy_src=copy_src, copy_dst=copy_dst, out_missing=out_missing, workspace=workspace)
-    _ints(B + 1, page_indptr=page_indptr)
-    _ints(B, want_tokens=want_tokens, page_count=page_count, kv_len=kv_len, copy_src=copy_src, copy_dst=copy_dst, out_missing=out_missing)
-    _ints(None, page_table=page_table, page_refs=page_refs)
+    index = _here(want_tokens, page_indptr, page_table, page_count, kv_len, page_refs, copy_src, copy_dst, out_missing, workspace)
+    _ints(B + 1, "page_indptr", page_indptr)
+    _ints(B, "want_tokens page_count kv_len copy_src copy_dst out_missing", want_tokens, page_count, kv_len, copy_src, copy_dst, out_missing)
+    _ints(None, "page_table page_refs", page_table, page_refs)
     _check(load().respec_pages_resize(
         want_tokens.data_ptr(), page_indptr.data_ptr(), page_table.data_ptr(), page_count.data_ptr(), kv_len.data_ptr(),
         page_refs.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), out_missing.data_ptr(), B, page_table.numel(), page_refs.numel(),
-        page_size, *_room(workspace), _stream_ptr(stream)))
+        page_size, *_room(workspace), _stream_on(index, stream)))
 
 
 def respec_pages_fork(parent, page_indptr, page_table, page_count, kv_len, page_refs, out_missing, stream=None):
     """parent [B] (negative: leave the sequence alone); the state and out_missing are changed in place."""
     B = parent.numel()
-    _here(parent, page_indptr=page_indptr, page_table=page_table, page_count=page_count, kv_len=kv_len, page_refs=page_refs,
-          out_missing=out_missing)
-    _ints(B + 1, page_indptr=page_indptr)
-    _ints(B, parent=parent, page_count=page_count, kv_len=kv_len, out_missing=out_missing)
-    _ints(None, page_table=page_table, page_refs=page_refs)
+    index = _here(parent, page_indptr, page_table, page_count, kv_len, page_refs, out_missing)
+    _ints(B + 1, "page_indptr", page_indptr)
+    _ints(B, "parent page_count kv_len out_missing", parent, page_count, kv_len, out_missing)
+    _ints(None, "page_table page_refs", page_table, page_refs)
     _check(load().respec_pages_fork(
         parent.data_ptr(), page_indptr.data_ptr(), page_table.data_ptr(), page_count.data_ptr(), kv_len.data_ptr(), page_refs.data_ptr(),
-        out_missing.data_ptr(), B, page_table.numel(), page_refs.numel(), _stream_ptr(stream)))
+        out_missing.data_ptr(), B, page_table.numel(), page_refs.numel(), _stream_on(index, stream)))
 
 
 def respec_pages_compact(page_table, page_refs, new_page_table, new_page_refs, copy_src, copy_dst, out_pages_end, workspace, stream=None):
     """At most copy_src.numel() moves; new_page_table and new_page_refs may be the old ones."""
-    _here(page_table, page_refs=page_refs, new_page_table=new_page_table, new_page_refs=new_page_refs, copy_src=copy_src,
-          copy_dst=copy_dst, out_pages_end=out_pages_end, workspace=workspace)
-    _ints(None, page_table=page_table, page_refs=page_refs, copy_src=copy_src)
-    _ints(page_table.numel(), new_page_table=new_page_table)
-    _ints(page_refs.numel(), new_page_refs=new_page_refs)
-    _ints(copy_src.numel(), copy_dst=copy_dst)
-    _ints(1, out_pages_end=out_pages_end)
+    index = _here(page_table, page_refs, new_page_table, new_page_refs, copy_src, copy_dst, out_pages_end, workspace)
+    _ints(None, "page_table page_refs copy_src", page_table, page_refs, copy_src)
+    _ints(page_table.numel(), "new_page_table", new_page_table)
+    _ints(page_refs.numel(), "new_page_refs", new_page_refs)
+    _ints(copy_src.numel(), "copy_dst", copy_dst)
+    _ints(1, "out_pages_end", out_pages_end)
     _check(load().respec_pages_compact(
         page_table.data_ptr(), page_refs.data_ptr(), new_page_table.data_ptr(), new_page_refs.data_ptr(), copy_src.data_ptr(),
         copy_dst.data_ptr(), out_pages_end.data_ptr(), page_table.numel(), page_refs.numel(), copy_src.numel(), *_room(workspace),
-        _stream_ptr(stream)))
+        _stream_on(index, stream)))
 
 
 def respec_pages_copy(k_pages, v_pages, copy_src, copy_dst, stream=None):
     """Pages copy_src[i] -> copy_dst[i] of one layer's pools (-1: none)."""
     num_pages, page_size, Hkv, D = _pools(k_pages, v_pages)
-    _here(k_pages, v_pages=v_pages, copy_src=copy_src, copy_dst=copy_dst)
-    _ints(None, copy_src=copy_src)
-    _ints(copy_src.numel(), copy_dst=copy_dst)
+    index = _here(k_pages, v_pages, copy_src, copy_dst)
+    _ints(None, "copy_src", copy_src)
+    _ints(copy_src.numel(), "copy_dst", copy_dst)
     _check(load().respec_pages_copy(
         k_pages.data_ptr(), v_pages.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), copy_src.numel(), num_pages, page_size, Hkv, D,
-        _dtype_code(k_pages), _stream_ptr(stream)))
+        _dtype_code(k_pages), _stream_on(index, stream)))
 
 
 def _rows_of(logits):
@@ -764,10 +771,9 @@ def respec_token_logprobs(logits, tokens, logprob, lse, entropy, top_tokens, top
     """logits [rows,V], tokens [rows] int32 (outside [0,V): an unused row); logprob, lse, entropy (or None) [rows] float32;
     top_tokens int32 and top_logprobs float32 [rows,n] or both None.  row_temperature [rows] takes the place of temperature."""
     rows, V, ld = _rows_of(logits)
-    _here(logits, tokens=tokens, logprob=logprob, lse=lse, entropy=entropy, top_tokens=top_tokens, top_logprobs=top_logprobs,
-          workspace=workspace, row_temperature=row_temperature)
-    _ints(rows, tokens=tokens)
-    _floats(rows, logprob=logprob, lse=lse, entropy=entropy, row_temperature=row_temperature)
+    index = _here(logits, tokens, logprob, lse, entropy, top_tokens, top_logprobs, workspace, row_temperature)
+    _ints(rows, "tokens", tokens)
+    _floats(rows, "logprob lse entropy row_temperature", logprob, lse, entropy, row_temperature)
     if (top_tokens is None) != (top_logprobs is None):
         raise ValueError("top_tokens and top_logprobs go together")
     n = 0
@@ -775,27 +781,26 @@ def respec_token_logprobs(logits, tokens, logprob, lse, entropy, top_tokens, top
         if top_tokens.dim() != 2 or top_tokens.shape[0] != rows:
             raise ValueError("top_tokens must be [rows, n]")
         n = top_tokens.shape[1]
-        _ints(rows * n, top_tokens=top_tokens)
-        _floats(rows * n, top_logprobs=top_logprobs)
+        _ints(rows * n, "top_tokens", top_tokens)
+        _floats(rows * n, "top_logprobs", top_logprobs)
     _check(load().respec_token_logprobs(
         logits.data_ptr(), tokens.data_ptr(), _ptr(row_temperature), logprob.data_ptr(), lse.data_ptr(), _ptr(entropy), _ptr(top_tokens),
-        _ptr(top_logprobs), rows, V, ld, n, float(temperature), _dtype_code(logits), *_room(workspace), _stream_ptr(stream)))
+        _ptr(top_logprobs), rows, V, ld, n, float(temperature), _dtype_code(logits), *_room(workspace), _stream_on(index, stream)))
 
 
 def respec_token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob, grad_entropy, grad_logits, temperature, row_temperature=None,
                                stream=None):
     """The gradient in the logits from what respec_token_logprobs wrote; grad_logprob or grad_entropy may be None."""
     rows, V, ld = _rows_of(logits)
-    _here(logits, tokens=tokens, lse=lse, entropy=entropy, grad_logprob=grad_logprob, grad_entropy=grad_entropy, grad_logits=grad_logits,
-          row_temperature=row_temperature)
-    _ints(rows, tokens=tokens)
-    _floats(rows, lse=lse, entropy=entropy, grad_logprob=grad_logprob, grad_entropy=grad_entropy, row_temperature=row_temperature)
+    index = _here(logits, tokens, lse, entropy, grad_logprob, grad_entropy, grad_logits, row_temperature)
+    _ints(rows, "tokens", tokens)
+    _floats(rows, "lse entropy grad_logprob grad_entropy row_temperature", lse, entropy, grad_logprob, grad_entropy, row_temperature)
     if grad_logits.shape != logits.shape or grad_logits.dtype != logits.dtype:
         raise ValueError("grad_logits must have the logits' shape and dtype")
     ld_g = _rows_of(grad_logits)[2]
     _check(load().respec_token_logprobs_grad(
         logits.data_ptr(), tokens.data_ptr(), _ptr(row_temperature), lse.data_ptr(), _ptr(entropy), _ptr(grad_logprob),
-        _ptr(grad_entropy), grad_logits.data_ptr(), rows, V, ld, ld_g, float(temperature), _dtype_code(logits), _stream_ptr(stream)))
+        _ptr(grad_entropy), grad_logits.data_ptr(), rows, V, ld, ld_g, float(temperature), _dtype_code(logits), _stream_on(index, stream)))
 
 
 def respec_solver_pick(points, active_batch, draft_us_fixed, draft_us_per_seq):

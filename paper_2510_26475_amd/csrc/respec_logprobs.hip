@@ -621,7 +621,10 @@ struct GradRow {
 template <bool BF16, bool PIECES>
 __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradParams p) {
     using E = Elem<BF16>;
-    const int row = blockIdx.x / p.blocks_per_row, block = blockIdx.x % p.blocks_per_row;
+    // The last rows first, which the forward pass read last and left in the cache behind the L2s, and loads and stores that take no
+    // room there: forward and gradient of 2,048 rows of 151,936 bf16 logits take 298 us; 306 with ordinary loads, 314 with the
+    // rows in order as well, 356 with ordinary stores.
+    const int row = p.rows - 1 - blockIdx.x / p.blocks_per_row, block = blockIdx.x % p.blocks_per_row;
     const Row<BF16> r(p.logits, row, p.ld, p.V);
     char *out = static_cast<char *>(p.grad) + (int64_t)row * p.ld_g * E::kSize;
     GradRow g;
@@ -638,7 +641,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradParams p) {
         u32x4 raw[kUnroll];
         if (!unused)
             for (int u = 0; u < kUnroll; ++u)
-                if (r.whole(i0 + u * kThreads)) raw[u] = *r.at(i0 + u * kThreads);
+                if (r.whole(i0 + u * kThreads)) raw[u] = __builtin_nontemporal_load(r.at(i0 + u * kThreads));
         for (int u = 0; u < kUnroll; ++u) {
             const int i = i0 + u * kThreads;
             if (i >= r.pieces) break;
@@ -650,7 +653,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradParams p) {
                 u32x4 w;
                 for (int j = 0; j < 4; ++j)
                     w[j] = BF16 ? bf16_bits(v[2 * j]) | bf16_bits(v[(2 * j + 1) % E::kPer]) << 16 : __float_as_uint(v[j]);
-                *reinterpret_cast<u32x4 *>(out + first * E::kSize) = w;
+                __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(out + first * E::kSize));
             } else {
                 for (int64_t e = max(first, (int64_t)0); e < min(first + E::kPer, (int64_t)p.V); ++e)
                     store_one<BF16>(out, e, unused ? 0.f : g.at(load_one<BF16>(r.base, e), e));
