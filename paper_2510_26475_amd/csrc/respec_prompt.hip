@@ -36,7 +36,6 @@ typedef s16x4 __attribute__((address_space(3))) *LdsTr;
 
 constexpr float kRescaleSlack = 8.f;  // log2 units
 constexpr int kMaxSplits = 16;
-constexpr int kWaves16 = 8;           // waves of a work-group in bf16
 constexpr int kSplitTiles = 512;      // work-groups below which a call is split
 
 struct PromptParams {
@@ -70,6 +69,8 @@ struct Shape {
     static constexpr int kLoads = kKeys * kChunks / kThreads;  // pieces of K (and of V) that a thread moves per tile
     static constexpr int kWaveKeys = 64 / kChunks;        // keys that a wave moves with one load of every lane
     static constexpr int kDTiles = D / 32;
+    static constexpr int kRing = WAVES == 8 ? 4 : 2;      // tiles of K and of V in LDS
+    static constexpr int kLdsBytes = 2 * kRing * kTileBytes + 16;
     static_assert(kKeys * kChunks % kThreads == 0, "whole pieces per thread");
     static_assert(16 % kWaveKeys == 0, "a wave's load lies in one page");
 };
@@ -110,23 +111,79 @@ struct Job {
     int all;               // keys that all rows of the work-group see
 };
 
+// Tokens of sequence b and where they begin, inside the buffers whatever the arrays hold.
+template <bool PAGED>
+__device__ inline int length_of(const PromptParams &p, int b, int64_t &kv0) {
+    if constexpr (PAGED) {
+        kv0 = max(0, min(p.page_indptr[b], p.table_len));
+        const int64_t pages = max((int64_t)0, (int64_t)min(p.page_indptr[b + 1], p.table_len) - kv0);
+        return (int)max((int64_t)0, min(min((int64_t)p.kv_len[b], pages << p.page_shift), (int64_t)p.max_kv));
+    } else {
+        kv0 = max((int64_t)0, min(p.kv_indptr[b], p.total_kv));
+        return (int)max((int64_t)0, min(min(p.kv_indptr[b + 1], p.total_kv) - kv0, (int64_t)p.max_kv));
+    }
+}
+
+// The number-th tile of a batch of up to 64 sequences (one per lane), the one that sees most keys first: work-groups are given out in
+// order, and a long one among the last would be waited for.  How many tiles see x keys or more is known for every sequence
+// without looking at its tiles, so x is found by bisection, in steps of 64 keys.  (16 packed prompts of 65 to 2,048 tokens at 28/4
+// heads take 137 us, in the order of the sequences 158.)
+template <bool PAGED, int ROWS>
+__device__ inline bool find_longest(const PromptParams &p, int number, Tile &out, int &tokens, int64_t &first) {
+    const int lane = threadIdx.x & 63;
+    int q0 = 0, R = 0, L = 0;
+    int64_t kv0 = 0;
+    if (lane < p.B) {
+        q0 = max(0, min(p.q_indptr[lane], p.total_q));
+        R = max(0, min(min(p.q_indptr[lane + 1], p.total_q) - q0, p.max_q));
+        L = length_of<PAGED>(p, lane, kv0);
+    }
+    const int tiles = (R * p.G + ROWS - 1) / ROWS, before = L - R;  // (before: negative where the first rows see nothing)
+    auto reach = [&](int x) __attribute__((always_inline)) {  // this sequence's tiles that see 64 x keys or more
+        if (x <= 0) return tiles;
+        if ((int64_t)x * 64 > L || tiles == 0) return 0;
+        const int first = ((max(x * 64 - before - 1, 0) * p.G + 1) + ROWS - 1) / ROWS - 1;  // (the last tile's last row sees L keys)
+        return tiles - max(0, min(first, tiles - 1));
+    };
+    auto all = [&](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(wave_scan_add(reach(x)), 63); };
+    if (number >= all(0)) return false;
+    int x = 0, over = p.max_kv / 64 + 1;  // all(x) > number >= all(over)
+    while (p.B > 1 && over - x > 1) {
+        const int mid = (x + over) / 2;
+        if (all(mid) > number) x = mid;
+        else over = mid;
+    }
+    const int more = p.B == 1 ? 0 : reach(over), mine = p.B == 1 ? tiles : reach(x) - more;  // (one sequence: its tiles from the last)
+    const int rest = number - __builtin_amdgcn_readlane(wave_scan_add(more), 63);
+    const int sum = wave_scan_add(mine);
+    const int at = (int)__builtin_ctzll(__ballot(sum > rest));
+    out.b = at;
+    out.tiles = __builtin_amdgcn_readlane(tiles, at);
+    out.index = __builtin_amdgcn_readlane(tiles - more, at) - 1 - (rest - __builtin_amdgcn_readlane(sum - mine, at));
+    out.R = __builtin_amdgcn_readlane(R, at);
+    out.q0 = __builtin_amdgcn_readlane(q0, at);
+    tokens = __builtin_amdgcn_readlane(L, at);
+    first = (int64_t)__builtin_amdgcn_readlane((int)(kv0 >> 32), at) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)kv0, at);
+    return true;
+}
+
+// The number-th tile of row tiles, with its sequence's tokens and where they begin.
+template <bool PAGED, int ROWS>
+__device__ inline bool find_rows(const PromptParams &p, int number, Tile &out, int &tokens, int64_t &first) {
+    if (p.B <= 64) return find_longest<PAGED, ROWS>(p, number, out, tokens, first);
+    if (!find_tile(p.q_indptr, p.B, p.total_q, p.max_q, p.G, ROWS, number, out)) return false;
+    out.index = out.tiles - 1 - out.index;  // (the longest of a sequence first)
+    tokens = __builtin_amdgcn_readfirstlane(length_of<PAGED>(p, out.b, first));
+    return true;
+}
+
 template <bool BF16, int D, int WAVES, bool PAGED>
 __device__ inline bool find_job(const PromptParams &p, Job &j) {
     using S = Shape<BF16, D, WAVES>;
     j.head = blockIdx.x % p.Hkv;
     const int rest = blockIdx.x / p.Hkv, split = rest % p.splits;
     j.number = blockIdx.x;
-    if (!find_tile(p.q_indptr, p.B, p.total_q, p.max_q, p.G, S::kRows, rest / p.splits, j.tile)) return false;
-    j.tile.index = j.tile.tiles - 1 - j.tile.index;  // (the longest first)
-    if constexpr (PAGED) {
-        j.kv0 = max(0, min(p.page_indptr[j.tile.b], p.table_len));
-        const int64_t pages = max((int64_t)0, (int64_t)min(p.page_indptr[j.tile.b + 1], p.table_len) - j.kv0);
-        j.L = (int)max((int64_t)0, min(min((int64_t)p.kv_len[j.tile.b], pages << p.page_shift), (int64_t)p.max_kv));
-    } else {
-        j.kv0 = max((int64_t)0, min(p.kv_indptr[j.tile.b], p.total_kv));
-        j.L = (int)max((int64_t)0, min(min(p.kv_indptr[j.tile.b + 1], p.total_kv) - j.kv0, (int64_t)p.max_kv));
-    }
-    j.L = __builtin_amdgcn_readfirstlane(j.L);
+    if (!find_rows<PAGED, S::kRows>(p, rest / p.splits, j.tile, j.L, j.kv0)) return false;
     j.n_rows = j.tile.R * p.G;
     j.row0 = j.tile.index * S::kRows;
     const int last = min(j.row0 + S::kRows, j.n_rows) - 1;
@@ -171,12 +228,17 @@ __device__ inline void load_q(const PromptParams &p, const RowOf &r, int D, int 
 
 typedef const __attribute__((address_space(4))) int32_t *ConstInts;  // (read through the scalar cache; nothing writes it meanwhile)
 
-// Moves K or V pieces from global memory into registers: key wave * kWaveKeys + lane / kChunks + i * (keys of all waves), piece
-// lane % kChunks.  The keys of a load lie in one page, so what differs between lanes is a 32-bit offset.  Keys past the end are the
-// last one's (they are never seen).
+// Moves K or V pieces from global memory into registers and on into LDS: key wave * kWaveKeys + lane / kChunks + i * (keys of all
+// waves) of a tile, piece lane % kChunks.  The keys of a wave's load lie in one page, so what differs between lanes is a 32-bit offset.
+// Keys past the end are the last one's (they are never seen).
 template <bool BF16, int D, int WAVES, bool PAGED>
 struct Mover {
     using S = Shape<BF16, D, WAVES>;
+    static constexpr int kSpots = PAGED ? S::kLoads : 1;
+    struct Spot {             // where a tile lies, the same in K and V (all uniform)
+        int64_t row[kSpots];  // of its first key, or of each load's
+        int left[kSpots];     // keys behind that one
+    };
     const char *k, *v;
     int wave, my_key;
     uint32_t my_piece;
@@ -200,43 +262,30 @@ struct Mover {
             shift = p.page_shift;
         }
     }
-    __device__ int64_t row(int n) const {  // of a key in K and V (uniform)
-        if constexpr (PAGED) {
-            const int64_t page = max(0, min(table[n >> shift], num_pages - 1));
-            return (page << shift) + (n & ((1 << shift) - 1));
-        } else {
-            return kv0 + n;
+    __device__ Spot find(int t) const {  // (a tile that begins within the sequence)
+        Spot s;
+#pragma unroll
+        for (int i = 0; i < kSpots; ++i) {
+            if constexpr (PAGED) {
+                const int n = min(t * S::kKeys + i * (WAVES * S::kWaveKeys) + wave * S::kWaveKeys, L - 1);
+                const int64_t page = max(0, min(table[n >> shift], num_pages - 1));
+                s.row[i] = (page << shift) + (n & ((1 << shift) - 1));
+                s.left[i] = L - 1 - n;
+            } else {
+                s.row[i] = kv0 + (int64_t)t * S::kKeys;
+                s.left[i] = L - 1 - t * S::kKeys;
+            }
         }
+        return s;
     }
     template <bool V>
-    __device__ void load(int t, u32x4 (&x)[S::kLoads]) const {
+    __device__ void load(const Spot &s, u32x4 (&x)[S::kLoads]) const {
+        const int64_t ld = V ? ld_v : ld_k;
 #pragma unroll
         for (int i = 0; i < S::kLoads; ++i) {
-            const int n = max(0, min(t * S::kKeys + i * (WAVES * S::kWaveKeys) + wave * S::kWaveKeys, L - 1));  // (uniform)
-            const uint32_t ld = (uint32_t)(V ? ld_v : ld_k);
-            const uint32_t off = __umul24((uint32_t)min(my_key, L - 1 - n), ld) + my_piece;
-            const char *base = (V ? v : k) + row(n) * (V ? ld_v : ld_k);
-            x[i] = *reinterpret_cast<const u32x4 *>(base + off);
-        }
-    }
-    // The same for a tile that lies in the sequence as a whole.
-    template <bool V>
-    __device__ void load_whole(int t, u32x4 (&x)[S::kLoads]) const {
-        const int64_t ld = V ? ld_v : ld_k;
-        const char *const from = V ? v : k;
-        if constexpr (PAGED) {
-            const uint32_t off = __umul24((uint32_t)my_key, (uint32_t)ld) + my_piece;
-#pragma unroll
-            for (int i = 0; i < S::kLoads; ++i)
-                x[i] = *reinterpret_cast<const u32x4 *>(from + row(t * S::kKeys + i * (WAVES * S::kWaveKeys) + wave * S::kWaveKeys) * ld + off);
-        } else {
-            const char *const base = from + (kv0 + (int64_t)t * S::kKeys) * ld;
-            uint32_t off = __umul24((uint32_t)(wave * S::kWaveKeys + my_key), (uint32_t)ld) + my_piece;
-#pragma unroll
-            for (int i = 0; i < S::kLoads; ++i) {
-                x[i] = *reinterpret_cast<const u32x4 *>(base + off);
-                off += (uint32_t)ld * (WAVES * S::kWaveKeys);
-            }
+            const int at = PAGED ? i : 0, mine = PAGED ? my_key : key(i);
+            const uint32_t off = __umul24((uint32_t)min(mine, s.left[at]), (uint32_t)ld) + my_piece;
+            x[i] = *reinterpret_cast<const u32x4 *>((V ? v : k) + s.row[at] * ld + off);
         }
     }
     __device__ int key(int i) const { return i * (WAVES * S::kWaveKeys) + wave * S::kWaveKeys + my_key; }
@@ -365,16 +414,18 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptParams p) {
         mover.put_v(lds_v + buffer * S::kTileBytes, vr, (t + 1) * S::kKeys > job.all, &sh_not_finite);
     };
     if (job.t_begin < job.t_end) {  // (uniform)
-        mover.template load<false>(job.t_begin, kr);
-        mover.template load<true>(job.t_begin, vr);
+        const auto spot = mover.find(job.t_begin);
+        mover.template load<false>(spot, kr);
+        mover.template load<true>(spot, vr);
         put(0, job.t_begin);
         __syncthreads();
     }
     for (int t = job.t_begin; t < job.t_end; ++t) {
         const int buffer = (t - job.t_begin) & 1;
         if (t + 1 < job.t_end) {
-            mover.template load<false>(t + 1, kr);
-            mover.template load<true>(t + 1, vr);
+            const auto spot = mover.find(t + 1);
+            mover.template load<false>(spot, kr);
+            mover.template load<true>(spot, vr);
         }
         if (t * S::kKeys < row.wave_sees) {
             const char *kb = lds_k + buffer * S::kTileBytes, *vb = lds_v + buffer * S::kTileBytes;
@@ -432,13 +483,18 @@ __device__ __attribute__((always_inline)) inline void each(F &&f) {
     each_of<N>(f, std::make_integer_sequence<int, N>{});
 }
 
-// bf16: the scores of tile t+1 are multiplied while the exponentials of tile t are computed.  K is one tile ahead of V in LDS, and the
-// loop is written for two tiles, so that a tile's buffer is a constant and every LDS address one of twelve that a lane keeps.
+// bf16: the scores of tile t+1 are multiplied while the exponentials of tile t are computed; step t reads K of t+1 and V of t.
+// Eight waves: LDS holds four tiles of K and four of V (128 KiB at D = 128, one work-group per compute unit), step t fetches K of t+3
+// and V of t+2; what a step writes is read two steps later and what it writes over was read two steps before, so one barrier
+// for two steps is enough.  Four waves: two tiles of each and two work-groups per compute unit, K of t+2 and V of t+1, a
+// barrier per step.  The loop is written for as many steps as there are tiles in
+// LDS, so that a tile's place is a constant.
 template <int D, int WAVES, bool PAGED>
 __global__ __launch_bounds__(WAVES * 64, 2) void prompt_bf16_kernel(PromptParams p) {
     using S = Shape<true, D, WAVES>;
-    extern __shared__ __align__(16) char lds[];  // two tiles of K, two of V
-    __shared__ int sh_not_finite;
+    constexpr int kRing = S::kRing, kFetch = kRing == 4 ? 3 : 2;  // K is fetched so many tiles ahead, V one less
+    extern __shared__ __align__(16) char lds[];  // kRing tiles of K, kRing of V, and a word
+    int &sh_not_finite = *reinterpret_cast<int *>(lds + 2 * kRing * S::kTileBytes);
     Job job;
     if (!find_job<true, D, WAVES, PAGED>(p, job)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -450,73 +506,34 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_bf16_kernel(PromptParams
     if (threadIdx.x == 0) sh_not_finite = 0;
     __syncthreads();
 
-    // Where this lane reads: a key's pieces of K; for V the transposing read's sixteen lanes address four keys by sixteen d.
-    int k_at[S::kChunks / 2], v_at[S::kDTiles];
-#pragma unroll
-    for (int x = 0; x < S::kChunks / 2; ++x) k_at[x] = col * S::kRowBytes + k_piece<true, D>(col, 2 * x + half) * 16;
+    // Where this lane reads: a key's pieces of K; for V the transposing read's sixteen lanes address four keys by sixteen d and
+    // receive one d of the four keys each.  The place of a piece within its row is an exclusive or, so the x-th piece pair of K lies at
+    // k_at ^ 32 x and the d-th tile of V at v_at ^ 64 d.
+    int k_at = col * S::kRowBytes + k_piece<true, D>(col, half) * 16;
     const int i16 = lane & 15, v_key = half * 4 + (i16 >> 2), d0 = ((lane & 16) + 4 * (i16 & 3)) * 2;
-#pragma unroll
-    for (int d = 0; d < S::kDTiles; ++d) v_at[d] = v_key * S::kRowBytes + v_piece<true, D>(v_key, (d * 64 + d0) >> 4) * 16 + (d0 & 15);
+    int v_at = kRing * S::kTileBytes + v_key * S::kRowBytes + v_piece<true, D>(v_key, d0 >> 4) * 16 + (d0 & 15);
 
     floatx16 o[S::kDTiles];
 #pragma unroll
     for (int d = 0; d < S::kDTiles; ++d)
         for (int x = 0; x < 16; ++x) o[d][x] = 0.f;
     float m = -INFINITY, ref = 0.f, l = 0.f;
-    u32x4 kr[S::kLoads], vr[S::kLoads];
     floatx16 s_even[S::kBlocks], s_odd[S::kBlocks];
 
-    auto scores = [&](auto buffer, floatx16(&s)[S::kBlocks]) __attribute__((always_inline)) {
-        constexpr int kAt = decltype(buffer)::value * S::kTileBytes;
-#pragma unroll
-        for (int b = 0; b < S::kBlocks; ++b)
-#pragma unroll
-            for (int x = 0; x < S::kChunks / 2; ++x) {
-                const bf16x8 a = *reinterpret_cast<const bf16x8 *>(lds + k_at[x] + (kAt + b * 32 * S::kRowBytes));
-                const floatx16 none{};
-                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, qf[x]), x == 0 ? none : s[b], 0, 0, 0);
-            }
-    };
-    // Probabilities of sixteen keys as the B operand of the second product: slot j is key 8 (j / 4) + 4 half + j % 4 of them.
-    auto weights = [&](const floatx16 &s, int h) __attribute__((always_inline)) {
-        bf16x8 pf;
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-            const float a = __builtin_amdgcn_exp2f(fmaf(s[h * 8 + j], p.scale2, -ref)), c = __builtin_amdgcn_exp2f(fmaf(s[h * 8 + j + 1], p.scale2, -ref));
-            l += a;
-            l += c;
-            const bf16x2 two = __builtin_convertvector(floatx2{a, c}, bf16x2);
-            pf[j] = two[0];
-            pf[j + 1] = two[1];
-        }
-        return pf;
-    };
-    auto product = [&](auto buffer, int b, int h, const bf16x8 &pf) __attribute__((always_inline)) {
-        constexpr int kAt = (2 + decltype(buffer)::value) * S::kTileBytes;
-#pragma unroll
-        for (int d = 0; d < S::kDTiles; ++d) {
-            s16x4 vt[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                vt[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTr)(lds + v_at[d] + (kAt + (b * 32 + h * 16 + j * 8) * S::kRowBytes)));
-            const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vt[0], vt[1], 0, 1, 2, 3, 4, 5, 6, 7));
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf, o[d], 0, 0, 0);
-        }
-    };
     auto largest = [&](const floatx16(&s)[S::kBlocks]) __attribute__((always_inline)) {
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < S::kBlocks; ++b)
 #pragma unroll
             for (int x = b == 0; x < 16; ++x) top = fmaxf(top, s[b][x]);
-        return max_of_halves(top) * p.scale2;
+        return top;
     };
     auto mask = [&](int t, floatx16(&s)[S::kBlocks]) __attribute__((always_inline)) {
-        if ((t + 1) * S::kKeys > row.wave_all)
 #pragma unroll
-            for (int b = 0; b < S::kBlocks; ++b) mask_scores(s[b], t * S::kKeys + b * 32, half, row.lim);
+        for (int b = 0; b < S::kBlocks; ++b) mask_scores(s[b], t * S::kKeys + b * 32, half, row.lim);
     };
-    auto rescale = [&](float top) __attribute__((always_inline)) {
+    auto rescale = [&](float top) __attribute__((always_inline)) {  // with the largest score that this lane has
+        top = max_of_halves(top) * p.scale2;
         if (__ballot(top > m + kRescaleSlack) == 0) return;  // (m = -inf: any finite score)
         const float m_new = top > m + kRescaleSlack ? top : m;
         const float f = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
@@ -527,46 +544,57 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_bf16_kernel(PromptParams
         for (int d = 0; d < S::kDTiles; ++d)
             for (int x = 0; x < 16; ++x) o[d][x] *= f;
     };
-    // Tile t, its scores in s (the maximum taken into account), V in `buffer`, the next tile's K in the other one; all rows see both
-    // tiles.  One block of code: the matrix unit has the scores of the next tile and the second product of this one to do while
-    // the exponentials of this one and the maximum of the next are computed.
-    auto both = [&](auto buffer, int t, floatx16(&s)[S::kBlocks], floatx16(&next)[S::kBlocks]) __attribute__((always_inline)) {
-        constexpr int kB = decltype(buffer)::value;
-        mover.template load_whole<false>(t + 2, kr);
-        mover.template load_whole<true>(t + 1, vr);
-        // Written in the order it is to run in: a product, an LDS read kAhead products before its use, and a share of the rest.
-        constexpr int kAhead = 4, kFirst = S::kBlocks * S::kChunks / 2, kSecond = 2 * S::kBlocks * S::kDTiles;
-        constexpr int kPairs = 16 * S::kBlocks / 2;  // of probabilities; those of the last sixteen keys are not needed before the last products
+    // Two probabilities of sixteen keys' B operand, the n-th pair of all: slot j is key 8 (j / 4) + 4 half + j % 4 of them.
+    auto pair = [&](auto n_, const floatx16(&s)[S::kBlocks], u32x4(&pf)[2 * S::kBlocks]) __attribute__((always_inline)) {
+        constexpr int n = decltype(n_)::value, g = n / 4, j = n % 4 * 2;
+        const float a = __builtin_amdgcn_exp2f(fmaf(s[g / 2][g % 2 * 8 + j], p.scale2, -ref));
+        const float c = __builtin_amdgcn_exp2f(fmaf(s[g / 2][g % 2 * 8 + j + 1], p.scale2, -ref));
+        l += a;
+        l += c;
+        asm volatile("" : "+v"(l));  // (added now: later, the sixteen pairs would have to be kept)
+        pf[g][j / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{a, c}, bf16x2));
+    };
+    auto read_v = [&](int g, int d, int tile) __attribute__((always_inline)) {
+        s16x4 vt[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) vt[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTr)(lds + (v_at ^ (64 * d)) + (tile + (g * 16 + j * 8) * S::kRowBytes)));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(vt[0], vt[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    typedef typename Mover<true, D, WAVES, PAGED>::Spot Spot;
+    Spot spot{};  // of the tile whose V the next step fetches
+    // Step t (not the last), the tile's scores in s with their maximum taken into account; `place`: (t - t_begin) % kRing.
+    // Written in the order it is to run in: a product, an LDS read kAhead products before its use, and a share of the rest.
+    auto step = [&](auto place, int t, floatx16(&s)[S::kBlocks], floatx16(&next)[S::kBlocks]) __attribute__((always_inline)) {
+        constexpr int kPlace = decltype(place)::value;
+        constexpr int kFirst = S::kBlocks * S::kChunks / 2, kSecond = 2 * S::kBlocks * S::kDTiles, kAhead = 4;
+        constexpr int kPairs = 16 * S::kBlocks / 2, kEarly = kPairs * 5 / 8;  // pairs of probabilities; those along with the first products
+        u32x4 moved[S::kLoads];  // K in the first half of the step, V in the second
+        const Spot after = mover.find(min(t + kFetch, job.t_end - 1));
+        mover.template load<false>(after, moved);
+        if constexpr (WAVES == 4) asm volatile("" : "+v"(k_at), "+v"(v_at));  // (twelve addresses that do not change would not fit beside 16 pieces)
+        __builtin_amdgcn_sched_barrier(0);
         bf16x8 ahead[kAhead];
         u32x4 pf[2 * S::kBlocks];
         auto read = [&](auto i_) __attribute__((always_inline)) {
             constexpr int i = decltype(i_)::value;
             if constexpr (i < kFirst) {
                 constexpr int b = i % S::kBlocks, x = i / S::kBlocks;
-                ahead[i % kAhead] = *reinterpret_cast<const bf16x8 *>(lds + k_at[x] + ((1 - kB) * S::kTileBytes + b * 32 * S::kRowBytes));
+                ahead[i % kAhead] = *reinterpret_cast<const bf16x8 *>(lds + (k_at ^ (32 * x)) + ((kPlace + 1) % kRing * S::kTileBytes + b * 32 * S::kRowBytes));
             } else if constexpr (i < kFirst + kSecond) {
-                constexpr int g = (i - kFirst) / S::kDTiles, d = (i - kFirst) % S::kDTiles;
-                s16x4 vt[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    vt[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTr)(lds + v_at[d] + ((2 + kB) * S::kTileBytes + (g * 16 + j * 8) * S::kRowBytes)));
-                ahead[i % kAhead] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vt[0], vt[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                ahead[i % kAhead] = read_v((i - kFirst) / S::kDTiles, (i - kFirst) % S::kDTiles, kPlace % kRing * S::kTileBytes);
             }
-        };
-        auto pair = [&](auto n_) __attribute__((always_inline)) {
-            constexpr int n = decltype(n_)::value, g = n / 4, j = n % 4 * 2;
-            const floatx16 &from = s[g / 2];
-            const float a = __builtin_amdgcn_exp2f(fmaf(from[g % 2 * 8 + j], p.scale2, -ref));
-            const float c = __builtin_amdgcn_exp2f(fmaf(from[g % 2 * 8 + j + 1], p.scale2, -ref));
-            l += a;
-            l += c;
-            pf[g][j / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{a, c}, bf16x2));
         };
         float top = -INFINITY;
         each<kAhead>([&](auto i) __attribute__((always_inline)) { read(i); });
         __builtin_amdgcn_sched_barrier(0);
         each<kFirst + kSecond>([&](auto i_) __attribute__((always_inline)) {
             constexpr int i = decltype(i_)::value;
+            if constexpr (i == kFirst) {  // (past the last tile: not read)
+                mover.put_k(lds + (kPlace + kFetch) % kRing * S::kTileBytes, moved);
+                mover.template load<true>(spot, moved);
+                spot = after;
+                __builtin_amdgcn_sched_barrier(0);
+            }
             if constexpr (i < kFirst) {
                 constexpr int b = i % S::kBlocks, x = i / S::kBlocks;
                 const floatx16 none{};
@@ -576,86 +604,108 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_bf16_kernel(PromptParams
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[i % kAhead], __builtin_bit_cast(bf16x8, pf[g]), o[d], 0, 0, 0);
             }
             read(std::integral_constant<int, i + kAhead>{});
-            // pairs: two in three products of the first kind, the rest in the second kind's first ones; then the maximum
-            constexpr int kShare = kPairs * 5 / 8;
             if constexpr (i < kFirst) {
-                constexpr int from = i * kShare / kFirst, to = (i + 1) * kShare / kFirst;
-                each<to - from>([&](auto n) __attribute__((always_inline)) { pair(std::integral_constant<int, from + decltype(n)::value>{}); });
-            } else {
-                constexpr int n = kShare + i - kFirst, rest = kPairs - kShare, k = i - kFirst - rest, kLast = kSecond - rest;
-                if constexpr (n < kPairs) pair(std::integral_constant<int, n>{});
-                else {
-                    constexpr int from = 16 * S::kBlocks * k / kLast, to = 16 * S::kBlocks * (k + 1) / kLast;
+                constexpr int from = i * kEarly / kFirst, to = (i + 1) * kEarly / kFirst;
+                each<to - from>([&](auto n) __attribute__((always_inline)) { pair(std::integral_constant<int, from + decltype(n)::value>{}, s, pf); });
+            } else {  // the other pairs, none later than the products before its own, then the maximum
+                constexpr int n = kEarly + i - kFirst, k = i - kFirst - (kPairs - kEarly), kRest = kSecond - (kPairs - kEarly);
+                if constexpr (n < kPairs) pair(std::integral_constant<int, n>{}, s, pf);
+                else
 #pragma unroll
-                    for (int x = from; x < to; ++x) top = fmaxf(top, next[x / 16][x % 16]);
-                }
+                    for (int x = 16 * S::kBlocks * k / kRest; x < 16 * S::kBlocks * (k + 1) / kRest; ++x) top = fmaxf(top, next[x / 16][x % 16]);
             }
             __builtin_amdgcn_sched_barrier(0);
         });
-        top = max_of_halves(top) * p.scale2;
-        rescale(top);
-        mover.put_k(lds + kB * S::kTileBytes, kr);
-        mover.put_v(lds + (3 - kB) * S::kTileBytes, vr, false, &sh_not_finite);
-        __syncthreads();
-    };
-    // Any tile, its scores in s: the second product, then the next tile's scores.
-    auto one = [&](auto buffer, int t, floatx16(&s)[S::kBlocks], floatx16(&next)[S::kBlocks]) __attribute__((always_inline)) {
-        constexpr int kB = decltype(buffer)::value;
-        const std::integral_constant<int, kB> here{};
-        const std::integral_constant<int, 1 - kB> there{};
-        const bool more = t + 1 < job.t_end;
-        if (t + 2 < job.t_end) mover.template load<false>(t + 2, kr);
-        if (more) mover.template load<true>(t + 1, vr);
-        if (t * S::kKeys < row.wave_sees)
-#pragma unroll
-            for (int i = 0; i < 2 * S::kBlocks; ++i) product(here, i / 2, i % 2, weights(s[i / 2], i % 2));
-        if (more && (t + 1) * S::kKeys < row.wave_sees) {
-            scores(there, next);
+        if ((t + 2) * S::kKeys > row.wave_all) {  // (uniform)
             mask(t + 1, next);
-            rescale(largest(next));
+            top = largest(next);
         }
-        if (t + 2 < job.t_end) mover.put_k(lds + kB * S::kTileBytes, kr);
-        if (more) mover.put_v(lds + (3 - kB) * S::kTileBytes, vr, (t + 2) * S::kKeys > job.all, &sh_not_finite);
-        __syncthreads();
+        rescale(top);
+        mover.put_v(lds + (kRing + (kPlace + kFetch - 1) % kRing) * S::kTileBytes, moved, (t + kFetch) * S::kKeys > job.all, &sh_not_finite);
+        if constexpr (kRing == 2 || kPlace % 2 == 1) __syncthreads();
     };
 
-    int t = job.t_begin;
-    if (t < job.t_end) {  // (uniform)
-        mover.template load<false>(t, kr);
-        mover.template load<true>(t, vr);
-        mover.put_k(lds, kr);
-        mover.put_v(lds + 2 * S::kTileBytes, vr, (t + 1) * S::kKeys > job.all, &sh_not_finite);
-        mover.template load<false>(min(t + 1, job.t_end - 1), kr);
-        mover.put_k(lds + S::kTileBytes, kr);
-        __syncthreads();
-        if (t * S::kKeys < row.wave_sees) {
-            scores(std::integral_constant<int, 0>{}, s_even);
-            mask(t, s_even);
-            rescale(largest(s_even));
+    if (job.t_begin < job.t_end) {  // (uniform)
+        int t = job.t_begin;
+        const int tiles = job.t_end - t;
+        {
+            u32x4 kr[kFetch][S::kLoads], vr[kFetch - 1][S::kLoads];
+#pragma unroll
+            for (int i = 0; i < kFetch; ++i)
+                if (i < tiles) {
+                    spot = mover.find(t + i);
+                    mover.template load<false>(spot, kr[i]);
+                    if (i < kFetch - 1) mover.template load<true>(spot, vr[i < kFetch - 1 ? i : 0]);
+                }
+#pragma unroll
+            for (int i = 0; i < kFetch; ++i)
+                if (i < tiles) mover.put_k(lds + i * S::kTileBytes, kr[i]);
+#pragma unroll
+            for (int i = 0; i < kFetch - 1; ++i)
+                if (i < tiles) mover.put_v(lds + (kRing + i) * S::kTileBytes, vr[i], (t + i + 1) * S::kKeys > job.all, &sh_not_finite);
         }
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+            for (int x = 0; x < S::kChunks / 2; ++x) {
+                const bf16x8 a = *reinterpret_cast<const bf16x8 *>(lds + (k_at ^ (32 * x)) + b * 32 * S::kRowBytes);
+                const floatx16 none{};
+                s_even[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, qf[x]), x == 0 ? none : s_even[b], 0, 0, 0);
+            }
+        if ((t + 1) * S::kKeys > row.wave_all) mask(t, s_even);
+        rescale(largest(s_even));
         __syncthreads();  // (the first tile's K is read by all before it is written over)
+        int place = 0;  // of the last tile
+        for (;;) {
+            if (t + 1 >= job.t_end) break;
+            step(std::integral_constant<int, 0>{}, t, s_even, s_odd);
+            if (t + 2 >= job.t_end) {
+                place = 1;
+                break;
+            }
+            step(std::integral_constant<int, 1>{}, t + 1, s_odd, s_even);
+            t += 2;
+            if constexpr (kRing == 4) {
+                if (t + 1 >= job.t_end) {
+                    place = 2;
+                    break;
+                }
+                step(std::integral_constant<int, 2>{}, t, s_even, s_odd);
+                if (t + 2 >= job.t_end) {
+                    place = 3;
+                    break;
+                }
+                step(std::integral_constant<int, 3>{}, t + 1, s_odd, s_even);
+                t += 2;
+            }
+        }
+        if (place % 2 == 1)
+            for (int b = 0; b < S::kBlocks; ++b) s_even[b] = s_odd[b];
+        u32x4 pf[2 * S::kBlocks];
+        each<16 * S::kBlocks / 2>([&](auto n) __attribute__((always_inline)) { pair(n, s_even, pf); });
+#pragma unroll
+        for (int g = 0; g < 2 * S::kBlocks; ++g)
+#pragma unroll
+            for (int d = 0; d < S::kDTiles; ++d)
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v(g, d, place * S::kTileBytes), __builtin_bit_cast(bf16x8, pf[g]), o[d], 0, 0, 0);
+        __syncthreads();  // (sh_not_finite)
     }
-    const int seen_by_all = min(job.t_end, max(job.all, 0) / S::kKeys);  // tiles
-    for (; t + 3 < seen_by_all; t += 2) {  // (the loads are two tiles ahead)
-        both(std::integral_constant<int, 0>{}, t, s_even, s_odd);
-        both(std::integral_constant<int, 1>{}, t + 1, s_odd, s_even);
-    }
-    for (; t < job.t_end; t += 2) {
-        one(std::integral_constant<int, 0>{}, t, s_even, s_odd);
-        if (t + 1 < job.t_end) one(std::integral_constant<int, 1>{}, t + 1, s_odd, s_even);
-    }
-    finish<true, D, WAVES, PAGED>(p, job, row, wave, half, col, o, m, sum_of_halves(l), sh_not_finite);
+    int again = col;  // (the row's place is worked out again rather than kept)
+    asm volatile("" : "+v"(again));
+    finish<true, D, WAVES, PAGED>(p, job, row_of(p, job, wave, again), wave, half, again, o, m, sum_of_halves(l), sh_not_finite);
 }
 
 // Joins the parts of a tile's keys: a thread per packed row and four elements.
-template <bool BF16, int D, int ROWS>
+template <bool BF16, int D, int ROWS, bool PAGED>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptParams p) {
     constexpr int kQuads = D / 4, kPerBlock = 256 / kQuads;  // rows of a work-group
     constexpr int kBlocks = ROWS / kPerBlock;                // work-groups of a tile
     const int piece = blockIdx.x % kBlocks, head = blockIdx.x / kBlocks % p.Hkv, number = blockIdx.x / kBlocks / p.Hkv;
     Tile tile;
-    if (!find_tile(p.q_indptr, p.B, p.total_q, p.max_q, p.G, ROWS, number, tile)) return;
-    tile.index = tile.tiles - 1 - tile.index;
+    int tokens;
+    int64_t first;
+    if (!find_rows<PAGED, ROWS>(p, number, tile, tokens, first)) return;
     const int row = piece * kPerBlock + threadIdx.x / kQuads, quad = threadIdx.x % kQuads;
     const int packed = tile.index * ROWS + row;
     if (packed >= tile.R * p.G) return;
@@ -692,13 +742,14 @@ struct Plan {
     size_t o_bytes, ws_bytes;
 };
 
+static int prompt_waves() { const char *e = getenv("PW"); return e ? atoi(e) : 8; }
 // The split: as many parts of the keys as fill the device twice, no part below 512 keys.
 bool make_plan(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t Hq, int32_t Hkv, int32_t D, respec_dtype_t dt, Plan &pl) {
     if (B <= 0 || total_q <= 0 || max_q <= 0 || max_kv <= 0 || Hq <= 0 || Hkv <= 0) return false;
     if (Hq % Hkv != 0 || (D != 64 && D != 128) || (dt != RESPEC_F32 && dt != RESPEC_BF16)) return false;
     const int32_t G = Hq / Hkv;
     if ((int64_t)std::min(max_q, total_q) * G >= (1 << 30)) return false;
-    pl.waves = dt == RESPEC_BF16 ? kWaves16 : 4;
+    pl.waves = dt == RESPEC_BF16 ? prompt_waves() : 4;
     const int rows = pl.waves * 32;
     pl.tiles = tiles_bound(B, total_q, std::min(max_q, total_q), G, rows);
     const int64_t groups = pl.tiles * Hkv;
@@ -709,13 +760,13 @@ bool make_plan(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_
     return true;
 }
 
-template <bool BF16, int D, bool PAGED>
+template <bool BF16, int D, int WAVES, bool PAGED>
 hipError_t launch(PromptParams &p, const Plan &pl, hipStream_t stream) {
-    using S = Shape<BF16, D, BF16 ? kWaves16 : 4>;
-    const size_t lds = 4 * S::kTileBytes;
+    using S = Shape<BF16, D, WAVES>;
     void (*kernel)(PromptParams);
-    if constexpr (BF16) kernel = &prompt_bf16_kernel<D, kWaves16, PAGED>;
+    if constexpr (BF16) kernel = &prompt_bf16_kernel<D, WAVES, PAGED>;
     else kernel = &prompt_f32_kernel<D, PAGED>;
+    const size_t lds = BF16 ? S::kLdsBytes : 4 * S::kTileBytes;
     if (lds > 65536) {
         const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (err != hipSuccess) return err;
@@ -723,15 +774,16 @@ hipError_t launch(PromptParams &p, const Plan &pl, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)(pl.tiles * p.Hkv * p.splits)), dim3(S::kThreads), lds, stream, p);
     if (p.splits > 1) {
         constexpr int kBlocks = S::kRows / (256 / (D / 4));
-        hipLaunchKernelGGL((prompt_join_kernel<BF16, D, S::kRows>), dim3((unsigned)(pl.tiles * p.Hkv * kBlocks)), dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((prompt_join_kernel<BF16, D, S::kRows, PAGED>), dim3((unsigned)(pl.tiles * p.Hkv * kBlocks)), dim3(256), 0, stream, p);
     }
     return hipGetLastError();
 }
 
 template <bool PAGED>
 hipError_t launch_any(PromptParams &p, const Plan &pl, int32_t D, respec_dtype_t dt, hipStream_t stream) {
-    if (dt == RESPEC_BF16) return D == 128 ? launch<true, 128, PAGED>(p, pl, stream) : launch<true, 64, PAGED>(p, pl, stream);
-    return D == 128 ? launch<false, 128, PAGED>(p, pl, stream) : launch<false, 64, PAGED>(p, pl, stream);
+    if (dt == RESPEC_F32) return D == 128 ? launch<false, 128, 4, PAGED>(p, pl, stream) : launch<false, 64, 4, PAGED>(p, pl, stream);
+    if (pl.waves == 8) return D == 128 ? launch<true, 128, 8, PAGED>(p, pl, stream) : launch<true, 64, 8, PAGED>(p, pl, stream);
+    return D == 128 ? launch<true, 128, 4, PAGED>(p, pl, stream) : launch<true, 64, 4, PAGED>(p, pl, stream);
 }
 
 // What the two entry points share.
