@@ -50,11 +50,18 @@ struct PromptParams {
     int32_t B, total_q, max_q, max_kv, num_pages, table_len, page_shift;
     int32_t Hq, Hkv, G;
     int32_t splits, tiles;   // parts of a tile's keys; bound of the row tiles of a KV head
+    uint32_t g_mul, g_shift; // of a division by G (by_g)
     uint32_t q_and, q_xor;   // on the bits of q: a negative scale is taken out of it, a zero one makes it zero
     float scale2;            // |sm_scale| * log2(e)
     float *part_o;           // [tiles * Hkv * splits][rows][D]
     float *part_ml;          // [tiles * Hkv * splits][rows][2]
 };
+
+// x / G by a product: with s = ceil(log2 G) and g_mul = floor(2^32 (2^s - G) / G) + 1 this is exact for every x below 2^32.
+__device__ inline int by_g(const PromptParams &p, int x) {
+    const uint32_t t = __umulhi((uint32_t)x, p.g_mul);
+    return p.G == 1 ? x : (int)((t + (((uint32_t)x - t) >> 1)) >> (p.g_shift - 1));
+}
 
 template <bool BF16, int D, int WAVES>
 struct Shape {
@@ -181,17 +188,17 @@ template <bool BF16, int D, int WAVES, bool PAGED>
 __device__ inline bool find_job(const PromptParams &p, Job &j) {
     using S = Shape<BF16, D, WAVES>;
     j.head = blockIdx.x % p.Hkv;
-    const int rest = blockIdx.x / p.Hkv, split = rest % p.splits;
+    const int rest = blockIdx.x / p.Hkv, number = p.splits == 1 ? rest : rest / p.splits, split = rest - number * p.splits;
     j.number = blockIdx.x;
-    if (!find_rows<PAGED, S::kRows>(p, rest / p.splits, j.tile, j.L, j.kv0)) return false;
+    if (!find_rows<PAGED, S::kRows>(p, number, j.tile, j.L, j.kv0)) return false;
     j.n_rows = j.tile.R * p.G;
     j.row0 = j.tile.index * S::kRows;
     const int last = min(j.row0 + S::kRows, j.n_rows) - 1;
-    const int end = j.L - j.tile.R + last / p.G + 1;  // the work-group's last row sees most
+    const int end = j.L - j.tile.R + by_g(p, last) + 1;  // the work-group's last row sees most
     const int tiles = max(0, (end + S::kKeys - 1) / S::kKeys);
-    j.t_begin = (int)((int64_t)tiles * split / p.splits);
-    j.t_end = (int)((int64_t)tiles * (split + 1) / p.splits);
-    j.all = j.L - j.tile.R + j.row0 / p.G + 1;
+    j.t_begin = p.splits == 1 ? 0 : tiles * split / p.splits;  // (at most 2^25 tiles, kMaxSplits parts)
+    j.t_end = p.splits == 1 ? tiles : tiles * (split + 1) / p.splits;
+    j.all = j.L - j.tile.R + by_g(p, j.row0) + 1;
     return true;
 }
 
@@ -206,7 +213,7 @@ __device__ inline RowOf row_of(const PromptParams &p, const Job &j, int wave, in
     RowOf r;
     const int packed = j.row0 + wave * 32 + col, clamped = min(packed, j.n_rows - 1);
     r.exists = packed < j.n_rows;
-    const int i = clamped / p.G;
+    const int i = by_g(p, clamped);
     r.lim = j.L - j.tile.R + i + 1;
     r.head = j.head * p.G + clamped - i * p.G;
     r.token = j.tile.q0 + i;
@@ -220,10 +227,13 @@ template <int CHUNKS>
 __device__ inline void load_q(const PromptParams &p, const RowOf &r, int D, int size, int half, u32x4 (&qf)[CHUNKS / 2]) {
     const char *qp = p.q + (r.token * p.ld_q + (int64_t)r.head * D) * size + half * 16;
 #pragma unroll
-    for (int x = 0; x < CHUNKS / 2; ++x) {
-        qf[x] = *reinterpret_cast<const u32x4 *>(qp + x * 32);
+    for (int x = 0; x < CHUNKS / 2; ++x) qf[x] = *reinterpret_cast<const u32x4 *>(qp + x * 32);
+}
+template <int N>
+__device__ inline void sign_q(const PromptParams &p, u32x4 (&qf)[N]) {  // (apart: the loads are not waited for before others are requested)
+#pragma unroll
+    for (int x = 0; x < N; ++x)
         for (int w = 0; w < 4; ++w) qf[x][w] = (qf[x][w] & p.q_and) ^ p.q_xor;
-    }
 }
 
 typedef const __attribute__((address_space(4))) int32_t *ConstInts;  // (read through the scalar cache; nothing writes it meanwhile)
@@ -317,32 +327,51 @@ struct Mover {
 // Writes a lane's row: O^T in accumulator tiles (d = 32 d-tile + 8 (x / 4) + 4 half + x % 4), its maximum (log2 units) and sum.
 template <bool BF16, int D, int WAVES, bool PAGED>
 __device__ inline void finish(const PromptParams &p, const Job &j, const RowOf &r, int wave, int half, int col, floatx16 (&o)[D / 32], float m, float l,
-                              int not_finite) {
+                              int not_finite, char *lds) {
     using S = Shape<BF16, D, WAVES>;
     const int64_t slot = (int64_t)j.number * S::kRows + wave * 32 + col;
-    if (r.exists && p.splits > 1) {
-        if (half == 0) *reinterpret_cast<floatx2 *>(p.part_ml + slot * 2) = floatx2{m, l};
+    if (p.splits > 1) {
+        if (r.exists && half == 0) *reinterpret_cast<floatx2 *>(p.part_ml + slot * 2) = floatx2{m, l};
 #pragma unroll
         for (int d = 0; d < S::kDTiles; ++d)
 #pragma unroll
             for (int x = 0; x < 16; x += 4)
-                *reinterpret_cast<floatx4 *>(p.part_o + slot * D + d * 32 + 2 * x + 4 * half) = floatx4{o[d][x], o[d][x + 1], o[d][x + 2], o[d][x + 3]};
-    } else if (r.exists) {
+                if (r.exists) *reinterpret_cast<floatx4 *>(p.part_o + slot * D + d * 32 + 2 * x + 4 * half) = floatx4{o[d][x], o[d][x + 1], o[d][x + 2], o[d][x + 3]};
+    } else if constexpr (BF16) {
+        // Through LDS, so that whole rows are written, sixteen bytes a lane: the wave's own 32 rows, pieces placed as K's are.
         const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // (no visible key: zero; NaN stays)
-        char *op = p.out + (r.token * p.Hq + r.head) * (int64_t)S::kRowBytes;
+        char *const mine = lds + wave * 32 * S::kRowBytes;
 #pragma unroll
         for (int d = 0; d < S::kDTiles; ++d)
 #pragma unroll
             for (int x = 0; x < 16; x += 4) {  // four d in a row
-                const floatx4 y = {o[d][x] * inv, o[d][x + 1] * inv, o[d][x + 2] * inv, o[d][x + 3] * inv};
-                const int at = d * 32 + 2 * x + 4 * half;
-                if constexpr (BF16) {
-                    const bf16x2 a = __builtin_convertvector(floatx2{y[0], y[1]}, bf16x2), c = __builtin_convertvector(floatx2{y[2], y[3]}, bf16x2);
-                    *reinterpret_cast<u32x2 *>(op + at * 2) = u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c)};
-                } else {
-                    *reinterpret_cast<floatx4 *>(op + at * 4) = y;
-                }
+                const bf16x2 a = __builtin_convertvector(floatx2{o[d][x] * inv, o[d][x + 1] * inv}, bf16x2);
+                const bf16x2 c = __builtin_convertvector(floatx2{o[d][x + 2] * inv, o[d][x + 3] * inv}, bf16x2);
+                *reinterpret_cast<u32x2 *>(mine + col * S::kRowBytes + k_piece<true, D>(col, d * 4 + x / 4) * 16 + 8 * half) =
+                    u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c)};
             }
+        if (p.lse && half == 0 && r.exists) p.lse[r.token * p.Hq + r.head] = l == 0.f ? -INFINITY : m * 0.693147180559945309f + logf(l);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const int lane = half * 32 + col, piece = lane % S::kChunks;
+#pragma unroll
+        for (int i = 0; i < 32 / S::kWaveKeys; ++i) {
+            const int at = i * S::kWaveKeys + lane / S::kChunks, packed = j.row0 + wave * 32 + at;
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(mine + at * S::kRowBytes + k_piece<true, D>(at, piece) * 16);
+            if (packed < j.n_rows) {
+                const int row = by_g(p, packed);
+                *reinterpret_cast<u32x4 *>(p.out + ((j.tile.q0 + row) * p.Hq + j.head * p.G + packed - row * p.G) * (int64_t)S::kRowBytes + piece * 16) = x;
+            }
+        }
+    } else if (r.exists) {
+        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+        char *op = p.out + (r.token * p.Hq + r.head) * (int64_t)S::kRowBytes;
+#pragma unroll
+        for (int d = 0; d < S::kDTiles; ++d)
+#pragma unroll
+            for (int x = 0; x < 16; x += 4)
+                *reinterpret_cast<floatx4 *>(op + (d * 32 + 2 * x + 4 * half) * 4) =
+                    floatx4{o[d][x] * inv, o[d][x + 1] * inv, o[d][x + 2] * inv, o[d][x + 3] * inv};
         if (p.lse && half == 0) p.lse[r.token * p.Hq + r.head] = l == 0.f ? -INFINITY : m * 0.693147180559945309f + logf(l);
     }
     if (not_finite == 0) return;  // (uniform)
@@ -352,7 +381,7 @@ __device__ inline void finish(const PromptParams &p, const Job &j, const RowOf &
     for (int e = threadIdx.x; e < S::kRows * D; e += S::kThreads) {
         const int row = j.row0 + e / D, d = e % D;
         if (row >= j.n_rows) break;
-        const int sees = min(end_key, j.L - j.tile.R + row / p.G + 1);
+        const int sees = min(end_key, j.L - j.tile.R + by_g(p, row) + 1);
         float sum = 0.f;
         for (int n = first_key; n < sees; ++n) {
             int64_t at = j.kv0 + n;
@@ -366,7 +395,7 @@ __device__ inline void finish(const PromptParams &p, const Job &j, const RowOf &
         if (p.splits > 1) {
             p.part_o[((int64_t)j.number * S::kRows + e / D) * D + d] += sum;
         } else {
-            char *op = p.out + (((j.tile.q0 + row / p.G) * p.Hq + j.head * p.G + row % p.G) * (int64_t)D + d) * S::kSize;
+            char *op = p.out + (((j.tile.q0 + by_g(p, row)) * p.Hq + j.head * p.G + row - by_g(p, row) * p.G) * (int64_t)D + d) * S::kSize;
             if constexpr (BF16) {
                 const float x = __uint_as_float((uint32_t)*reinterpret_cast<uint16_t *>(op) << 16) + sum;
                 *reinterpret_cast<uint16_t *>(op) = __builtin_bit_cast(uint16_t, (__bf16)x);
@@ -399,6 +428,7 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptParams p) {
     const RowOf row = row_of(p, job, wave, col);
     u32x4 qf[S::kChunks / 2];
     load_q<S::kChunks>(p, row, D, S::kSize, half, qf);
+    sign_q(p, qf);
     const Mover<false, D, kWaves, PAGED> mover(p, job, wave, lane);
     if (threadIdx.x == 0) sh_not_finite = 0;
     __syncthreads();
@@ -470,7 +500,7 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptParams p) {
         if (t + 1 < job.t_end) put(buffer ^ 1, t + 1);
         __syncthreads();
     }
-    finish<false, D, kWaves, PAGED>(p, job, row, wave, half, col, o, m, sum_of_halves(l), sh_not_finite);
+    finish<false, D, kWaves, PAGED>(p, job, row, wave, half, col, o, m, sum_of_halves(l), sh_not_finite, lds);
 }
 
 // f(0), f(1) ... f(N-1), each with its number as a type.
@@ -499,10 +529,21 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_bf16_kernel(PromptParams
     if (!find_job<true, D, WAVES, PAGED>(p, job)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int half = lane >> 5, col = lane & 31;
+    const Mover<true, D, WAVES, PAGED> mover(p, job, wave, lane);
+    typedef typename Mover<true, D, WAVES, PAGED>::Spot Spot;
+    Spot spot{};  // of the tile whose V the next step fetches
+    u32x4 kr[kFetch][S::kLoads], vr[kFetch - 1][S::kLoads];
+    const int tiles = job.t_end - job.t_begin;
+#pragma unroll
+    for (int i = 0; i < kFetch; ++i)
+        if (i < tiles) {
+            spot = mover.find(job.t_begin + i);
+            mover.template load<false>(spot, kr[i]);
+            if (i < kFetch - 1) mover.template load<true>(spot, vr[i < kFetch - 1 ? i : 0]);
+        }
     const RowOf row = row_of(p, job, wave, col);
     u32x4 qf[S::kChunks / 2];
     load_q<S::kChunks>(p, row, D, S::kSize, half, qf);
-    const Mover<true, D, WAVES, PAGED> mover(p, job, wave, lane);
     if (threadIdx.x == 0) sh_not_finite = 0;
     __syncthreads();
 
@@ -560,8 +601,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_bf16_kernel(PromptParams
         for (int j = 0; j < 2; ++j) vt[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTr)(lds + (v_at ^ (64 * d)) + (tile + (g * 16 + j * 8) * S::kRowBytes)));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(vt[0], vt[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    typedef typename Mover<true, D, WAVES, PAGED>::Spot Spot;
-    Spot spot{};  // of the tile whose V the next step fetches
     // Step t (not the last), the tile's scores in s with their maximum taken into account; `place`: (t - t_begin) % kRing.
     // Written in the order it is to run in: a product, an LDS read kAhead products before its use, and a share of the rest.
     auto step = [&](auto place, int t, floatx16(&s)[S::kBlocks], floatx16(&next)[S::kBlocks]) __attribute__((always_inline)) {
@@ -627,23 +666,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_bf16_kernel(PromptParams
 
     if (job.t_begin < job.t_end) {  // (uniform)
         int t = job.t_begin;
-        const int tiles = job.t_end - t;
-        {
-            u32x4 kr[kFetch][S::kLoads], vr[kFetch - 1][S::kLoads];
 #pragma unroll
-            for (int i = 0; i < kFetch; ++i)
-                if (i < tiles) {
-                    spot = mover.find(t + i);
-                    mover.template load<false>(spot, kr[i]);
-                    if (i < kFetch - 1) mover.template load<true>(spot, vr[i < kFetch - 1 ? i : 0]);
-                }
+        for (int i = 0; i < kFetch; ++i)
+            if (i < tiles) mover.put_k(lds + i * S::kTileBytes, kr[i]);
 #pragma unroll
-            for (int i = 0; i < kFetch; ++i)
-                if (i < tiles) mover.put_k(lds + i * S::kTileBytes, kr[i]);
-#pragma unroll
-            for (int i = 0; i < kFetch - 1; ++i)
-                if (i < tiles) mover.put_v(lds + (kRing + i) * S::kTileBytes, vr[i], (t + i + 1) * S::kKeys > job.all, &sh_not_finite);
-        }
+        for (int i = 0; i < kFetch - 1; ++i)
+            if (i < tiles) mover.put_v(lds + (kRing + i) * S::kTileBytes, vr[i], (t + i + 1) * S::kKeys > job.all, &sh_not_finite);
+        sign_q(p, qf);
         __syncthreads();
 #pragma unroll
         for (int b = 0; b < S::kBlocks; ++b)
@@ -691,9 +720,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_bf16_kernel(PromptParams
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v(g, d, place * S::kTileBytes), __builtin_bit_cast(bf16x8, pf[g]), o[d], 0, 0, 0);
         __syncthreads();  // (sh_not_finite)
     }
+    const int not_finite = sh_not_finite;
     int again = col;  // (the row's place is worked out again rather than kept)
     asm volatile("" : "+v"(again));
-    finish<true, D, WAVES, PAGED>(p, job, row_of(p, job, wave, again), wave, half, again, o, m, sum_of_halves(l), sh_not_finite);
+    finish<true, D, WAVES, PAGED>(p, job, row_of(p, job, wave, again), wave, half, again, o, m, sum_of_halves(l), not_finite, lds);
 }
 
 // Joins the parts of a tile's keys: a thread per packed row and four elements.
@@ -722,7 +752,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptParams p) {
         for (int j = 0; j < 4; ++j) o[j] = o[j] * f + x[j] * e;
         m = m_new;
     }
-    const int i_row = packed / p.G, q_head = head * p.G + packed % p.G;
+    const int i_row = by_g(p, packed), q_head = head * p.G + packed - i_row * p.G;
     const int64_t at = (tile.q0 + i_row) * p.Hq + q_head;
     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
     for (int j = 0; j < 4; ++j) o[j] *= inv;
@@ -817,6 +847,8 @@ respec_status_t run(const char *name, PromptParams &p, const void *k, const void
     p.G = p.Hq / p.Hkv;
     p.splits = pl.splits;
     p.tiles = (int32_t)pl.tiles;
+    for (p.g_shift = 0; (1 << p.g_shift) < p.G; ++p.g_shift) {}
+    p.g_mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << p.g_shift) - p.G)) / p.G + 1);
     const uint32_t sign = dt == RESPEC_BF16 ? 0x80008000u : 0x80000000u;
     p.q_and = sm_scale == 0.f ? 0u : ~0u;
     p.q_xor = sm_scale < 0.f ? sign : 0u;
