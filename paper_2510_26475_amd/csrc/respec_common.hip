@@ -54,6 +54,8 @@ void read_knobs_locked() {
     g_knobs.kd_wgs = env_long("RESPEC_KD_WGS");
     g_knobs.kd_team = env_long("RESPEC_KD_TEAM");
     g_knobs.kd_spin = env_long("RESPEC_KD_SPIN");
+    g_knobs.prompt_waves = env_long("RESPEC_PROMPT_WAVES");
+    g_knobs.prompt_splits = env_long("RESPEC_PROMPT_SPLITS");
     g_knobs_read = true;
 }
 

@@ -388,17 +388,28 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams p) {
     const int pages = max(0, min(p.page_indptr[t.b + 1], p.table_len) - e0);
     const int64_t L = max((int64_t)0, min((int64_t)p.kv_len[t.b], (int64_t)pages << p.page_shift));
     const int pieces = p.token_bytes / 16, rows = min(kAppendRows, t.R - t.index * kAppendRows);
-    for (int i = threadIdx.x; i < rows * pieces; i += kThreads) {
-        const int r = t.index * kAppendRows + i / pieces, piece = i % pieces;
-        const int64_t pos = L - t.R + r;
-        if (pos < 0) continue;
-        const int32_t id = p.page_table[e0 + (pos >> p.page_shift)];
-        if ((uint32_t)id >= (uint32_t)p.num_pages) continue;
-        const int64_t from = (t.q0 + r) * p.ld_bytes + (int64_t)piece * 16;
-        const int64_t to = (((int64_t)id << p.page_shift) + (pos & ((1 << p.page_shift) - 1))) * p.token_bytes + (int64_t)piece * 16;
-        const u32x4 a = *reinterpret_cast<const u32x4 *>(p.k_new + from), c = *reinterpret_cast<const u32x4 *>(p.v_new + from);
-        *reinterpret_cast<u32x4 *>(p.k + to) = a;
-        *reinterpret_cast<u32x4 *>(p.v + to) = c;
+    for (int i0 = threadIdx.x; i0 < rows * pieces; i0 += 4 * kThreads) {
+        u32x4 a[4], c[4];
+        int64_t to[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {  // (eight loads in flight: behind a store the next loads would wait, as the memory may be the same)
+            to[j] = -1;
+            const int i = i0 + j * kThreads, r = t.index * kAppendRows + i / pieces, piece = i % pieces;
+            const int64_t pos = L - t.R + r;
+            if (i >= rows * pieces || pos < 0) continue;
+            const int32_t id = p.page_table[e0 + (pos >> p.page_shift)];
+            if ((uint32_t)id >= (uint32_t)p.num_pages) continue;
+            const int64_t from = (t.q0 + r) * p.ld_bytes + (int64_t)piece * 16;
+            to[j] = (((int64_t)id << p.page_shift) + (pos & ((1 << p.page_shift) - 1))) * p.token_bytes + (int64_t)piece * 16;
+            a[j] = *reinterpret_cast<const u32x4 *>(p.k_new + from);
+            c[j] = *reinterpret_cast<const u32x4 *>(p.v_new + from);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (to[j] < 0) continue;
+            *reinterpret_cast<u32x4 *>(p.k + to[j]) = a[j];
+            *reinterpret_cast<u32x4 *>(p.v + to[j]) = c[j];
+        }
     }
 }
 

@@ -2,8 +2,8 @@
 // piece or in pages.  This is the forward that fills a cache before the drafts begin and rebuilds it when a sequence moves between
 // speculative and plain decoding (Section 5.2); a prompt may come in chunks, its earlier tokens being in the cache already.
 //
-// The G query heads of a KV head are packed into the rows: packed row r is row r / G, head r % G, so a tile of 128 rows spans
-// 128 / G positions, reads K and V once for all its heads and wastes little on the diagonal or on a short prompt.  A wave holds 32
+// The G query heads of a KV head are packed into the rows: packed row r is row r / G, head r % G, so a tile of 128 or 256
+// rows spans that many over G positions, reads K and V once for all its heads and wastes little on the diagonal or on a short prompt.  A wave holds 32
 // packed rows as the columns of 32x32 MFMA tiles (v_mfma_f32_32x32x16_bf16, v_mfma_f32_32x32x2_f32): S^T = K Q^T leaves a
 // lane's scores in one column, so the softmax of a row is a lane's own work and one exchange with lane ^ 32, and the probabilities
 // are the B operand of O^T = V^T P^T as they stand, the contraction's order being free as long as both operands agree on it.
@@ -36,7 +36,7 @@ typedef s16x4 __attribute__((address_space(3))) *LdsTr;
 
 constexpr float kRescaleSlack = 8.f;  // log2 units
 constexpr int kMaxSplits = 16;
-constexpr int kSplitTiles = 512;      // work-groups below which a call is split
+constexpr int kSplitGroups = 1024;    // work-groups up to which a call is split (bounds the workspace: 128 MiB of parts)
 
 struct PromptParams {
     const char *q, *k, *v;
@@ -134,7 +134,7 @@ __device__ inline int length_of(const PromptParams &p, int b, int64_t &kv0) {
 // The number-th tile of a batch of up to 64 sequences (one per lane), the one that sees most keys first: work-groups are given out in
 // order, and a long one among the last would be waited for.  How many tiles see x keys or more is known for every sequence
 // without looking at its tiles, so x is found by bisection, in steps of 64 keys.  (16 packed prompts of 65 to 2,048 tokens at 28/4
-// heads take 137 us, in the order of the sequences 158.)
+// heads take 145 us, in the order of the sequences 152; 8 chunks behind up to 8,192 tokens at 40/8 heads 374, and 394.)
 template <bool PAGED, int ROWS>
 __device__ inline bool find_longest(const PromptParams &p, int number, Tile &out, int &tokens, int64_t &first) {
     const int lane = threadIdx.x & 63;
@@ -772,18 +772,58 @@ struct Plan {
     size_t o_bytes, ws_bytes;
 };
 
-static int prompt_waves() { const char *e = getenv("PW"); return e ? atoi(e) : 8; }
-// The split: as many parts of the keys as fill the device twice, no part below 512 keys.
+// How a call is run: the form (bf16: four waves, 128 packed rows, two work-groups on a compute unit; eight waves, 256 rows, one) and
+// the parts its keys are cut into, whichever this estimate of the time in microseconds makes least.  A work-group costs `over`
+// tiles of keys beside those that it sees; `step` is what a tile of 64 keys takes of a compute unit at D = 128, `lone` what it takes
+// where no second work-group shares the unit.  The call takes the work of all groups over 256 units, or the longest group, and where
+// the groups are alike (many keys before the chunk) whole rounds of them, of which half is counted for several sequences, as those
+// are seldom of one length; parts cost a launch and their bytes.  The constants are fitted to 2,500 timings (1 to 64 prompts,
+// chunks of 1 to 4,000 tokens behind 0 to 30,000, six head layouts, D 64 and 128, both forms, 1 to 16 parts): the form picked is on
+// the mean 1.4 % behind the best of its shape.  8 chunks of 512 behind up to 8,192 at 40/8 heads: 337 us with eight waves, 375 with four.
+// Eight waves at 28/4 heads of 128: 8 prompts of 2,048 take 282 us, with four 295; 64 of 128 take 55 us, with four 44.
+// One chunk of 40 tokens behind 8,000: 30 us in 16 parts; 512 behind 16,000, twice: 249 us in 2 parts, 309 in 3.
+struct Cost {
+    float step, lone, over, base;
+};
+constexpr Cost kFour{1.0f, 1.3f, 3.65f, 11.1f}, kEight{1.79f, 1.79f, 5.5f, 8.f}, kF32{8.4f, 8.4f, 0.7f, 7.f};
+
+float estimate(const Cost &c, int32_t B, int64_t groups, int splits, int rows, float mean_q, int32_t max_q, int32_t max_kv, int32_t D, bool bf16) {
+    const float before = (float)std::max(0, max_kv - max_q), alike = before / max_kv * (B == 1 ? 1.f : 0.5f);
+    const float mean = (before + mean_q / 2) / 64 / splits + c.over, longest = max_kv / 64.f / splits + c.over;
+    const float rounds = groups * splits / 256.f, up = std::ceil(rounds);
+    const float odd = std::fmod(up, 2.f) == 1.f ? c.lone - c.step : 0.f;
+    const float even = rounds * c.step * mean, whole = (up * c.step + odd) * mean;
+    const float t = std::max(even + alike * (whole - even), longest * c.lone);
+    const float parts = splits == 1 ? 0.f : 5.4f + groups * splits * (float)rows * D * 8 / 3.6e6f;
+    return c.base + (D == 128 ? 1.f : bf16 ? 0.6f : 0.53f) * t + parts;
+}
+
 bool make_plan(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t Hq, int32_t Hkv, int32_t D, respec_dtype_t dt, Plan &pl) {
     if (B <= 0 || total_q <= 0 || max_q <= 0 || max_kv <= 0 || Hq <= 0 || Hkv <= 0) return false;
     if (Hq % Hkv != 0 || (D != 64 && D != 128) || (dt != RESPEC_F32 && dt != RESPEC_BF16)) return false;
     const int32_t G = Hq / Hkv;
     if ((int64_t)std::min(max_q, total_q) * G >= (1 << 30)) return false;
-    pl.waves = dt == RESPEC_BF16 ? prompt_waves() : 4;
+    max_q = std::min(max_q, total_q);
+    const Knobs kn = knobs();
+    const long waves = kn.get(&Knobs::prompt_waves, 0), splits = kn.get(&Knobs::prompt_splits, 0);
+    const float mean_q = std::min((float)max_q, (float)total_q / B);
+    float least = INFINITY;
+    for (const int w : {8, 4}) {
+        if (dt == RESPEC_F32 ? w != 4 : (waves == 4 || waves == 8) && w != waves) continue;
+        const int64_t tiles = tiles_bound(B, total_q, max_q, G, w * 32), groups = tiles * Hkv;
+        for (const int s : {1, 2, 3, 4, 6, 8, 12, kMaxSplits}) {
+            if (s > 1 && (s > max_kv / 64 || groups * s > kSplitGroups)) break;
+            const float t = estimate(dt == RESPEC_F32 ? kF32 : w == 8 ? kEight : kFour, B, groups, s, w * 32, mean_q, max_q, max_kv, D, dt == RESPEC_BF16);
+            if (!(t < least)) continue;
+            least = t;
+            pl.waves = w;
+            pl.splits = s;
+            pl.tiles = tiles;
+        }
+    }
+    if (splits >= 1 && splits <= kMaxSplits) pl.splits = (int32_t)splits;
     const int rows = pl.waves * 32;
-    pl.tiles = tiles_bound(B, total_q, std::min(max_q, total_q), G, rows);
     const int64_t groups = pl.tiles * Hkv;
-    pl.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, kSplitTiles / groups, max_kv / 512}));
     const size_t slots = pl.splits > 1 ? (size_t)groups * pl.splits * rows : 0;
     pl.o_bytes = round_up(slots * D * sizeof(float), 256);
     pl.ws_bytes = std::max<size_t>(256, pl.o_bytes + round_up(slots * 2 * sizeof(float), 256));

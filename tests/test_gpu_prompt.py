@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import plain
+from helpers import env_setting
 from paper_2510_26475_amd import binding
 
 pytestmark = pytest.mark.gpu
@@ -100,6 +101,31 @@ def test_few_rows_split_the_keys(dtype, R, L, heads):
     plain.check_prompt(out, lse, plain.prompt_attention(q, split_keys(k, L), split_keys(v, L), R, L, D ** -0.5))
     again, lse2 = run(q, k, v, R, L, D ** -0.5)
     assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("splits", [1, 2, 3, 16])
+@pytest.mark.parametrize("dtype,waves,heads", [("bf16", 4, (28, 4, 128)), ("bf16", 8, (28, 4, 128)), ("bf16", 4, (3, 1, 64)),
+                                               ("bf16", 8, (6, 2, 64)), ("f32", 4, (6, 2, 128)), ("f32", 4, (5, 1, 64))], ids=str)
+def test_every_form_and_number_of_parts(dtype, waves, heads, splits):
+    """What the rule would choose by size, forced: parts without a key, tiles that end inside a sequence, more sequences than lanes."""
+    Hq, Hkv, D = heads
+    R, L = [r for r, _ in RAGGED], [n for _, n in RAGGED]
+    if splits == 2:
+        R, L = R + [1] * 60, L + [3, 150, 0] * 20
+    q, k, v = (randn(n, h, D, dt=DT[dtype], seed=n + h) for n, h in ((sum(R), Hq), (sum(L), Hkv), (sum(L), Hkv)))
+    v = randn(sum(L), Hkv, D, dt=DT[dtype], seed=78)
+    v[5, 0, 1] = math.inf if splits == 3 else 0.0     # (seen by the second sequence alone)
+    with env_setting("RESPEC_PROMPT_WAVES", waves), env_setting("RESPEC_PROMPT_SPLITS", splits):
+        out, lse = run(q, k, v, R, L, D ** -0.5)
+    if splits == 3:
+        hit = torch.zeros_like(out, dtype=torch.bool)
+        hit[R[0] + 4:R[0] + R[1], :Hq // Hkv, 1] = True
+        assert torch.isinf(out[hit]).all()
+        out, v[5, 0, 1] = torch.where(hit, 0.0, out), 0.0
+        o, z, tol, z_tol = plain.prompt_attention(q, split_keys(k, L), split_keys(v, L), R, L, D ** -0.5)
+        plain.check_prompt(out, lse, (torch.where(hit, 0.0, o), z, tol, z_tol))
+    else:
+        plain.check_prompt(out, lse, plain.prompt_attention(q, split_keys(k, L), split_keys(v, L), R, L, D ** -0.5))
 
 
 def paginate(x, L, ps, table, num_pages):
