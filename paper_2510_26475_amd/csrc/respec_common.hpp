@@ -46,7 +46,7 @@ struct Knobs {
     long kd_wgs;            // RESPEC_KD_WGS: work-groups of the distillation kernel
     long kd_team;           // RESPEC_KD_TEAM: 0 = one work-group per row pair, which it streams twice
     long kd_spin;           // RESPEC_KD_SPIN: 10 ns ticks that a member's part of a row is waited for
-    long prompt_waves;      // RESPEC_PROMPT_WAVES: 4/8 waves per work-group of the bf16 prompt attention
+    long prompt_waves;      // RESPEC_PROMPT_WAVES: waves that share a tile of keys in the prompt attention (bf16 4/8, fp32 1/4)
     long prompt_splits;     // RESPEC_PROMPT_SPLITS: parts (1-16) the keys of its row tiles are cut into
     long get(long Knobs::*field, long fallback) const { return this->*field == kUnset ? fallback : this->*field; }
 };

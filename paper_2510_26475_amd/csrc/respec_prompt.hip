@@ -375,8 +375,13 @@ __device__ inline void finish(const PromptParams &p, const Job &j, const RowOf &
         if (p.lse && half == 0) p.lse[r.token * p.Hq + r.head] = l == 0.f ? -INFINITY : m * 0.693147180559945309f + logf(l);
     }
     if (not_finite == 0) return;  // (uniform)
-    // The values that put_v left out, added to what the work-group has written: a row and a d of it per thread.
-    __syncthreads();
+    // The values that put_v left out, added to what the work-group (WAVES = 1: the wave) has written: a row and a d of it per thread.
+    if constexpr (WAVES > 1) {
+        __syncthreads();
+    } else {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        __builtin_amdgcn_wave_barrier();
+    }
     const int first_key = max(j.t_begin, j.all / S::kKeys) * S::kKeys, end_key = j.t_end * S::kKeys;
     for (int e = threadIdx.x; e < S::kRows * D; e += S::kThreads) {
         const int row = j.row0 + e / D, d = e % D;
@@ -413,25 +418,34 @@ __device__ inline void mask_scores(floatx16 &s, int first_key, int half, int lim
         if (first_key + 8 * (x / 4) + 4 * half + x % 4 >= lim) s[x] = -INFINITY;
 }
 
-// fp32: one tile of 32 keys after the other.
-template <int D, bool PAGED>
-__global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptParams p) {
-    constexpr int kWaves = 4;
-    using S = Shape<false, D, kWaves>;
-    extern __shared__ __align__(16) char lds[];  // two tiles of K, two of V
+// fp32: one tile of 32 keys after the other.  WAVES = 4: four waves of 32 rows each read the same tiles, two of K and two of V in
+// LDS.  WAVES = 1: the four waves of a work-group hold the same 32 rows, each takes every fourth tile, through LDS of its own
+// and without a barrier, and the first one joins what they found.
+template <int D, int WAVES, bool PAGED>
+__global__ __launch_bounds__(256, WAVES == 4 ? 2 : 1) void prompt_f32_kernel(PromptParams p) {
+    using S = Shape<false, D, WAVES>;
+    constexpr bool kShared = WAVES == 4;
+    constexpr int kStride = kShared ? 1 : 4;
+    extern __shared__ __align__(16) char lds[];
     __shared__ int sh_not_finite;
-    char *const lds_k = lds, *const lds_v = lds + 2 * S::kTileBytes;
     Job job;
-    if (!find_job<false, D, kWaves, PAGED>(p, job)) return;
+    if (!find_job<false, D, WAVES, PAGED>(p, job)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int half = lane >> 5, col = lane & 31;
-    const RowOf row = row_of(p, job, wave, col);
+    char *const lds_k = kShared ? lds : lds + wave * 2 * S::kTileBytes, *const lds_v = lds_k + (kShared ? 2 : 1) * S::kTileBytes;
+    const RowOf row = row_of(p, job, kShared ? wave : 0, col);
     u32x4 qf[S::kChunks / 2];
     load_q<S::kChunks>(p, row, D, S::kSize, half, qf);
-    sign_q(p, qf);
-    const Mover<false, D, kWaves, PAGED> mover(p, job, wave, lane);
+    const Mover<false, D, WAVES, PAGED> mover(p, job, kShared ? wave : 0, lane);
     if (threadIdx.x == 0) sh_not_finite = 0;
-    __syncthreads();
+    auto ready = [&]() __attribute__((always_inline)) {  // (what was put is there to read)
+        if constexpr (kShared) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
 
     floatx16 o[S::kDTiles];
 #pragma unroll
@@ -443,17 +457,22 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptParams p) {
         mover.put_k(lds_k + buffer * S::kTileBytes, kr);
         mover.put_v(lds_v + buffer * S::kTileBytes, vr, (t + 1) * S::kKeys > job.all, &sh_not_finite);
     };
-    if (job.t_begin < job.t_end) {  // (uniform)
-        const auto spot = mover.find(job.t_begin);
+    const int first = job.t_begin + (kShared ? 0 : wave);
+    if (first < job.t_end) {  // (uniform in the waves that share a tile)
+        const auto spot = mover.find(first);
         mover.template load<false>(spot, kr);
         mover.template load<true>(spot, vr);
-        put(0, job.t_begin);
-        __syncthreads();
     }
-    for (int t = job.t_begin; t < job.t_end; ++t) {
-        const int buffer = (t - job.t_begin) & 1;
-        if (t + 1 < job.t_end) {
-            const auto spot = mover.find(t + 1);
+    sign_q(p, qf);
+    __syncthreads();  // (sh_not_finite)
+    if (first < job.t_end) {
+        put(0, first);
+        ready();
+    }
+    for (int t = first; t < job.t_end; t += kStride) {
+        const int buffer = kShared ? (t - first) & 1 : 0;
+        if (t + kStride < job.t_end) {
+            const auto spot = mover.find(t + kStride);
             mover.template load<false>(spot, kr);
             mover.template load<true>(spot, vr);
         }
@@ -497,10 +516,48 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptParams p) {
                                                                 0, 0, 0);
             }
         }
-        if (t + 1 < job.t_end) put(buffer ^ 1, t + 1);
-        __syncthreads();
+        if constexpr (!kShared) ready();  // (the tile has been read)
+        if (t + kStride < job.t_end) put(kShared ? buffer ^ 1 : 0, t + kStride);
+        ready();
     }
-    finish<false, D, kWaves, PAGED>(p, job, row, wave, half, col, o, m, sum_of_halves(l), sh_not_finite, lds);
+    l = sum_of_halves(l);
+    if constexpr (!kShared) {
+        constexpr int kPieces = S::kDTiles * 4;  // of a lane's accumulators
+        static_assert(kPieces * 1024 == S::kTileBytes, "a wave's accumulators fill its tile of K");
+        if (wave != 0) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                *reinterpret_cast<floatx4 *>(lds_k + i * 1024 + lane * 16) =
+                    floatx4{o[i / 4][i % 4 * 4], o[i / 4][i % 4 * 4 + 1], o[i / 4][i % 4 * 4 + 2], o[i / 4][i % 4 * 4 + 3]};
+            *reinterpret_cast<floatx2 *>(lds_v + lane * 8) = floatx2{m, l};
+        }
+        __syncthreads();
+        if (wave != 0) return;
+        floatx2 ml[4] = {{m, l}};
+        float most = m;
+#pragma unroll
+        for (int w = 1; w < 4; ++w) {
+            ml[w] = *reinterpret_cast<const floatx2 *>(lds_v + w * 2 * S::kTileBytes + lane * 8);
+            most = fmaxf(most, ml[w][0]);
+        }
+        l = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = ml[w][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w][0] - most);  // (a NaN of l or o stays one)
+            l = fmaf(ml[w][1], f, l);
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                if (w == 0) {
+                    for (int x = 0; x < 4; ++x) o[i / 4][i % 4 * 4 + x] *= f;
+                    continue;
+                }
+                const floatx4 other = *reinterpret_cast<const floatx4 *>(lds_k + w * 2 * S::kTileBytes + i * 1024 + lane * 16);
+                for (int x = 0; x < 4; ++x) o[i / 4][i % 4 * 4 + x] = fmaf(other[x], f, o[i / 4][i % 4 * 4 + x]);
+            }
+        }
+        m = most;
+    }
+    finish<false, D, WAVES, PAGED>(p, job, row, kShared ? wave : 0, half, col, o, m, l, sh_not_finite, lds);
 }
 
 // f(0), f(1) ... f(N-1), each with its number as a type.
@@ -772,20 +829,21 @@ struct Plan {
     size_t o_bytes, ws_bytes;
 };
 
-// How a call is run: the form (bf16: four waves, 128 packed rows, two work-groups on a compute unit; eight waves, 256 rows, one) and
-// the parts its keys are cut into, whichever this estimate of the time in microseconds makes least.  A work-group costs `over`
+// How a call is run: the form (bf16: four waves, 128 packed rows, two work-groups on a compute unit; eight waves, 256 rows, one; fp32:
+// 128 rows, or 32 whose tiles of keys four waves share out) and the parts its keys are cut into, whichever this estimate of the time in microseconds makes least.  A work-group costs `over`
 // tiles of keys beside those that it sees; `step` is what a tile of 64 keys takes of a compute unit at D = 128, `lone` what it takes
 // where no second work-group shares the unit.  The call takes the work of all groups over 256 units, or the longest group, and where
 // the groups are alike (many keys before the chunk) whole rounds of them, of which half is counted for several sequences, as those
-// are seldom of one length; parts cost a launch and their bytes.  The constants are fitted to 2,500 timings (1 to 64 prompts,
+// are seldom of one length; parts cost a launch and their bytes.  The constants are fitted to 3,200 timings (1 to 64 prompts,
 // chunks of 1 to 4,000 tokens behind 0 to 30,000, six head layouts, D 64 and 128, both forms, 1 to 16 parts): the form picked is on
 // the mean 1.4 % behind the best of its shape.  8 chunks of 512 behind up to 8,192 at 40/8 heads: 337 us with eight waves, 375 with four.
 // Eight waves at 28/4 heads of 128: 8 prompts of 2,048 take 282 us, with four 295; 64 of 128 take 55 us, with four 44.
+// fp32 at 8/2 heads of 64: 4 prompts of 200 tokens take 13 us with four waves on 32 rows, 21 with 128; 32 of them 42 us, and 30.
 // One chunk of 40 tokens behind 8,000: 30 us in 16 parts; 512 behind 16,000, twice: 249 us in 2 parts, 309 in 3.
 struct Cost {
     float step, lone, over, base;
 };
-constexpr Cost kFour{1.0f, 1.3f, 3.65f, 11.1f}, kEight{1.79f, 1.79f, 5.5f, 8.f}, kF32{8.4f, 8.4f, 0.7f, 7.f};
+constexpr Cost kFour{1.0f, 1.3f, 3.65f, 11.1f}, kEight{1.79f, 1.79f, 5.5f, 8.f}, kF32{7.5f, 10.6f, 0.25f, 7.9f}, kF32Keys{3.9f, 2.2f, 1.8f, 8.1f};
 
 float estimate(const Cost &c, int32_t B, int64_t groups, int splits, int rows, float mean_q, int32_t max_q, int32_t max_kv, int32_t D, bool bf16) {
     const float before = (float)std::max(0, max_kv - max_q), alike = before / max_kv * (B == 1 ? 1.f : 0.5f);
@@ -795,7 +853,7 @@ float estimate(const Cost &c, int32_t B, int64_t groups, int splits, int rows, f
     const float even = rounds * c.step * mean, whole = (up * c.step + odd) * mean;
     const float t = std::max(even + alike * (whole - even), longest * c.lone);
     const float parts = splits == 1 ? 0.f : 5.4f + groups * splits * (float)rows * D * 8 / 3.6e6f;
-    return c.base + (D == 128 ? 1.f : bf16 ? 0.6f : 0.53f) * t + parts;
+    return c.base + (D == 128 ? 1.f : bf16 ? 0.6f : 0.52f) * t + parts;
 }
 
 bool make_plan(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t Hq, int32_t Hkv, int32_t D, respec_dtype_t dt, Plan &pl) {
@@ -808,12 +866,13 @@ bool make_plan(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_
     const long waves = kn.get(&Knobs::prompt_waves, 0), splits = kn.get(&Knobs::prompt_splits, 0);
     const float mean_q = std::min((float)max_q, (float)total_q / B);
     float least = INFINITY;
-    for (const int w : {8, 4}) {
-        if (dt == RESPEC_F32 ? w != 4 : (waves == 4 || waves == 8) && w != waves) continue;
+    for (const int w : {8, 4, 1}) {
+        const bool fits = dt == RESPEC_F32 ? w != 8 : w != 1, forced = dt == RESPEC_F32 ? waves == 1 || waves == 4 : waves == 4 || waves == 8;
+        if (!fits || (forced && w != waves)) continue;
         const int64_t tiles = tiles_bound(B, total_q, max_q, G, w * 32), groups = tiles * Hkv;
         for (const int s : {1, 2, 3, 4, 6, 8, 12, kMaxSplits}) {
             if (s > 1 && (s > max_kv / 64 || groups * s > kSplitGroups)) break;
-            const float t = estimate(dt == RESPEC_F32 ? kF32 : w == 8 ? kEight : kFour, B, groups, s, w * 32, mean_q, max_q, max_kv, D, dt == RESPEC_BF16);
+            const float t = estimate(dt == RESPEC_F32 ? (w == 4 ? kF32 : kF32Keys) : w == 8 ? kEight : kFour, B, groups, s, w * 32, mean_q, max_q, max_kv, D, dt == RESPEC_BF16);
             if (!(t < least)) continue;
             least = t;
             pl.waves = w;
@@ -835,13 +894,13 @@ hipError_t launch(PromptParams &p, const Plan &pl, hipStream_t stream) {
     using S = Shape<BF16, D, WAVES>;
     void (*kernel)(PromptParams);
     if constexpr (BF16) kernel = &prompt_bf16_kernel<D, WAVES, PAGED>;
-    else kernel = &prompt_f32_kernel<D, PAGED>;
-    const size_t lds = BF16 ? S::kLdsBytes : 4 * S::kTileBytes;
+    else kernel = &prompt_f32_kernel<D, WAVES, PAGED>;
+    const size_t lds = BF16 ? S::kLdsBytes : (WAVES == 1 ? 8 : 4) * S::kTileBytes;
     if (lds > 65536) {
         const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (err != hipSuccess) return err;
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(pl.tiles * p.Hkv * p.splits)), dim3(S::kThreads), lds, stream, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(pl.tiles * p.Hkv * p.splits)), dim3(BF16 ? S::kThreads : 256), lds, stream, p);
     if (p.splits > 1) {
         constexpr int kBlocks = S::kRows / (256 / (D / 4));
         hipLaunchKernelGGL((prompt_join_kernel<BF16, D, S::kRows, PAGED>), dim3((unsigned)(pl.tiles * p.Hkv * kBlocks)), dim3(256), 0, stream, p);
@@ -851,6 +910,7 @@ hipError_t launch(PromptParams &p, const Plan &pl, hipStream_t stream) {
 
 template <bool PAGED>
 hipError_t launch_any(PromptParams &p, const Plan &pl, int32_t D, respec_dtype_t dt, hipStream_t stream) {
+    if (dt == RESPEC_F32 && pl.waves == 1) return D == 128 ? launch<false, 128, 1, PAGED>(p, pl, stream) : launch<false, 64, 1, PAGED>(p, pl, stream);
     if (dt == RESPEC_F32) return D == 128 ? launch<false, 128, 4, PAGED>(p, pl, stream) : launch<false, 64, 4, PAGED>(p, pl, stream);
     if (pl.waves == 8) return D == 128 ? launch<true, 128, 8, PAGED>(p, pl, stream) : launch<true, 64, 8, PAGED>(p, pl, stream);
     return D == 128 ? launch<true, 128, 4, PAGED>(p, pl, stream) : launch<true, 64, 4, PAGED>(p, pl, stream);

@@ -105,7 +105,8 @@ def test_few_rows_split_the_keys(dtype, R, L, heads):
 
 @pytest.mark.parametrize("splits", [1, 2, 3, 16])
 @pytest.mark.parametrize("dtype,waves,heads", [("bf16", 4, (28, 4, 128)), ("bf16", 8, (28, 4, 128)), ("bf16", 4, (3, 1, 64)),
-                                               ("bf16", 8, (6, 2, 64)), ("f32", 4, (6, 2, 128)), ("f32", 4, (5, 1, 64))], ids=str)
+                                               ("bf16", 8, (6, 2, 64)), ("f32", 4, (6, 2, 128)), ("f32", 4, (5, 1, 64)),
+                                               ("f32", 1, (6, 2, 128)), ("f32", 1, (5, 1, 64))], ids=str)
 def test_every_form_and_number_of_parts(dtype, waves, heads, splits):
     """What the rule would choose by size, forced: parts without a key, tiles that end inside a sequence, more sequences than lanes."""
     Hq, Hkv, D = heads
