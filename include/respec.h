@@ -276,7 +276,7 @@ respec_status_t respec_commit_accepted_paged(void *k_pages, void *v_pages, const
  *   out       [total_q, Hq, D]    dt, contiguous (written)
  *   lse       [total_q, Hq] f32 or NULL (written), as in respec_verify_attention
  *   max_q_per_seq, max_kv_len   host-side upper bounds of R_b and L_b; rows or keys beyond them are
- *             not processed
+ *             not processed (max_kv_len at most 2^31 - 257).  How the work is cut follows them: close ones are faster
  *   D in {64, 128}; Hq % Hkv == 0; strides multiples of 16 bytes; data pointers 16-byte aligned.
  *   workspace respec_prompt_attention_workspace_bytes(...) bytes, 256-byte aligned, scratch (nothing
  *             to prepare, nothing survives): calls that overlap need one each, captured ones too.

@@ -14,6 +14,7 @@
 //
 // All sums are fp32 within a thread (some hundred terms), and in a fixed order across threads.
 #include "respec_common.hpp"
+#include "respec_tiles.hpp"
 
 #include <algorithm>
 #include <cmath>
@@ -715,6 +716,7 @@ respec_status_t respec_token_logprobs(const void *logits, const int32_t *tokens,
     if (!logits || !tokens || !out_logprob || !out_lse) return fail(RESPEC_ERR_INVALID_ARG, "token_logprobs: null pointer argument");
     const respec_status_t st = check_rows("token_logprobs", rows, V, ld, temperature, row_temperature != nullptr, logits_dt, logits);
     if (st != RESPEC_OK) return st;
+    if (!grid_fits(rows, kThreads)) return fail(RESPEC_ERR_UNSUPPORTED, "token_logprobs: too many rows (%d)", rows);
     if (top_n < 0) return fail(RESPEC_ERR_INVALID_ARG, "token_logprobs: top_n must not be negative (%d)", top_n);
     if (top_n > kMaxTop) return fail(RESPEC_ERR_UNSUPPORTED, "token_logprobs: at most %d alternatives (%d)", kMaxTop, top_n);
     if (top_n > 0 && (!out_top_tokens || !out_top_logprobs))
@@ -780,7 +782,7 @@ respec_status_t respec_token_logprobs_grad(const void *logits, const int32_t *to
     const bool pieces = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(grad_logits)) & 15) == 0 && (ld - ld_g) * esz % 16 == 0;
     const int64_t per_block = (int64_t)kThreads * kUnroll * (bf16 ? 8 : 4);
     const int64_t blocks = (V + (pieces ? 16 / esz - 1 : 0) + per_block - 1) / per_block;
-    if (blocks * rows > 0x7fffffff) return fail(RESPEC_ERR_UNSUPPORTED, "token_logprobs_grad: too many rows");
+    if (!grid_fits(blocks * rows, kThreads)) return fail(RESPEC_ERR_UNSUPPORTED, "token_logprobs_grad: too many rows");
     p.blocks_per_row = (int32_t)blocks;
     const dim3 grid((unsigned)(blocks * rows));
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);

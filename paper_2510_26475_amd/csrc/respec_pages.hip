@@ -178,7 +178,7 @@ __global__ __launch_bounds__(kThreads) void resize_apply_kernel(ResizeParams p) 
     bool ok = (word & kRefusedBit) == 0;
     if (ok && need > 0) {  // (uniform)
         const int n_free = block_sum_of<kThreads>(p.block_free, p.blocks, lds);
-        ok = p.begin[b] + need <= n_free;
+        ok = p.begin[b] >= 0 && (int64_t)p.begin[b] + need <= n_free;  // (parts of page_table that overlap can ask for more than 2^31)
     }
     const Seq q = seq_of(s, b);
     const int len = s.kv_len[b];
@@ -197,11 +197,12 @@ __global__ __launch_bounds__(kThreads) void resize_apply_kernel(ResizeParams p) 
     }
     for (int e = q.count + threadIdx.x; e < pages; e += kThreads) {
         const int32_t id = fresh[split + e - q.count];
+        if (!is_page(s, id)) continue;  // (never, with tables as the header has them)
         s.page_table[q.e0 + e] = id;
         s.page_refs[id] = 1;
     }
     if (threadIdx.x == 0) {
-        if (split) {
+        if (split && is_page(s, fresh[0])) {
             int32_t *entry = &s.page_table[q.e0 + (len >> s.page_shift)];
             atomicSub(&s.page_refs[*entry], 1);
             p.copy_src[b] = *entry;
@@ -428,6 +429,7 @@ respec_status_t check_state(const char *name, const void *a, const void *b, cons
     if (!a || !b || !c || !d || !e) return fail(RESPEC_ERR_INVALID_ARG, "%s: null pointer argument", name);
     if (B <= 0 || table_len <= 0 || num_pages <= 0)
         return fail(RESPEC_ERR_INVALID_ARG, "%s: sizes must be positive (B=%d page_table_len=%d num_pages=%d)", name, B, table_len, num_pages);
+    if (!grid_fits(B, kThreads)) return fail(RESPEC_ERR_UNSUPPORTED, "%s: too many sequences (%d)", name, B);
     return RESPEC_OK;
 }
 
@@ -615,7 +617,7 @@ respec_status_t respec_append_paged(const void *k_new, const void *v_new, void *
     p.page_shift = shift;
     p.token_bytes = (int32_t)token;
     const int64_t grid = tiles_bound(B, total_q, max_q_per_seq, 1, kAppendRows);
-    if (grid > 0x7fffffff) return fail(RESPEC_ERR_UNSUPPORTED, "append_paged: too many rows");
+    if (!grid_fits(grid, kThreads)) return fail(RESPEC_ERR_UNSUPPORTED, "append_paged: too many rows");
     hipLaunchKernelGGL(append_kernel, dim3((unsigned)grid), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), p);
     return launched("append_paged");
 }

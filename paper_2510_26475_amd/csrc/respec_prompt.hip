@@ -926,6 +926,7 @@ respec_status_t run(const char *name, PromptParams &p, const void *k, const void
     if (p.Hq % p.Hkv != 0) return fail(RESPEC_ERR_INVALID_ARG, "%s: Hq=%d is not a multiple of Hkv=%d", name, p.Hq, p.Hkv);
     if (!std::isfinite(sm_scale)) return fail(RESPEC_ERR_INVALID_ARG, "%s: sm_scale must be finite", name);
     if (D != 64 && D != 128) return fail(RESPEC_ERR_UNSUPPORTED, "%s: head size %d is neither 64 nor 128", name, D);
+    if (p.max_kv > INT32_MAX - 256) return fail(RESPEC_ERR_UNSUPPORTED, "%s: max_kv_len must lie 256 below 2^31 - 1 or more", name);
     const int64_t esz = dt == RESPEC_BF16 ? 2 : 4;
     if (p.ld_q < (int64_t)p.Hq * D || p.ld_k < (int64_t)p.Hkv * D || p.ld_v < (int64_t)p.Hkv * D)
         return fail(RESPEC_ERR_INVALID_ARG, "%s: a token stride is smaller than a token", name);
@@ -937,7 +938,7 @@ respec_status_t run(const char *name, PromptParams &p, const void *k, const void
         return fail(RESPEC_ERR_INVALID_ARG, "%s: data pointers must be 16-byte aligned", name);
     Plan pl;
     p.max_q = std::min(p.max_q, p.total_q);
-    if (!make_plan(p.B, p.total_q, p.max_q, p.max_kv, p.Hq, p.Hkv, D, dt, pl) || pl.tiles * p.Hkv * pl.splits > (1 << 26))
+    if (!make_plan(p.B, p.total_q, p.max_q, p.max_kv, p.Hq, p.Hkv, D, dt, pl) || !grid_fits(pl.tiles * p.Hkv * pl.splits, pl.waves == 8 ? 512 : 256))
         return fail(RESPEC_ERR_UNSUPPORTED, "%s: too many rows", name);
     if (!workspace || workspace_bytes < pl.ws_bytes || !aligned_to(workspace, 256))
         return fail(RESPEC_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) needed, got %zu", name, pl.ws_bytes,

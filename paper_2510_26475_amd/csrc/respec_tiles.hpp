@@ -60,4 +60,7 @@ inline int64_t tiles_bound(int32_t B, int32_t total_q, int32_t max_q, int32_t G,
     return std::max<int64_t>(1, std::min(by_rows, by_seqs));
 }
 
+// Whether a grid of `blocks` work-groups can be launched: its threads are counted in 32 bits.
+inline bool grid_fits(int64_t blocks, int threads) { return blocks <= 0xffffffffLL / threads; }
+
 }  // namespace respec

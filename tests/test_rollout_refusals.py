@@ -55,6 +55,10 @@ BAD = [
     ("respec_prompt_attention", dict(workspace=ctypes.c_void_p(0x100010)), WORKSPACE),
     ("respec_prompt_attention", dict(workspace_bytes=10), WORKSPACE), ("respec_prompt_attention", dict(workspace=None), WORKSPACE),
     ("respec_prompt_attention", dict(total_q=1 << 30, max_q=1 << 30, B=1, max_kv=1 << 30), UNSUPPORTED),
+    ("respec_prompt_attention", dict(total_q=1 << 24, max_q=1, B=1 << 24, max_kv=1), UNSUPPORTED),
+    ("respec_prompt_attention", dict(max_kv=2 ** 31 - 200), UNSUPPORTED),
+    ("respec_append_paged", dict(B=1 << 24, total_q=1 << 24, max_q=1), UNSUPPORTED), ("respec_pages_fork", dict(B=1 << 24), UNSUPPORTED),
+    ("respec_token_logprobs", dict(rows=1 << 24), UNSUPPORTED), ("respec_token_logprobs_grad", dict(rows=1 << 24), UNSUPPORTED),
     ("respec_prompt_attention_paged", dict(page_size=24), UNSUPPORTED), ("respec_prompt_attention_paged", dict(page_size=8), UNSUPPORTED),
     ("respec_prompt_attention_paged", dict(num_pages=0), INVALID), ("respec_prompt_attention_paged", dict(page_table_len=0), INVALID),
     ("respec_prompt_attention_paged", dict(workspace_bytes=0), WORKSPACE), ("respec_prompt_attention_paged", dict(ld_q=1028), UNSUPPORTED),
