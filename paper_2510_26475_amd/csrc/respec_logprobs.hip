@@ -257,6 +257,21 @@ struct Deal {
     }
 };
 
+// The largest value (in bits from the top down to `last`) that `top` or more of what `reached` counts reach, or a smaller one that exactly
+// `top` reach; 0 if there are fewer.  Two bits at a time, as the three counts need not wait for one another.
+template <typename F>
+__device__ inline uint32_t reached_by(int top, int last, F &&reached) {
+    uint32_t least = 0;
+    for (int bit = 30; bit >= last; bit -= 2) {
+        const uint32_t c1 = least | 1u << bit, c2 = least | 2u << bit, c3 = least | 3u << bit;
+        const int n1 = reached(c1), n2 = reached(c2), n3 = reached(c3);
+        if (n1 < top) continue;
+        least = n3 >= top ? c3 : n2 >= top ? c2 : c1;
+        if ((n3 >= top ? n3 : n2 >= top ? n2 : n1) == top) break;
+    }
+    return least;
+}
+
 // The best keys among a wave's groups: the `top` groups with the largest maxima hold them (of groups with equal maxima the first
 // ones), so only those, or a few more, are read again.  Leaves them, unsorted and with a few more, in `cand`; returns their number.
 template <bool BF16>
@@ -269,15 +284,10 @@ __device__ inline int best_of_groups(const Row<BF16> &r, const Deal &deal, int w
     for (int j = 0; j < kGroups / 64; ++j) x[j] = j * 64 + lane < n ? order_of(maxima[j * 64 + lane]) : 0u;
     // A value that `top` lanes' own maxima reach: bit by bit, by the upper half alone for bf16, which is all there is to its order.
     constexpr int kLast = BF16 ? 16 : 0;
-    uint32_t mine = 0, least = 0;
+    uint32_t mine = 0;
 #pragma unroll
     for (int j = 0; j < kGroups / 64; ++j) mine = max(mine, x[j]);
-    for (int bit = 31; bit >= kLast; --bit) {
-        const int c = (int)__popcll(__ballot(mine >= (least | 1u << bit)));
-        if (c < top) continue;
-        least |= 1u << bit;
-        if (c == top) break;
-    }
+    uint32_t least = reached_by(top, kLast, [&](uint32_t from) __attribute__((always_inline)) { return (int)__popcll(__ballot(mine >= from)); });
     auto count = [&](uint32_t from) __attribute__((always_inline)) {
         int c = 0;
 #pragma unroll
@@ -288,17 +298,8 @@ __device__ inline int best_of_groups(const Row<BF16> &r, const Deal &deal, int w
     least = max(least, 1u);
     int ties = INT32_MAX, sel = 0;
     if (count(least) > kChosen) {  // Too many groups reach it: the top-th largest maximum of all.
-        int found = 0;
-        least = 0;
-        for (int bit = 31; bit >= kLast; --bit) {
-            const int c = count(least | 1u << bit);
-            if (c < top) continue;
-            least |= 1u << bit;
-            found = c;
-            if (c == top) break;
-        }
-        least = max(least, 1u);
-        if (found != top) ties = top - count(least + (1u << kLast));
+        least = max(reached_by(top, kLast, count), 1u);
+        if (count(least) != top) ties = top - count(least + (1u << kLast));
     }
 #pragma unroll
     for (int j = 0; j < kGroups / 64; ++j)
@@ -316,7 +317,8 @@ __device__ inline int best_of_groups(const Row<BF16> &r, const Deal &deal, int w
     int kept = held;
     for (int q0 = 0; q0 < pieces; q0 += 64) {
         const int q = q0 + lane;
-        const int i = q < pieces ? deal.piece(chosen[q / run], wave, q % run) : deal.end;
+        const int group = run == 1 ? q : q / run;
+        const int i = q < pieces ? deal.piece(chosen[group], wave, q - group * run) : deal.end;
         u32x4 raw{};
         if (i < deal.end) raw = *r.at(i);
         float v[E::kPer];
@@ -340,7 +342,8 @@ __device__ inline int best_of_groups(const Row<BF16> &r, const Deal &deal, int w
     for (int i = 0; i < held; ++i) best.insert(cand[i], top);
     for (int q0 = 0; q0 < pieces; q0 += 64) {
         const int q = q0 + lane;
-        const int i = q < pieces ? deal.piece(chosen[q / run], wave, q % run) : deal.end;
+        const int group = run == 1 ? q : q / run;
+        const int i = q < pieces ? deal.piece(chosen[group], wave, q - group * run) : deal.end;
         u32x4 raw{};
         if (i < deal.end) raw = *r.at(i);
         float v[E::kPer];
@@ -512,6 +515,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobParams p) {
         for (int c = threadIdx.x; c < n; c += kThreads) {
             const uint64_t mine = left[c];
             int rank = 0;
+#pragma unroll 8
             for (int i = 0; i < n; ++i) rank += left[i] > mine;
             if (rank < p.top) {
                 if (p.parts == 1) write_top(p, row, rank, mine, a, inv_t);
@@ -533,6 +537,15 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobParams p)
     __shared__ int sh_kept;
     __shared__ Sums sh_sums;
     const int row = blockIdx.x, lane = threadIdx.x & 63, top = p.top;
+    // (asked for before the token is known: a row without one leaves what is read unused)
+    const int64_t slot = (int64_t)row * p.parts;
+    const int all = p.parts * top;
+    constexpr int kAhead = 8;
+    uint64_t early[kAhead] = {};
+    if (top > 0)
+        for (int j = 0; j < kAhead; ++j) early[j] = p.part_top[slot * top + max(0, min((int)threadIdx.x + j * kThreads, all - 1))];
+    Sums a{-INFINITY, 0.f, 0.f};
+    if (threadIdx.x < 64 && lane < p.parts) a = {p.part_sums[(slot + lane) * 4], p.part_sums[(slot + lane) * 4 + 1], p.part_sums[(slot + lane) * 4 + 2]};
     const int32_t token = p.tokens[row];
     if ((uint32_t)token >= (uint32_t)p.V) {
         write_unused(p, row);
@@ -540,13 +553,11 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobParams p)
     }
     float inv_t;
     const float scale = row_scale_of<BF16>(p, row, inv_t);
-    const int64_t slot = (int64_t)row * p.parts;
-    const int all = p.parts * top;
-    for (int i = threadIdx.x; i < all; i += kThreads) keys[i] = p.part_top[slot * top + i];
+    for (int j = 0; j < kAhead; ++j)
+        if ((int)threadIdx.x + j * kThreads < all) keys[threadIdx.x + j * kThreads] = early[j];
+    for (int i = threadIdx.x + kAhead * kThreads; i < all; i += kThreads) keys[i] = p.part_top[slot * top + i];
     if (threadIdx.x < 64) {
         const float token_logit = load_one<BF16>(static_cast<const char *>(p.logits) + (int64_t)row * p.ld * Elem<BF16>::kSize, token);
-        Sums a{-INFINITY, 0.f, 0.f};
-        if (lane < p.parts) a = {p.part_sums[(slot + lane) * 4], p.part_sums[(slot + lane) * 4 + 1], p.part_sums[(slot + lane) * 4 + 2]};
         a = join_wave(a, scale);
         if (lane == 0) {
             write_row(p, row, a, token_logit, inv_t);
@@ -564,14 +575,9 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobParams p)
         const int q = j * 64 + lane;
         x[j] = q < firsts ? (uint32_t)(keys[q / deep * top + q % deep] >> 32) : 0;
     }
-    uint32_t least = 0;
-    for (int bit = 31; bit >= (BF16 ? 16 : 0); --bit) {
-        const uint32_t c = least | 1u << bit;
-        const int n = (int)__popcll(__ballot(x[0] >= c)) + (int)__popcll(__ballot(x[1] >= c));
-        if (n < top) continue;
-        least = c;
-        if (n == top) break;
-    }
+    const uint32_t least = reached_by(top, BF16 ? 16 : 0, [&](uint32_t from) __attribute__((always_inline)) {
+        return (int)__popcll(__ballot(x[0] >= from)) + (int)__popcll(__ballot(x[1] >= from));
+    });
     for (int i = threadIdx.x; i < all; i += kThreads)
         if (keys[i] != 0 && (uint32_t)(keys[i] >> 32) >= least) {
             const int to = atomicAdd(&sh_kept, 1);  // (any order: the ranks are the keys')
@@ -579,11 +585,12 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobParams p)
         }
     __syncthreads();
     const int kept = sh_kept;
-    const Sums a = sh_sums;
+    a = sh_sums;
     if (kept <= kJoin) {
         for (int c = threadIdx.x; c < kept; c += kThreads) {
             const uint64_t mine = cand[c];
             int rank = 0;
+#pragma unroll 8
             for (int i = 0; i < kept; ++i) rank += cand[i] > mine;
             if (rank < top) write_top(p, row, rank, mine, a, inv_t);
         }
