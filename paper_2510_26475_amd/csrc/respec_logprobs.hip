@@ -46,6 +46,7 @@ struct LogprobParams {
     int32_t *top_tokens;
     float *top_logprobs;
     int32_t rows, V, top, parts;
+    int32_t deep, deep_mul;  // entries of every part's list that the join looks at first; q / deep = q deep_mul / 2^16 for q < 256
     int64_t ld;
     float temperature;
     float *part_sums;    // [rows * parts][4]: reference, s, t
@@ -568,16 +569,22 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobParams p)
     if (top == 0) return;
     __syncthreads();
     uint64_t *cand = keys + all;
-    // the top-th best of the first `deep` entries of every list (at most 64 + 63 keys), by every wave
-    const int deep = (top + p.parts - 1) / p.parts, firsts = deep * p.parts;
-    uint32_t x[2];
-    for (int j = 0; j < 2; ++j) {
-        const int q = j * 64 + lane;
-        x[j] = q < firsts ? (uint32_t)(keys[q / deep * top + q % deep] >> 32) : 0;
-    }
-    const uint32_t least = reached_by(top, BF16 ? 16 : 0, [&](uint32_t from) __attribute__((always_inline)) {
-        return (int)__popcll(__ballot(x[0] >= from)) + (int)__popcll(__ballot(x[1] >= from));
-    });
+    // the top-th best of the first `deep` entries of every list, by every wave: of 3 top keys, close to the top-th of all
+    // (64 rows with 32 alternatives: 22 us, by a list's first entries alone 34)
+    constexpr int kFirsts = 4;
+    const int firsts = p.deep * p.parts;
+    static_assert(3 * kMaxTop + kMaxParts <= 64 * kFirsts, "a register each");
+    uint32_t x[kFirsts] = {};
+#pragma unroll
+    for (int j = 0; j < kFirsts; ++j)
+        if (j * 64 < firsts) {  // (uniform)
+            const int q = j * 64 + lane, list = (int)((uint32_t)(q * p.deep_mul) >> 16);
+            if (q < firsts) x[j] = (uint32_t)(keys[list * top + q - list * p.deep] >> 32);
+        }
+    const auto reach = [&](int j, uint32_t from) __attribute__((always_inline)) { return (int)__popcll(__ballot(x[j] >= from)); };
+    uint32_t least;
+    if (firsts <= 64) least = reached_by(top, BF16 ? 16 : 0, [&](uint32_t from) __attribute__((always_inline)) { return reach(0, from); });
+    else least = reached_by(top, BF16 ? 16 : 0, [&](uint32_t from) __attribute__((always_inline)) { return reach(0, from) + reach(1, from) + reach(2, from) + reach(3, from); });
     for (int i = threadIdx.x; i < all; i += kThreads)
         if (keys[i] != 0 && (uint32_t)(keys[i] >> 32) >= least) {
             const int to = atomicAdd(&sh_kept, 1);  // (any order: the ranks are the keys')
@@ -676,10 +683,12 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradParams p) {
 }
 
 // ------------------------------------------------------------------------------------------ host side
-// Parts of a row: work-groups to fill the device, no part below 256 pieces, and no more parts than a wave has lanes.
-int parts_of(int32_t rows, int32_t V, bool bf16) {
+// Parts of a row: work-groups to fill the device, no part below 256 pieces, and no more parts than a wave has lanes.  Where many alternatives are
+// asked for, a wave's part holds three times as many groups, or most of them would be read again (8 rows of 151,936 bf16 logits with
+// 64 alternatives take 26 us, in parts of 256 pieces 49).
+int parts_of(int32_t rows, int32_t V, int32_t top, bool bf16) {
     const int64_t pieces = V / (bf16 ? 8 : 4);
-    const int64_t most = std::min<int64_t>(std::min<int64_t>(kMaxParts, kFill / rows), pieces / kThreads);
+    const int64_t most = std::min<int64_t>(std::min<int64_t>(kMaxParts, kFill / rows), pieces / std::max(kThreads, 12 * top));
     return (int)std::max<int64_t>(1, most);
 }
 
@@ -746,7 +755,9 @@ respec_status_t respec_token_logprobs(const void *logits, const int32_t *tokens,
     p.top = top_n;
     p.ld = ld;
     p.temperature = temperature;
-    p.parts = parts_of(rows, V, logits_dt == RESPEC_BF16);
+    p.parts = parts_of(rows, V, top_n, logits_dt == RESPEC_BF16);
+    p.deep = std::max(1, std::min(top_n, (3 * top_n + p.parts - 1) / p.parts));
+    p.deep_mul = 65536 / p.deep + 1;
     p.part_sums = static_cast<float *>(workspace);
     p.part_top = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + sums_bytes());
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
