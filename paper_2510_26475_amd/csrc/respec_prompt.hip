@@ -154,19 +154,26 @@ __device__ inline bool find_longest(const PromptParams &p, int number, Tile &out
     };
     auto all = [&](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(wave_scan_add(reach(x)), 63); };
     if (number >= all(0)) return false;
-    int x = 0, over = p.max_kv / 64 + 1;  // all(x) > number >= all(over)
+    int x = 0, over = p.max_kv / 64 + 1, n_over = 0;  // all(x) > number >= all(over)
     while (p.B > 1 && over - x > 1) {
-        const int mid = (x + over) / 2;
-        if (all(mid) > number) x = mid;
-        else over = mid;
+        const int at = (x + over) / 2, n_at = all(at);
+        if (n_at > number) x = at;
+        else over = at, n_over = n_at;
     }
     const int more = p.B == 1 ? 0 : reach(over), mine = p.B == 1 ? tiles : reach(x) - more;  // (one sequence: its tiles from the last)
-    const int rest = number - __builtin_amdgcn_readlane(wave_scan_add(more), 63);
-    const int sum = wave_scan_add(mine);
-    const int at = (int)__builtin_ctzll(__ballot(sum > rest));
+    // Among the tiles of a step one of every sequence in turn: an XCD, which is given every eighth work-group, then meets fewer sequences' keys
+    // at a time than with one sequence after the other (16 prompts of 1,024 tokens at 28/4 heads take 166 us, and 174).
+    int rest = number - (p.B == 1 ? 0 : n_over), turn = 0;
+    uint64_t left = __ballot(mine > 0);
+    if (p.B == 1) turn = rest, rest = 0;
+    for (int n = (int)__popcll(left); rest >= n; n = (int)__popcll(left)) {
+        rest -= n;
+        left = __ballot(mine > ++turn);
+    }
+    const int at = (int)__builtin_ctzll(__ballot((left >> lane & 1) != 0 && (int)__popcll(left & ((1ull << lane) - 1)) == rest));
     out.b = at;
     out.tiles = __builtin_amdgcn_readlane(tiles, at);
-    out.index = __builtin_amdgcn_readlane(tiles - more, at) - 1 - (rest - __builtin_amdgcn_readlane(sum - mine, at));
+    out.index = __builtin_amdgcn_readlane(tiles - more, at) - 1 - turn;
     out.R = __builtin_amdgcn_readlane(R, at);
     out.q0 = __builtin_amdgcn_readlane(q0, at);
     tokens = __builtin_amdgcn_readlane(L, at);
