@@ -23,6 +23,7 @@ constexpr int kPagesPerBlock = 4 * kRankThreads;  // page_refs that a work-group
 // Up to here a work-group counts the pages before its own for itself (compaction of 16,384 pages 10.0 us with its enqueuing, of
 // 16,385 in a launch more 11.9; at 32,768 the counting would take 14 us, the launch 5).
 constexpr int kFewPages = 4 * kPagesPerBlock;
+constexpr int kFewSequences = 32;             // up to here, and up to kPagesPerBlock pages, a resize is one launch
 constexpr int32_t kKeep = INT32_MIN;          // a page that compaction neither moves nor fills
 
 struct PageState {
@@ -97,6 +98,72 @@ struct ResizeParams {
 };
 constexpr int32_t kSplitBit = 1 << 30, kRefusedBit = INT32_MIN, kNeedMask = kSplitBit - 1;
 
+// What sequence b needs, by the state before the call, as a word of `need`; `take`: the pages that it is counted for.
+__device__ inline int plan_of(const ResizeParams &p, int b, int &take) {
+    const PageState &s = p.s;
+    take = 0;
+    if (p.want[b] < 0) return 0;
+    const Seq q = seq_of(s, b);
+    const int64_t pages = ((int64_t)p.want[b] + ((1 << s.page_shift) - 1)) >> s.page_shift;
+    const int len = max(0, s.kv_len[b]), at = len >> s.page_shift;
+    bool split = false;
+    if (p.want[b] > len && (len & ((1 << s.page_shift) - 1)) != 0 && at < q.count) {
+        const int32_t id = s.page_table[q.e0 + at];
+        split = is_page(s, id) && s.page_refs[id] > 1;
+    }
+    const int64_t need = max((int64_t)0, pages - q.count) + split;
+    const int word = (int)min(need, (int64_t)kNeedMask) | (split ? kSplitBit : 0);
+    if (pages > q.cap) return word | kRefusedBit;
+    take = (int)need;
+    return word;
+}
+// (parts of page_table that overlap can ask for more than 2^31)
+__device__ inline bool is_served(int word, int begin, int n_free) {
+    const int need = word & kNeedMask;
+    return (word & kRefusedBit) == 0 && (need == 0 || (begin >= 0 && (int64_t)begin + need <= n_free));
+}
+
+// Carries out the plan of sequence b, by the threads of a work-group or of a wave (`all_read`: everybody has read what one writes).  A page named by
+// several sequences that let go of it in one call is counted down by each; a page handed out was free before the call, so no
+// other sequence of the call names it.
+template <int THREADS, typename F>
+__device__ inline void resize_one(const ResizeParams &p, int b, int word, bool ok, const int32_t *fresh, int me, F &&all_read) {
+    const PageState &s = p.s;
+    const int want = p.want[b];
+    const bool split = (word & kSplitBit) != 0;
+    const Seq q = seq_of(s, b);
+    const int len = s.kv_len[b];
+    all_read();
+    if (me == 0) {
+        p.missing[b] = want >= 0 && !ok ? word & kNeedMask : 0;
+        p.copy_src[b] = p.copy_dst[b] = -1;
+    }
+    if (want < 0 || !ok) return;
+    const int pages = (int)(((int64_t)want + ((1 << s.page_shift) - 1)) >> s.page_shift);
+    for (int e = pages + me; e < q.count; e += THREADS) {
+        const int32_t id = s.page_table[q.e0 + e];
+        if (is_page(s, id)) atomicSub(&s.page_refs[id], 1);
+        s.page_table[q.e0 + e] = -1;
+    }
+    for (int e = q.count + me; e < pages; e += THREADS) {
+        const int32_t id = fresh[split + e - q.count];
+        if (!is_page(s, id)) continue;  // (never, with tables as the header has them)
+        s.page_table[q.e0 + e] = id;
+        s.page_refs[id] = 1;
+    }
+    if (me == 0) {
+        if (split && is_page(s, fresh[0])) {
+            int32_t *entry = &s.page_table[q.e0 + (len >> s.page_shift)];
+            atomicSub(&s.page_refs[*entry], 1);
+            p.copy_src[b] = *entry;
+            p.copy_dst[b] = *entry = fresh[0];
+            s.page_refs[fresh[0]] = 1;
+        }
+        s.page_count[b] = pages;
+        s.kv_len[b] = min(len, want);
+    }
+}
+
 // The last work-group: what every sequence needs, by the state before the call.  The others: how many pages of a block are free,
 // and (RANK) which these are in the order of all.
 template <bool RANK>
@@ -122,21 +189,8 @@ __global__ __launch_bounds__(kRankThreads) void resize_plan_kernel(ResizeParams 
     int base = 0;
     for (int b0 = 0; b0 < s.B; b0 += kRankThreads) {
         const int b = b0 + threadIdx.x;
-        int word = 0, take = 0;
-        if (b < s.B && p.want[b] >= 0) {
-            const Seq q = seq_of(s, b);
-            const int64_t pages = ((int64_t)p.want[b] + ((1 << s.page_shift) - 1)) >> s.page_shift;
-            const int len = max(0, s.kv_len[b]), at = len >> s.page_shift;
-            bool split = false;
-            if (p.want[b] > len && (len & ((1 << s.page_shift) - 1)) != 0 && at < q.count) {
-                const int32_t id = s.page_table[q.e0 + at];
-                split = is_page(s, id) && s.page_refs[id] > 1;
-            }
-            const int64_t need = max((int64_t)0, pages - q.count) + split;
-            word = (int)min(need, (int64_t)kNeedMask) | (split ? kSplitBit : 0);
-            if (pages > q.cap) word |= kRefusedBit;
-            else take = (int)need;
-        }
+        int take = 0;
+        const int word = b < s.B ? plan_of(p, b, take) : 0;
         const int to = block_scan<kRankThreads>(take, total, lds);
         if (b < s.B) {
             p.begin[b] = base + to - take;
@@ -166,51 +220,41 @@ __global__ __launch_bounds__(kRankThreads) void resize_rank_kernel(ResizeParams 
         if (is_free[i]) p.fresh[rank++] = blockIdx.x * kPagesPerBlock + threadIdx.x * 4 + i;
 }
 
-// One work-group per sequence.  A page named by several sequences that let go of it in one call is counted down by each; a page
-// handed out was free before the call, so no other sequence of the call names it.
+// One work-group per sequence.
 __global__ __launch_bounds__(kThreads) void resize_apply_kernel(ResizeParams p) {
     __shared__ int lds[kThreads / 64];
+    const int b = blockIdx.x, word = p.need[b], begin = p.begin[b];
+    const int n_free = (word & kNeedMask) > 0 ? block_sum_of<kThreads>(p.block_free, p.blocks, lds) : 0;  // (uniform)
+    resize_one<kThreads>(p, b, word, is_served(word, begin, n_free), p.fresh + begin, threadIdx.x, []() { __syncthreads(); });
+}
+
+// Few sequences and pages: all of it in one work-group, at the end a wave per sequence.  Replayed from a graph a resize of 8 sequences takes
+// 3.6 us, in two launches 5.6; of 32 sequences 5.9, and 6.7; of 64 7.4, and 6.6.  Enqueued one by one 6.1 and 9.0.
+__global__ __launch_bounds__(kRankThreads) void resize_few_kernel(ResizeParams p) {
+    __shared__ int lds[kRankThreads / 64];
+    __shared__ int32_t fresh[kPagesPerBlock];
+    __shared__ int begin[kFewSequences], need[kFewSequences];
     const PageState &s = p.s;
-    const int b = blockIdx.x;
-    const int want = p.want[b];
-    const int word = p.need[b], need = word & kNeedMask;
-    const bool split = (word & kSplitBit) != 0;
-    bool ok = (word & kRefusedBit) == 0;
-    if (ok && need > 0) {  // (uniform)
-        const int n_free = block_sum_of<kThreads>(p.block_free, p.blocks, lds);
-        ok = p.begin[b] >= 0 && (int64_t)p.begin[b] + need <= n_free;  // (parts of page_table that overlap can ask for more than 2^31)
+    int is_free[4], n = 0, n_free, total;
+    for (int i = 0; i < 4; ++i) {
+        const int page = threadIdx.x * 4 + i;
+        is_free[i] = page < s.num_pages && s.page_refs[page] == 0;
+        n += is_free[i];
     }
-    const Seq q = seq_of(s, b);
-    const int len = s.kv_len[b];
-    __syncthreads();  // (count and length are read by everybody before one thread writes them)
-    if (threadIdx.x == 0) {
-        p.missing[b] = want >= 0 && !ok ? need : 0;
-        p.copy_src[b] = p.copy_dst[b] = -1;
+    int take = 0;
+    const int word = (int)threadIdx.x < s.B ? plan_of(p, threadIdx.x, take) : 0;
+    int rank = block_scan<kRankThreads>(n, n_free, lds) - n;
+    for (int i = 0; i < 4; ++i)
+        if (is_free[i]) fresh[rank++] = threadIdx.x * 4 + i;
+    const int to = block_scan<kRankThreads>(take, total, lds);
+    if ((int)threadIdx.x < s.B) {
+        begin[threadIdx.x] = to - take;
+        need[threadIdx.x] = word;
     }
-    if (want < 0 || !ok) return;
-    const int pages = (int)(((int64_t)want + ((1 << s.page_shift) - 1)) >> s.page_shift);
-    const int32_t *fresh = p.fresh + p.begin[b];
-    for (int e = pages + threadIdx.x; e < q.count; e += kThreads) {
-        const int32_t id = s.page_table[q.e0 + e];
-        if (is_page(s, id)) atomicSub(&s.page_refs[id], 1);
-        s.page_table[q.e0 + e] = -1;
-    }
-    for (int e = q.count + threadIdx.x; e < pages; e += kThreads) {
-        const int32_t id = fresh[split + e - q.count];
-        if (!is_page(s, id)) continue;  // (never, with tables as the header has them)
-        s.page_table[q.e0 + e] = id;
-        s.page_refs[id] = 1;
-    }
-    if (threadIdx.x == 0) {
-        if (split && is_page(s, fresh[0])) {
-            int32_t *entry = &s.page_table[q.e0 + (len >> s.page_shift)];
-            atomicSub(&s.page_refs[*entry], 1);
-            p.copy_src[b] = *entry;
-            p.copy_dst[b] = *entry = fresh[0];
-            s.page_refs[fresh[0]] = 1;
-        }
-        s.page_count[b] = pages;
-        s.kv_len[b] = min(len, want);
+    __syncthreads();  // (the state has been read as it was before the call)
+    for (int b = threadIdx.x >> 6; b < s.B; b += kRankThreads / 64) {  // (uniform in a wave)
+        const bool ok = is_served(need[b], begin[b], n_free);
+        resize_one<64>(p, b, need[b], ok, fresh + (ok ? begin[b] : 0), threadIdx.x & 63, []() { __builtin_amdgcn_wave_barrier(); });
     }
 }
 
@@ -490,6 +534,10 @@ respec_status_t respec_pages_resize(const int32_t *want_tokens, const int32_t *p
     p.need = p.begin + B;
     p.fresh = p.need + B;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (B <= kFewSequences && num_pages <= kPagesPerBlock) {
+        hipLaunchKernelGGL(resize_few_kernel, dim3(1), dim3(kRankThreads), 0, stream, p);
+        return launched("pages_resize");
+    }
     if (num_pages <= kFewPages) {
         hipLaunchKernelGGL(resize_plan_kernel<true>, dim3(p.blocks + 1), dim3(kRankThreads), 0, stream, p);
     } else {

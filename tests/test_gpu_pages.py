@@ -98,7 +98,7 @@ def test_forks_that_cannot_be():
     c.fork([-1, -1, 1, -1, -1])                            # of an empty sequence: empty
 
 
-@pytest.mark.parametrize("num_pages,B,ps", [(1, 1, 16), (37, 5, 16), (1024, 40, 64), (1025, 300, 16), (4096, 2000, 16), (4097, 20, 64), (9000, 33, 1024),
+@pytest.mark.parametrize("num_pages,B,ps", [(1, 1, 16), (37, 5, 16), (1024, 40, 64), (1025, 300, 16), (4096, 2000, 16), (4096, 64, 16), (4097, 20, 64), (9000, 33, 1024),
                                               (16384, 9, 16), (16385, 1030, 16), (70000, 60, 16)])
 def test_random_histories(num_pages, B, ps):
     rng = random.Random(num_pages)
