@@ -855,9 +855,9 @@ constexpr Cost kFour{1.0f, 1.3f, 3.65f, 11.1f}, kEight{1.79f, 1.79f, 5.5f, 8.f},
 float estimate(const Cost &c, int32_t B, int64_t groups, int splits, int rows, float mean_q, int32_t max_q, int32_t max_kv, int32_t D, bool bf16) {
     const float before = (float)std::max(0, max_kv - max_q), alike = before / max_kv * (B == 1 ? 1.f : 0.5f);
     const float mean = (before + mean_q / 2) / 64 / splits + c.over, longest = max_kv / 64.f / splits + c.over;
-    const float rounds = groups * splits / 256.f, up = std::ceil(rounds);
-    const float odd = std::fmod(up, 2.f) == 1.f ? c.lone - c.step : 0.f;
-    const float even = rounds * c.step * mean, whole = (up * c.step + odd) * mean;
+    const int64_t up = (groups * splits + 255) / 256;
+    const float odd = up % 2 == 1 ? c.lone - c.step : 0.f;
+    const float even = groups * splits / 256.f * c.step * mean, whole = (up * c.step + odd) * mean;
     const float t = std::max(even + alike * (whole - even), longest * c.lone);
     const float parts = splits == 1 ? 0.f : 5.4f + groups * splits * (float)rows * D * 8 / 3.6e6f;
     return c.base + (D == 128 ? 1.f : bf16 ? 0.6f : 0.52f) * t + parts;
