@@ -593,18 +593,23 @@ def _stream_on(index, stream):
     return _current_raw_stream(index)
 
 
+_INT32, _FLOAT32 = torch.int32, torch.float32
+
+
 def _ints(n, names, *tensors):
     """Contiguous int32 tensors of n elements (None: any number)."""
-    for i, t in enumerate(tensors):
-        if t.dtype is not torch.int32 or (n is not None and t.numel() != n) or not t.is_contiguous():
-            raise TypeError(f"{names.split()[i]} must be contiguous int32" + ("" if n is None else f" [{n}]"))
+    for t in tensors:
+        if t.dtype is not _INT32 or (n is not None and t.numel() != n) or not t.is_contiguous():
+            name = names.split()[[x is t for x in tensors].index(True)]
+            raise TypeError(f"{name} must be contiguous int32" + ("" if n is None else f" [{n}]"))
 
 
 def _floats(n, names, *tensors):
     """Contiguous float32 tensors of n elements; None may stand for an absent one."""
-    for i, t in enumerate(tensors):
-        if t is not None and (t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous()):
-            raise TypeError(f"{names.split()[i]} must be contiguous float32 [{n}]")
+    for t in tensors:
+        if t is not None and (t.dtype is not _FLOAT32 or t.numel() != n or not t.is_contiguous()):
+            name = names.split()[[x is t for x in tensors].index(True)]
+            raise TypeError(f"{name} must be contiguous float32 [{n}]")
 
 
 def _ptr(t):
@@ -618,11 +623,18 @@ def _room(workspace):
     return _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
 
 
-def _token_stride(t, name):
+def _token_stride(t, tokens, heads, D, name):
     """Elements between the tokens of a [tokens, heads, D] tensor whose tokens are contiguous in themselves."""
-    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+    token, head, one = t.stride()
+    if one != 1 or (head != D and heads > 1):
         raise ValueError(f"{name} must be [tokens, heads, D] with contiguous tokens")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return token if tokens > 1 else heads * D
+
+
+def _three(t, name):
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens, heads, D]")
+    return t.shape
 
 
 def respec_prompt_attention_workspace_bytes(B, total_q, total_kv, max_q_per_seq, max_kv_len, Hq, Hkv, D, dt) -> int:
@@ -632,71 +644,73 @@ def respec_prompt_attention_workspace_bytes(B, total_q, total_kv, max_q_per_seq,
 def respec_prompt_attention(q, k, v, q_indptr, kv_indptr, out, lse, max_q_per_seq, max_kv_len, sm_scale, workspace, stream=None):
     """q [total_q,Hq,D], k and v [total_kv,Hkv,D] (slices along the token stride are fine), out contiguous; q_indptr int32,
     kv_indptr int64."""
-    total_q, Hq, D = q.shape
-    total_kv, Hkv, _ = k.shape
-    B = q_indptr.numel() - 1
+    total_q, Hq, D = shape = _three(q, "q")
+    total_kv, Hkv, Dk = kv_shape = _three(k, "k")
+    B, dtype = q_indptr.numel() - 1, q.dtype
     index = _here(q, k, v, q_indptr, kv_indptr, out, lse, workspace)
     _ints(B + 1, "q_indptr", q_indptr)
-    if kv_indptr.dtype != torch.int64 or kv_indptr.numel() != B + 1 or not kv_indptr.is_contiguous():
+    if kv_indptr.dtype is not torch.int64 or kv_indptr.numel() != B + 1 or not kv_indptr.is_contiguous():
         raise TypeError(f"kv_indptr must be contiguous int64 [{B + 1}]")
-    if k.dtype != q.dtype or v.dtype != q.dtype or out.dtype != q.dtype:
+    if k.dtype is not dtype or v.dtype is not dtype or out.dtype is not dtype:
         raise TypeError("q, k, v and out must share one dtype")
-    if k.shape[2] != D or v.shape != k.shape or out.shape != q.shape or not out.is_contiguous():
+    if Dk != D or v.shape != kv_shape or out.shape != shape or not out.is_contiguous():
         raise ValueError("k and v must be [total_kv, Hkv, D] with q's D, and out contiguous in q's shape")
     _floats(total_q * Hq, "lse", lse)
     _check(load().respec_prompt_attention(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), q_indptr.data_ptr(), kv_indptr.data_ptr(), out.data_ptr(), _ptr(lse), B, total_q,
-        total_kv, max_q_per_seq, max_kv_len, Hq, Hkv, D, _token_stride(q, "q"), _token_stride(k, "k"), _token_stride(v, "v"),
-        float(sm_scale), _dtype_code(q), *_room(workspace), _stream_on(index, stream)))
+        total_kv, max_q_per_seq, max_kv_len, Hq, Hkv, D, _token_stride(q, total_q, Hq, D, "q"), _token_stride(k, total_kv, Hkv, D, "k"),
+        _token_stride(v, total_kv, Hkv, D, "v"), float(sm_scale), _dtype_code(q), *_room(workspace), _stream_on(index, stream)))
 
 
 def _pools(k_pages, v_pages):
-    if k_pages.dim() != 4 or v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype or not (
+    shape = k_pages.shape
+    if len(shape) != 4 or v_pages.shape != shape or v_pages.dtype is not k_pages.dtype or not (
             k_pages.is_contiguous() and v_pages.is_contiguous()):
         raise ValueError("k_pages and v_pages must be contiguous [num_pages, page_size, Hkv, D] of one shape and dtype")
-    return k_pages.shape
+    return shape
 
 
 def respec_prompt_attention_paged(q, k_pages, v_pages, q_indptr, page_indptr, page_table, kv_len, out, lse, max_q_per_seq,
                                   max_kv_len, sm_scale, workspace, stream=None):
     """q [total_q,Hq,D] (token stride), k_pages and v_pages [num_pages, page_size, Hkv, D]; out is written in place."""
-    total_q, Hq, D = q.shape
+    total_q, Hq, D = shape = _three(q, "q")
     num_pages, page_size, Hkv, Dk = _pools(k_pages, v_pages)
-    B = q_indptr.numel() - 1
+    B, dtype = q_indptr.numel() - 1, q.dtype
     index = _here(q, k_pages, v_pages, q_indptr, page_indptr, page_table, kv_len, out, lse, workspace)
     _ints(B + 1, "q_indptr page_indptr", q_indptr, page_indptr)
     _ints(B, "kv_len", kv_len)
     _ints(None, "page_table", page_table)
-    if k_pages.dtype != q.dtype or out.dtype != q.dtype:
+    if k_pages.dtype is not dtype or out.dtype is not dtype:
         raise TypeError("q, k_pages, v_pages and out must share one dtype")
-    if Dk != D or out.shape != q.shape or not out.is_contiguous():
+    if Dk != D or out.shape != shape or not out.is_contiguous():
         raise ValueError("k_pages and v_pages must have q's D, and out must be contiguous in q's shape")
     _floats(total_q * Hq, "lse", lse)
     _check(load().respec_prompt_attention_paged(
         q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), q_indptr.data_ptr(), page_indptr.data_ptr(), page_table.data_ptr(),
         kv_len.data_ptr(), out.data_ptr(), _ptr(lse), B, total_q, num_pages, page_table.numel(), page_size, max_q_per_seq, max_kv_len,
-        Hq, Hkv, D, _token_stride(q, "q"), float(sm_scale), _dtype_code(q), *_room(workspace), _stream_on(index, stream)))
+        Hq, Hkv, D, _token_stride(q, total_q, Hq, D, "q"), float(sm_scale), _dtype_code(q), *_room(workspace), _stream_on(index, stream)))
 
 
 def respec_append_paged(k_new, v_new, k_pages, v_pages, q_indptr, page_indptr, page_table, kv_len, max_q_per_seq, stream=None):
     """k_new, v_new [total_q, Hkv, D] (one token stride) into the last R_b of every sequence's kv_len tokens; the pools are
     changed in place."""
     num_pages, page_size, Hkv, D = _pools(k_pages, v_pages)
-    B = q_indptr.numel() - 1
+    total_q, H, Dn = shape = _three(k_new, "k_new")
+    B, dtype = q_indptr.numel() - 1, k_pages.dtype
     index = _here(k_new, v_new, k_pages, v_pages, q_indptr, page_indptr, page_table, kv_len)
     _ints(B + 1, "q_indptr page_indptr", q_indptr, page_indptr)
     _ints(B, "kv_len", kv_len)
     _ints(None, "page_table", page_table)
-    if k_new.dtype != k_pages.dtype or v_new.dtype != k_pages.dtype:
+    if k_new.dtype is not dtype or v_new.dtype is not dtype:
         raise TypeError("the new tokens must have the pools' dtype")
-    if tuple(k_new.shape[1:]) != (Hkv, D) or v_new.shape != k_new.shape:
+    if H != Hkv or Dn != D or v_new.shape != shape:
         raise ValueError("k_new and v_new must be [total_q, Hkv, D]")
-    ld = _token_stride(k_new, "k_new")
-    if _token_stride(v_new, "v_new") != ld:
+    ld = _token_stride(k_new, total_q, H, D, "k_new")
+    if _token_stride(v_new, total_q, H, D, "v_new") != ld:
         raise ValueError("k_new and v_new must have one token stride")
     _check(load().respec_append_paged(
         k_new.data_ptr(), v_new.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), q_indptr.data_ptr(), page_indptr.data_ptr(),
-        page_table.data_ptr(), kv_len.data_ptr(), B, k_new.shape[0], max_q_per_seq, num_pages, page_table.numel(), page_size, Hkv, D, ld,
+        page_table.data_ptr(), kv_len.data_ptr(), B, total_q, max_q_per_seq, num_pages, page_table.numel(), page_size, Hkv, D, ld,
         _dtype_code(k_pages), _stream_on(index, stream)))
 
 
@@ -757,9 +771,10 @@ def respec_pages_copy(k_pages, v_pages, copy_src, copy_dst, stream=None):
 
 def _rows_of(logits):
     rows, V = logits.shape
-    if V > 1 and logits.stride(1) != 1:
+    row, one = logits.stride()
+    if one != 1 and V > 1:
         raise ValueError("logits rows must be unit-stride")
-    return rows, V, logits.stride(0) if rows > 1 else V
+    return rows, V, row if rows > 1 else V
 
 
 def respec_token_logprobs_workspace_bytes(rows, V, top_n, dt) -> int:
@@ -778,9 +793,10 @@ def respec_token_logprobs(logits, tokens, logprob, lse, entropy, top_tokens, top
         raise ValueError("top_tokens and top_logprobs go together")
     n = 0
     if top_tokens is not None:
-        if top_tokens.dim() != 2 or top_tokens.shape[0] != rows:
+        shape = top_tokens.shape
+        if len(shape) != 2 or shape[0] != rows:
             raise ValueError("top_tokens must be [rows, n]")
-        n = top_tokens.shape[1]
+        n = shape[1]
         _ints(rows * n, "top_tokens", top_tokens)
         _floats(rows * n, "top_logprobs", top_logprobs)
     _check(load().respec_token_logprobs(
@@ -795,9 +811,9 @@ def respec_token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob, grad_
     index = _here(logits, tokens, lse, entropy, grad_logprob, grad_entropy, grad_logits, row_temperature)
     _ints(rows, "tokens", tokens)
     _floats(rows, "lse entropy grad_logprob grad_entropy row_temperature", lse, entropy, grad_logprob, grad_entropy, row_temperature)
-    if grad_logits.shape != logits.shape or grad_logits.dtype != logits.dtype:
+    rows_g, V_g, ld_g = _rows_of(grad_logits)
+    if rows_g != rows or V_g != V or grad_logits.dtype is not logits.dtype:
         raise ValueError("grad_logits must have the logits' shape and dtype")
-    ld_g = _rows_of(grad_logits)[2]
     _check(load().respec_token_logprobs_grad(
         logits.data_ptr(), tokens.data_ptr(), _ptr(row_temperature), lse.data_ptr(), _ptr(entropy), _ptr(grad_logprob),
         _ptr(grad_entropy), grad_logits.data_ptr(), rows, V, ld, ld_g, float(temperature), _dtype_code(logits), _stream_on(index, stream)))
