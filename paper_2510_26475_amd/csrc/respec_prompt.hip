@@ -963,6 +963,7 @@ respec_status_t run(const char *name, PromptParams &p, const void *k, const void
     p.tiles = (int32_t)pl.tiles;
     for (p.g_shift = 0; (1 << p.g_shift) < p.G; ++p.g_shift) {}
     p.g_mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << p.g_shift) - p.G)) / p.G + 1);
+    p.g_shift = std::max(1u, p.g_shift);  // (G = 1 divides nothing)
     const uint32_t sign = dt == RESPEC_BF16 ? 0x80008000u : 0x80000000u;
     p.q_and = sm_scale == 0.f ? 0u : ~0u;
     p.q_xor = sm_scale < 0.f ? sign : 0u;

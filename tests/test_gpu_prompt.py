@@ -294,3 +294,34 @@ def test_many_sequences_of_one_token():
     v = randn(B, 2, 64, dt=torch.bfloat16, seed=3)
     out, _ = run(q, k, v, [1] * B, [1] * B, 0.125)
     assert torch.equal(out, v.repeat_interleave(2, dim=1))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_loose_hints(dtype):
+    """Bounds far above the batch change how the work is cut, not what comes out."""
+    R, L = [40, 1, 0, 130], [40, 600, 9, 131]
+    q, k = randn(sum(R), 6, 128, dt=DT[dtype], seed=1), randn(sum(L), 2, 128, dt=DT[dtype], seed=2)
+    v = randn(sum(L), 2, 128, dt=DT[dtype], seed=3)
+    ref = plain.prompt_attention(q, split_keys(k, L), split_keys(v, L), R, L, 0.1)
+    for max_q, max_kv in ((130, 600), (sum(R), sum(L)), (1 << 20, 1 << 30), (1 << 20, 2 ** 31 - 257)):
+        out, lse = torch.full_like(q, 7.0), torch.full((sum(R), 6), 7.0, device="cuda")
+        ws = workspace(4, sum(R), sum(L), max_q, max_kv, (6, 2, 128), DT[dtype])
+        binding.respec_prompt_attention(q, k, v, offsets(R, torch.int32), offsets(L, torch.int64), out, lse, max_q, max_kv, 0.1, ws)
+        plain.check_prompt(out, lse, ref)
+
+
+def test_two_calls_at_once():
+    """On two streams, each with its workspace; both cut their keys into parts."""
+    calls = []
+    for seed, (R, L) in enumerate((([30, 2], [3000, 4100]), ([5, 50, 1], [700, 2000, 5000]))):
+        q, k = randn(sum(R), 8, 128, dt=torch.bfloat16, seed=seed), randn(sum(L), 2, 128, dt=torch.bfloat16, seed=seed + 9)
+        want, _ = run(q, k, k, R, L, 0.1)
+        ws = workspace(len(R), sum(R), sum(L), max(R), max(L), (8, 2, 128), torch.bfloat16)
+        calls.append((torch.cuda.Stream(), q, k, offsets(R, torch.int32), offsets(L, torch.int64), torch.zeros_like(q), max(R), max(L), ws, want))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for stream, q, k, a, b, out, max_q, max_kv, ws, _ in calls:
+            binding.respec_prompt_attention(q, k, k, a, b, out, None, max_q, max_kv, 0.1, ws, stream=stream)
+    torch.cuda.synchronize()
+    for *_, out, _, _, _, want in calls:
+        assert torch.equal(out, want)
