@@ -131,10 +131,16 @@ __device__ inline int length_of(const PromptParams &p, int b, int64_t &kv0) {
     }
 }
 
-// The number-th tile of a batch of up to 64 sequences (one per lane), the one that sees most keys first: work-groups are given out in
-// order, and a long one among the last would be waited for.  How many tiles see x keys or more is known for every sequence
-// without looking at its tiles, so x is found by bisection, in steps of 64 keys.  (16 packed prompts of 65 to 2,048 tokens at 28/4
-// heads take 145 us, in the order of the sequences 152; 8 chunks behind up to 8,192 tokens at 40/8 heads 374, and 394.)
+__device__ inline int bits_before(uint64_t mask) {  // set bits of lanes before this one
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// The number-th tile of a batch of up to 64 sequences (one per lane), those that see most keys first, in steps of kOrderStep keys:
+// work-groups are given out in order, and a long one among the last would be waited for.  How many tiles see x keys or more is known
+// for every sequence without looking at its tiles, so the step is found by bisection.  (16 packed prompts of 65 to 2,048 tokens at
+// 28/4 heads take 143 us, in the order of the sequences 161; 8 chunks behind up to 8,192 tokens at 40/8 heads 332, and 362; in steps of 64
+// keys 144 and 338.)
+constexpr int kOrderStep = 256, kInTurn = 32;
 template <bool PAGED, int ROWS>
 __device__ inline bool find_longest(const PromptParams &p, int number, Tile &out, int &tokens, int64_t &first) {
     const int lane = threadIdx.x & 63;
@@ -146,15 +152,15 @@ __device__ inline bool find_longest(const PromptParams &p, int number, Tile &out
         L = length_of<PAGED>(p, lane, kv0);
     }
     const int tiles = (R * p.G + ROWS - 1) / ROWS, before = L - R;  // (before: negative where the first rows see nothing)
-    auto reach = [&](int x) __attribute__((always_inline)) {  // this sequence's tiles that see 64 x keys or more
+    auto reach = [&](int x) __attribute__((always_inline)) {  // this sequence's tiles that see kOrderStep x keys or more
         if (x <= 0) return tiles;
-        if ((int64_t)x * 64 > L || tiles == 0) return 0;
-        const int first = ((max(x * 64 - before - 1, 0) * p.G + 1) + ROWS - 1) / ROWS - 1;  // (the last tile's last row sees L keys)
+        if ((int64_t)x * kOrderStep > L || tiles == 0) return 0;
+        const int first = ((max(x * kOrderStep - before - 1, 0) * p.G + 1) + ROWS - 1) / ROWS - 1;  // (the last tile's last row sees L keys)
         return tiles - max(0, min(first, tiles - 1));
     };
     auto all = [&](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(wave_scan_add(reach(x)), 63); };
     if (number >= all(0)) return false;
-    int x = 0, over = p.max_kv / 64 + 1, n_over = 0;  // all(x) > number >= all(over)
+    int x = 0, over = p.max_kv / kOrderStep + 1, n_over = 0;  // all(x) > number >= all(over)
     while (p.B > 1 && over - x > 1) {
         const int at = (x + over) / 2, n_at = all(at);
         if (n_at > number) x = at;
@@ -162,15 +168,22 @@ __device__ inline bool find_longest(const PromptParams &p, int number, Tile &out
     }
     const int more = p.B == 1 ? 0 : reach(over), mine = p.B == 1 ? tiles : reach(x) - more;  // (one sequence: its tiles from the last)
     // Among the tiles of a step one of every sequence in turn: an XCD, which is given every eighth work-group, then meets fewer sequences' keys
-    // at a time than with one sequence after the other (16 prompts of 1,024 tokens at 28/4 heads take 166 us, and 174).
+    // at a time than with one sequence after the other (16 prompts of 1,024 tokens at 28/4 heads take 162 us, and 166).  Of many sequences
+    // that is too much for its L2, and one comes after the other (64 of 256 tokens 84 us, in turn 88).
     int rest = number - (p.B == 1 ? 0 : n_over), turn = 0;
     uint64_t left = __ballot(mine > 0);
-    if (p.B == 1) turn = rest, rest = 0;
-    for (int n = (int)__popcll(left); rest >= n; n = (int)__popcll(left)) {
-        rest -= n;
-        left = __ballot(mine > ++turn);
+    int at;
+    if (__popcll(left) > kInTurn || p.B == 1) {
+        const int sum = wave_scan_add(mine);
+        at = (int)__builtin_ctzll(__ballot(sum > rest));
+        turn = rest - __builtin_amdgcn_readlane(sum - mine, at);
+    } else {
+        for (int n = (int)__popcll(left); rest >= n; n = (int)__popcll(left)) {
+            rest -= n;
+            left = __ballot(mine > ++turn);
+        }
+        at = (int)__builtin_ctzll(__ballot((left >> lane & 1) != 0 && bits_before(left) == rest));
     }
-    const int at = (int)__builtin_ctzll(__ballot((left >> lane & 1) != 0 && (int)__popcll(left & ((1ull << lane) - 1)) == rest));
     out.b = at;
     out.tiles = __builtin_amdgcn_readlane(tiles, at);
     out.index = __builtin_amdgcn_readlane(tiles - more, at) - 1 - turn;
