@@ -325,3 +325,14 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for *_, out, _, _, _, want in calls:
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads", [(1, 1, 128), (130, 1, 64), (300, 2, 64), (64, 1, 128)], ids=str)
+def test_one_head_and_more_heads_than_a_tile_has_rows(dtype, heads):
+    Hq, Hkv, D = heads
+    R, L = [3, 40, 1], [3, 140, 70]
+    q, k = randn(sum(R), Hq, D, dt=DT[dtype], seed=1), randn(sum(L), Hkv, D, dt=DT[dtype], seed=2)
+    v = randn(sum(L), Hkv, D, dt=DT[dtype], seed=3)
+    out, lse = run(q, k, v, R, L, D ** -0.5)
+    plain.check_prompt(out, lse, plain.prompt_attention(q, split_keys(k, L), split_keys(v, L), R, L, D ** -0.5))
