@@ -600,8 +600,8 @@ __device__ __attribute__((always_inline)) inline void each(F &&f) {
 // for two steps is enough.  Four waves: two tiles of each and two work-groups per compute unit, K of t+2 and V of t+1, a
 // barrier per step.  The loop is written for as many steps as there are tiles in
 // LDS, so that a tile's place is a constant.
-// One prompt of 16,384 tokens at 16/2 heads of 128 takes 990 us (1.1 PFLOP/s): the matrix pipes are busy 58 % of the cycles, of a clock
-// that the power holds at 1.6 to 1.7 GHz.  16 prompts of 65 to 2,048 at 28/4 heads take 143 us: a work-group spends 14,000 of its 44,000
+// One prompt of 16,384 tokens at 16/2 heads of 128 takes 980 us (1.1 PFLOP/s): the matrix pipes are busy 59 % of the cycles, of a clock
+// that the power holds at 1.7 GHz.  16 prompts of 65 to 2,048 at 28/4 heads take 140 us: a work-group spends 14,000 of its 44,000
 // cycles on its rows, Q, the first keys and the output, half of it behind the other work-group of its compute unit.
 template <int D, int WAVES, bool PAGED>
 __global__ __launch_bounds__(WAVES * 64, 2) void prompt_bf16_kernel(PromptParams p) {
