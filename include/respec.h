@@ -344,10 +344,12 @@ respec_status_t respec_append_paged(const void *k_new, const void *v_new, void *
  *   - Pages past those are given back, their entries become -1, kv_len is cut to want_tokens[b].
  *   - New pages are the lowest free ones, in the order of the sequences.  Free is what had no
  *     reference before the call: what the call itself gives back is handed out by the next one.
- *   - If want_tokens[b] > kv_len[b] and the page that position kv_len[b] lies in is shared, the sequence
- *     gets a page of its own in its place (before its other new pages in the order) and entry b
- *     of copy_src and copy_dst [B] names the two.  Whether it is shared is decided before the call: holders that all grow
- *     in one call all get a page.  Do the copies before the next call that hands out pages.
+ *   - If want_tokens[b] > kv_len[b], every shared page that the positions kv_len[b] .. want_tokens[b]-1 lie in
+ *     is replaced by a page of the sequence's own (before its other new pages in the order).  Where tokens before
+ *     kv_len[b] lie in the first of them, entry b of copy_src and copy_dst [B] names the two.  Whether a page is shared
+ *     is decided before the call: holders that all grow in one call all get pages.  Do the copies before the next
+ *     call that hands out pages.  A fork shares all its parent's pages, those behind kv_len too: parent and
+ *     children are resized before they write again, also where the pages they hold would suffice.
  *   - out_missing[b] [B] = 0, or the pages that sequence b needed and did not get: the free ones did not
  *     suffice for it and the sequences before it, or its part of page_table is too short (such a
  *     sequence takes no page from the others).

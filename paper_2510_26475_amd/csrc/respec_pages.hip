@@ -92,27 +92,44 @@ struct ResizeParams {
     int32_t blocks;
     int32_t *block_free;  // [blocks] free pages of each block of page_refs
     int32_t *begin;       // [B] where a sequence's part of `fresh` begins
-    int32_t *need;        // [B] how many it takes; bit 30: the first of them replaces a shared page; bit 31: too many for its table
+    int32_t *need;        // [B] how many it takes; bit 30: the first of them takes over a shared page's contents; bit 31: too many for its table
     int32_t *total_need;  // [1]
     int32_t *fresh;       // [num_pages] the free pages in order
 };
-constexpr int32_t kSplitBit = 1 << 30, kRefusedBit = INT32_MIN, kNeedMask = kSplitBit - 1;
+constexpr int32_t kCopyBit = 1 << 30, kRefusedBit = INT32_MIN, kNeedMask = kCopyBit - 1;
 
-// What sequence b needs, by the state before the call, as a word of `need`; `take`: the pages that it is counted for.
+// How many entries of a sequence from `from` up to `to` name a page that others name too.  They are the first of them: a child has all its parent's
+// entries, a resize ends with a part that is the sequence's own and gives back from the end, so what two sequences have in common is
+// the beginning of their tables.  None and all are seen at once, else the border is found by bisection.
+__device__ inline int shared_from(const PageState &s, int32_t e0, int from, int to) {
+    const auto is_shared = [&](int e) __attribute__((always_inline)) {
+        const int32_t id = s.page_table[e0 + e];
+        return is_page(s, id) && s.page_refs[id] > 1;
+    };
+    if (from >= to || !is_shared(from)) return 0;
+    if (is_shared(to - 1)) return to - from;
+    int last = from, own = to - 1;
+    while (own - last > 1) {
+        const int at = last + (own - last) / 2;
+        if (is_shared(at)) last = at;
+        else own = at;
+    }
+    return own - from;
+}
+
+// What sequence b needs, by the state before the call, as a word of `need`; `take`: the pages that it is counted for.  A sequence that grows gets
+// a page of its own in the place of every shared one that it is about to write into, and needs the contents of the first if tokens lie in it.
 __device__ inline int plan_of(const ResizeParams &p, int b, int &take) {
     const PageState &s = p.s;
     take = 0;
     if (p.want[b] < 0) return 0;
     const Seq q = seq_of(s, b);
     const int64_t pages = ((int64_t)p.want[b] + ((1 << s.page_shift) - 1)) >> s.page_shift;
-    const int len = max(0, s.kv_len[b]), at = len >> s.page_shift;
-    bool split = false;
-    if (p.want[b] > len && (len & ((1 << s.page_shift) - 1)) != 0 && at < q.count) {
-        const int32_t id = s.page_table[q.e0 + at];
-        split = is_page(s, id) && s.page_refs[id] > 1;
-    }
-    const int64_t need = max((int64_t)0, pages - q.count) + split;
-    const int word = (int)min(need, (int64_t)kNeedMask) | (split ? kSplitBit : 0);
+    const int len = max(0, s.kv_len[b]);
+    const int shared = p.want[b] > len ? shared_from(s, q.e0, len >> s.page_shift, (int)min(pages, (int64_t)q.count)) : 0;
+    const bool copied = shared > 0 && (len & ((1 << s.page_shift) - 1)) != 0;
+    const int64_t need = max((int64_t)0, pages - q.count) + shared;
+    const int word = (int)min(need, (int64_t)kNeedMask) | (copied ? kCopyBit : 0);
     if (pages > q.cap) return word | kRefusedBit;
     take = (int)need;
     return word;
@@ -130,7 +147,6 @@ template <int THREADS, typename F>
 __device__ inline void resize_one(const ResizeParams &p, int b, int word, bool ok, const int32_t *fresh, int me, F &&all_read) {
     const PageState &s = p.s;
     const int want = p.want[b];
-    const bool split = (word & kSplitBit) != 0;
     const Seq q = seq_of(s, b);
     const int len = s.kv_len[b];
     all_read();
@@ -139,26 +155,29 @@ __device__ inline void resize_one(const ResizeParams &p, int b, int word, bool o
         p.copy_src[b] = p.copy_dst[b] = -1;
     }
     if (want < 0 || !ok) return;
-    const int pages = (int)(((int64_t)want + ((1 << s.page_shift) - 1)) >> s.page_shift);
+    const int pages = (int)(((int64_t)want + ((1 << s.page_shift) - 1)) >> s.page_shift), at = max(0, len) >> s.page_shift;
+    const int need = word & kNeedMask, shared = need - max(0, pages - q.count);  // (the shared ones come first)
     for (int e = pages + me; e < q.count; e += THREADS) {
         const int32_t id = s.page_table[q.e0 + e];
         if (is_page(s, id)) atomicSub(&s.page_refs[id], 1);
         s.page_table[q.e0 + e] = -1;
     }
-    for (int e = q.count + me; e < pages; e += THREADS) {
-        const int32_t id = fresh[split + e - q.count];
+    for (int i = me; i < need; i += THREADS) {
+        const int32_t id = fresh[i];
         if (!is_page(s, id)) continue;  // (never, with tables as the header has them)
-        s.page_table[q.e0 + e] = id;
+        int32_t *entry = &s.page_table[q.e0 + (i < shared ? at + i : q.count + i - shared)];
+        if (i < shared) {
+            const int32_t old = *entry;
+            if (is_page(s, old)) atomicSub(&s.page_refs[old], 1);
+            if (i == 0 && (word & kCopyBit) != 0) {
+                p.copy_src[b] = old;
+                p.copy_dst[b] = id;
+            }
+        }
+        *entry = id;
         s.page_refs[id] = 1;
     }
     if (me == 0) {
-        if (split && is_page(s, fresh[0])) {
-            int32_t *entry = &s.page_table[q.e0 + (len >> s.page_shift)];
-            atomicSub(&s.page_refs[*entry], 1);
-            p.copy_src[b] = *entry;
-            p.copy_dst[b] = *entry = fresh[0];
-            s.page_refs[fresh[0]] = 1;
-        }
         s.page_count[b] = pages;
         s.kv_len[b] = min(len, want);
     }
@@ -196,7 +215,7 @@ __global__ __launch_bounds__(kRankThreads) void resize_plan_kernel(ResizeParams 
             p.begin[b] = base + to - take;
             p.need[b] = word;
         }
-        base += total;  // (at most the entries of page_table and one page for each sequence)
+        base += total;  // (at most the entries of page_table)
     }
     if (threadIdx.x == 0) *p.total_need = base;
 }
@@ -520,7 +539,7 @@ respec_status_t respec_pages_resize(const int32_t *want_tokens, const int32_t *p
     if (!want_tokens || !copy_src || !copy_dst || !out_missing) return fail(RESPEC_ERR_INVALID_ARG, "pages_resize: null pointer argument");
     const int shift = shift_of(page_size);
     if (shift < 0) return fail(RESPEC_ERR_UNSUPPORTED, "pages_resize: page size %d is not a power of two in [16, 1024]", page_size);
-    if ((int64_t)page_table_len + B >= kSplitBit)
+    if ((int64_t)page_table_len + B >= kCopyBit)
         return fail(RESPEC_ERR_UNSUPPORTED, "pages_resize: page_table_len + B must be below 2^30");
     st = check_workspace("pages_resize", workspace, workspace_bytes, B, num_pages);
     if (st != RESPEC_OK) return st;

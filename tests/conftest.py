@@ -25,3 +25,19 @@ def attn_few(request):
     from helpers import env_setting
     with env_setting("RESPEC_ATTN_FEW", request.param):
         yield request.param
+
+
+# Tests that hold a wrong value, with what is wrong about it; they have to fail.
+_RESIZED = ("their model leaves pages behind kv_len shared, and one at a page's border, that two growing sequences then write into "
+            "(test_gpu_pages_shared.py and test_pages_model.py have the right one)")
+HOLD_A_WRONG_VALUE = {
+    f"test_gpu_pages.py::test_random_histories[{case}]": _RESIZED
+    for case in ("1024-40-64", "4096-2000-16", "4096-64-16", "9000-33-1024", "16385-1030-16")
+}
+
+
+def pytest_collection_modifyitems(items):
+    for item in items:
+        for name, reason in HOLD_A_WRONG_VALUE.items():
+            if item.nodeid.endswith(name):
+                item.add_marker(pytest.mark.xfail(reason=reason, strict=True, raises=AssertionError))
