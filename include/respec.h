@@ -311,9 +311,10 @@ respec_status_t respec_prompt_attention_paged(const void *q, const void *k_pages
 /*
  * The K/V of new tokens into the pages that the paged attention reads: row i of sequence b
  * (k_new, v_new [total_q, Hkv, D], token stride ld_new elements) goes to position kv_len[b]-R_b+i.
- * Rows whose position is negative, past the sequence's pages, or in a page id outside
- * [0, num_pages) are not written anywhere.  kv_len is not changed.  Pages that are written must
- * belong to one sequence only (respec_pages_resize sees to that).
+ * Rows i >= max_q_per_seq, and rows whose position is negative, past the sequence's pages, or in a page id
+ * outside [0, num_pages) are not written anywhere; the others go where they belong all the same.
+ * kv_len is not changed.  Pages that are written must belong to one sequence only (respec_pages_resize
+ * sees to that).
  *   Hkv*D*sizeof(element) and the stride in bytes must be multiples of 16, data pointers 16-byte aligned.
  */
 respec_status_t respec_append_paged(const void *k_new, const void *v_new, void *k_pages, void *v_pages,

@@ -447,13 +447,15 @@ struct AppendParams {
 constexpr int kAppendRows = 8;  // rows of a work-group
 
 // Bound by HBM: 4,096 tokens of 8 heads of 128 (33.6 MB read and written) take 8.0 us, 8.2 with two loads in flight.
-
+// A row's position follows from the length and the number of rows as they are given, whatever of them is left out: rows past max_q, and
+// those whose position the sequence's pages do not have.
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams p) {
     Tile t;
     if (!find_tile(p.q_indptr, p.B, p.total_q, p.max_q, 1, kAppendRows, blockIdx.x, t)) return;
-    int e0 = max(0, min(p.page_indptr[t.b], p.table_len));
+    const int e0 = max(0, min(p.page_indptr[t.b], p.table_len));
     const int pages = max(0, min(p.page_indptr[t.b + 1], p.table_len) - e0);
-    const int64_t L = max((int64_t)0, min((int64_t)p.kv_len[t.b], (int64_t)pages << p.page_shift));
+    const int64_t end = (int64_t)pages << p.page_shift;
+    const int64_t pos0 = (int64_t)p.kv_len[t.b] - (min(p.q_indptr[t.b + 1], p.total_q) - t.q0);  // of row 0
     const int pieces = p.token_bytes / 16, rows = min(kAppendRows, t.R - t.index * kAppendRows);
     for (int i0 = threadIdx.x; i0 < rows * pieces; i0 += 4 * kThreads) {
         u32x4 a[4], c[4];
@@ -462,8 +464,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams p) {
         for (int j = 0; j < 4; ++j) {  // (eight loads in flight: behind a store the next loads would wait, as the memory may be the same)
             to[j] = -1;
             const int i = i0 + j * kThreads, r = t.index * kAppendRows + i / pieces, piece = i % pieces;
-            const int64_t pos = L - t.R + r;
-            if (i >= rows * pieces || pos < 0) continue;
+            const int64_t pos = pos0 + r;
+            if (i >= rows * pieces || pos < 0 || pos >= end) continue;
             const int32_t id = p.page_table[e0 + (pos >> p.page_shift)];
             if ((uint32_t)id >= (uint32_t)p.num_pages) continue;
             const int64_t from = (t.q0 + r) * p.ld_bytes + (int64_t)piece * 16;
