@@ -645,7 +645,7 @@ respec_status_t respec_token_logprobs(const void *logits, const int32_t *tokens,
  * The gradient of a loss over them in the logits: with g = dloss/dlogprob[r] and h = dloss/dentropy[r]
  *     grad_logits[r, x] = (g ([x = tokens[r]] - p(x)) - h p(x) (log p(x) + H_r)) / T
  * from the lse and entropy that respec_token_logprobs wrote for the same logits, tokens and
- * temperatures.  Rows without a token get zeros (and are not read).
+ * temperatures.  Rows without a token get zeros (and are not read); a row whose lse is NaN or -inf gets NaN.
  *   grad_logprob  [rows] f32 or NULL (zeros); grad_entropy [rows] f32 or NULL (zeros; entropy may be
  *                 NULL then); not both NULL
  *   grad_logits   [rows, V] logits_dt, row stride ld_g (written; bf16: rounded to nearest even).  It may be

@@ -625,9 +625,10 @@ struct GradRow {
     int32_t token;
     __device__ float at(float x, int64_t i) const {
         // (log p first: in log2 units the products with 1/T and log2 e of both terms would be rounded before their difference is)
-        const float log_p = fmaxf(fmaf(x, inv_t, -lse), kFar);
+        // (a NaN, of a row that is not finite, stays one in the probability; the maximum would drop it)
+        const float log_p = fmaf(x, inv_t, -lse);
         const float prob = __builtin_amdgcn_exp2f(log_p * 1.44269504088896341f);
-        float g = -prob * (g_lp + g_h * (log_p + H));
+        float g = -prob * (g_lp + g_h * (fmaxf(log_p, kFar) + H));
         if (i == token) g += g_lp;
         return g * inv_t;
     }
