@@ -279,7 +279,9 @@ respec_status_t respec_commit_accepted_paged(void *k_pages, void *v_pages, const
  *             not processed (max_kv_len at most 2^31 - 257).  How the work is cut follows them: close ones are faster
  *   D in {64, 128}; Hq % Hkv == 0; strides multiples of 16 bytes; data pointers 16-byte aligned.
  *   workspace respec_prompt_attention_workspace_bytes(...) bytes, 256-byte aligned, scratch (nothing
- *             to prepare, nothing survives): calls that overlap need one each, captured ones too.
+ *             to prepare, nothing survives): calls that overlap need one each, captured ones too.  What is named for
+ *             some sizes (at most 130 MiB) is enough for every call of these heads, D and dt whose other sizes
+ *             are no larger: few rows over many keys need most of it, as their keys are cut into parts.
  * A value of V that is not finite reaches only the rows that see its key.  Repeated calls give the same bits.
  */
 size_t respec_prompt_attention_workspace_bytes(int32_t B, int32_t total_q, int64_t total_kv, int32_t max_q_per_seq,

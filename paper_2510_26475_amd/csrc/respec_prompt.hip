@@ -855,7 +855,16 @@ struct Plan {
     int64_t tiles;  // bound of the row tiles of a KV head
     int32_t waves, splits;
     size_t o_bytes, ws_bytes;
+    size_t most_bytes;  // that a call with no larger sizes can need
 };
+
+struct PartBytes {
+    size_t o, all;
+};
+PartBytes part_bytes(size_t slots, int32_t D) {
+    const size_t o = round_up(slots * D * sizeof(float), 256);
+    return {o, std::max<size_t>(256, o + round_up(slots * 2 * sizeof(float), 256))};
+}
 
 // How a call is run: the form (bf16: four waves, 128 packed rows, two work-groups on a compute unit; eight waves, 256 rows, one; fp32:
 // 128 rows, or 32 whose tiles of keys four waves share out) and the parts its keys are cut into, whichever this estimate of the time in microseconds makes least.  A work-group costs `over`
@@ -894,10 +903,12 @@ bool make_plan(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_
     const long waves = kn.get(&Knobs::prompt_waves, 0), splits = kn.get(&Knobs::prompt_splits, 0);
     const float mean_q = std::min((float)max_q, (float)total_q / B);
     float least = INFINITY;
+    size_t most = 0;  // slots: all that the rule below may cut a call into, whose sizes are no larger
     for (const int w : {8, 4, 1}) {
         const bool fits = dt == RESPEC_F32 ? w != 8 : w != 1, forced = dt == RESPEC_F32 ? waves == 1 || waves == 4 : waves == 4 || waves == 8;
         if (!fits || (forced && w != waves)) continue;
         const int64_t tiles = tiles_bound(B, total_q, max_q, G, w * 32), groups = tiles * Hkv;
+        if (max_kv >= 128) most = std::max(most, (size_t)std::min<int64_t>(kSplitGroups, groups * std::min(kMaxSplits, max_kv / 64)) * w * 32);
         for (const int s : {1, 2, 3, 4, 6, 8, 12, kMaxSplits}) {
             if (s > 1 && (s > max_kv / 64 || groups * s > kSplitGroups)) break;
             const float t = estimate(dt == RESPEC_F32 ? (w == 4 ? kF32 : kF32Keys) : w == 8 ? kEight : kFour, B, groups, s, w * 32, mean_q, max_q, max_kv, D, dt == RESPEC_BF16);
@@ -909,11 +920,11 @@ bool make_plan(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_
         }
     }
     if (splits >= 1 && splits <= kMaxSplits) pl.splits = (int32_t)splits;
-    const int rows = pl.waves * 32;
-    const int64_t groups = pl.tiles * Hkv;
-    const size_t slots = pl.splits > 1 ? (size_t)groups * pl.splits * rows : 0;
-    pl.o_bytes = round_up(slots * D * sizeof(float), 256);
-    pl.ws_bytes = std::max<size_t>(256, pl.o_bytes + round_up(slots * 2 * sizeof(float), 256));
+    const size_t slots = pl.splits > 1 ? (size_t)(pl.tiles * Hkv) * pl.splits * pl.waves * 32 : 0;
+    const PartBytes need = part_bytes(slots, D);
+    pl.o_bytes = need.o;
+    pl.ws_bytes = need.all;
+    pl.most_bytes = part_bytes(std::max(slots, most), D).all;
     return true;
 }
 
@@ -1002,7 +1013,7 @@ size_t respec_prompt_attention_workspace_bytes(int32_t B, int32_t total_q, int64
     using namespace respec;
     Plan pl;
     if (total_kv <= 0 || !make_plan(B, total_q, std::min(max_q_per_seq, total_q), max_kv_len, Hq, Hkv, D, dt, pl)) return 0;
-    return pl.ws_bytes;
+    return pl.most_bytes;
 }
 
 respec_status_t respec_prompt_attention(const void *q, const void *k, const void *v, const int32_t *q_indptr, const int64_t *kv_indptr,
