@@ -336,7 +336,8 @@ respec_status_t respec_append_paged(const void *k_new, const void *v_new, void *
  *               entries name the pages it holds, the others are -1
  *   kv_len      [B] int32     tokens held (<= page_size * page_count[b])
  *   page_refs   [num_pages] int32   how many entries of page_table name a page; 0 = free
- * all in device memory, started by the caller as -1, zeros and zeros.  Nothing waits for the host:
+ * all in device memory, started by the caller as -1, zeros and zeros; page_table_len (resize: + B), num_pages and
+ * max_moves below 2^30 (RESPEC_ERR_UNSUPPORTED otherwise).  Nothing waits for the host:
  * a sequence that cannot be served is left as it was and says so in out_missing.  A page is shared
  * until one of its holders is about to write into it.  Copies of contents are only listed
  * (copy_src[i] -> copy_dst[i], -1 = none): respec_pages_copy carries them out, once per layer.

@@ -25,6 +25,7 @@ constexpr int kPagesPerBlock = 4 * kRankThreads;  // page_refs that a work-group
 constexpr int kFewPages = 4 * kPagesPerBlock;
 constexpr int kFewSequences = 32;             // up to here, and up to kPagesPerBlock pages, a resize is one launch
 constexpr int32_t kKeep = INT32_MIN;          // a page that compaction neither moves nor fills
+constexpr int32_t kMost = 1 << 30;            // pages, entries and moves lie below it: indices and strides are added in 32 bits
 
 struct PageState {
     const int32_t *page_indptr;
@@ -497,6 +498,8 @@ respec_status_t check_state(const char *name, const void *a, const void *b, cons
     if (!a || !b || !c || !d || !e) return fail(RESPEC_ERR_INVALID_ARG, "%s: null pointer argument", name);
     if (B <= 0 || table_len <= 0 || num_pages <= 0)
         return fail(RESPEC_ERR_INVALID_ARG, "%s: sizes must be positive (B=%d page_table_len=%d num_pages=%d)", name, B, table_len, num_pages);
+    if (table_len >= kMost || num_pages >= kMost)
+        return fail(RESPEC_ERR_UNSUPPORTED, "%s: page_table_len and num_pages must be below 2^30 (%d, %d)", name, table_len, num_pages);
     if (!grid_fits(B, kThreads)) return fail(RESPEC_ERR_UNSUPPORTED, "%s: too many sequences (%d)", name, B);
     return RESPEC_OK;
 }
@@ -595,6 +598,9 @@ respec_status_t respec_pages_compact(const int32_t *page_table, const int32_t *p
         return fail(RESPEC_ERR_INVALID_ARG, "pages_compact: null pointer argument");
     if (page_table_len <= 0 || num_pages <= 0 || max_moves <= 0)
         return fail(RESPEC_ERR_INVALID_ARG, "pages_compact: sizes must be positive (page_table_len=%d num_pages=%d max_moves=%d)", page_table_len,
+                    num_pages, max_moves);
+    if (page_table_len >= kMost || num_pages >= kMost || max_moves >= kMost)
+        return fail(RESPEC_ERR_UNSUPPORTED, "pages_compact: page_table_len, num_pages and max_moves must be below 2^30 (%d, %d, %d)", page_table_len,
                     num_pages, max_moves);
     const respec_status_t st = check_workspace("pages_compact", workspace, workspace_bytes, 1, num_pages);
     if (st != RESPEC_OK) return st;
