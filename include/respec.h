@@ -275,9 +275,12 @@ respec_status_t respec_commit_accepted_paged(void *k_pages, void *v_pages, const
  *   q_indptr  [B+1] int32; kv_indptr [B+1] int64
  *   out       [total_q, Hq, D]    dt, contiguous (written)
  *   lse       [total_q, Hq] f32 or NULL (written), as in respec_verify_attention
- *   max_q_per_seq, max_kv_len   host-side upper bounds of R_b and L_b; rows or keys beyond them are
- *             not processed (max_kv_len at most 2^31 - 257).  How the work is cut follows them: close ones are faster
- *   D in {64, 128}; Hq % Hkv == 0; strides multiples of 16 bytes; data pointers 16-byte aligned.
+ *   max_q_per_seq, max_kv_len   host-side upper bounds of R_b and L_b (max_kv_len at most 2^31 - 257).  Rows or keys
+ *             beyond them are not processed: as in respec_verify_attention, the sequence then counts as one of
+ *             max_q_per_seq rows or max_kv_len tokens.  How the work is cut follows them: close ones are faster
+ *   D in {64, 128}; Hq % Hkv == 0; strides multiples of 16 bytes; data pointers 16-byte aligned; tokens of
+ *             K and of V less than 2^24 bytes apart, min(max_q_per_seq, total_q) * Hq / Hkv below 2^30
+ *             (RESPEC_ERR_UNSUPPORTED otherwise).
  *   workspace respec_prompt_attention_workspace_bytes(...) bytes, 256-byte aligned, scratch (nothing
  *             to prepare, nothing survives): calls that overlap need one each, captured ones too.  What is named for
  *             some sizes (at most 130 MiB) is enough for every call of these heads, D and dt whose other sizes
@@ -317,7 +320,8 @@ respec_status_t respec_prompt_attention_paged(const void *q, const void *k_pages
  * outside [0, num_pages) are not written anywhere; the others go where they belong all the same.
  * kv_len is not changed.  Pages that are written must belong to one sequence only (respec_pages_resize
  * sees to that).
- *   Hkv*D*sizeof(element) and the stride in bytes must be multiples of 16, data pointers 16-byte aligned.
+ *   Hkv*D*sizeof(element) and the stride in bytes must be multiples of 16, the former at most 2^24; data
+ *   pointers 16-byte aligned.
  */
 respec_status_t respec_append_paged(const void *k_new, const void *v_new, void *k_pages, void *v_pages,
                                     const int32_t *q_indptr, const int32_t *page_indptr,
@@ -394,6 +398,7 @@ respec_status_t respec_pages_compact(const int32_t *page_table, const int32_t *p
  * respec_pages_copy: page copy_src[i] of both pools to page copy_dst[i], i < n, for the pools of
  * one layer.  Entries with an id outside [0, num_pages) or with copy_src[i] == copy_dst[i] are skipped.
  * The copies run at the same time: no page may be written twice, or be read by one and written by another.
+ *   Hkv*D*sizeof(element) must be a multiple of 16, at most 2^24.
  */
 respec_status_t respec_pages_copy(void *k_pages, void *v_pages, const int32_t *copy_src, const int32_t *copy_dst,
                                   int32_t n, int32_t num_pages, int32_t page_size, int32_t Hkv, int32_t D,
@@ -629,13 +634,15 @@ respec_status_t respec_kd_rows(const void *target_logits, const void *draft_logi
  *   logits    [rows, V], row stride ld elements (>= V)  logits_dt.  Any alignment; rows that start
  *             16-byte aligned are fastest
  *   tokens    [rows] int32
- *   row_temperature [rows] f32 or NULL: one temperature per row instead of `temperature`; one that is
- *             not positive and finite gives NaN
+ *   temperature   from 1e-30 on, finite (RESPEC_ERR_INVALID_ARG otherwise)
+ *   row_temperature [rows] f32 or NULL: one temperature per row instead of `temperature`; one below 1e-30 (0 too,
+ *             the samplers' greedy) or not finite gives NaN in its row
  *   out_entropy [rows] f32 or NULL; out_top_tokens, out_top_logprobs [rows, top_n] or NULL with top_n = 0
  *   top_n <= 64 (RESPEC_ERR_UNSUPPORTED otherwise)
  *   workspace respec_token_logprobs_workspace_bytes(...) bytes, 256-byte aligned, scratch (nothing to
  *             prepare, nothing survives); it does not depend on the number of rows
- * Sums are formed in a fixed order: repeated calls give the same bits.
+ * Log-probabilities and entropy come from differences of logits, so large logits over a low temperature cost them
+ * nothing; the lse is rounded to fp32.  Sums are formed in a fixed order: repeated calls give the same bits.
  */
 size_t respec_token_logprobs_workspace_bytes(int32_t rows, int32_t V, int32_t top_n, respec_dtype_t logits_dt);
 respec_status_t respec_token_logprobs(const void *logits, const int32_t *tokens, const float *row_temperature,
@@ -649,6 +656,8 @@ respec_status_t respec_token_logprobs(const void *logits, const int32_t *tokens,
  *     grad_logits[r, x] = (g ([x = tokens[r]] - p(x)) - h p(x) (log p(x) + H_r)) / T
  * from the lse and entropy that respec_token_logprobs wrote for the same logits, tokens and
  * temperatures.  Rows without a token get zeros (and are not read); a row whose lse is NaN or -inf gets NaN.
+ * p is exp(z - lse) and carries the rounding of the lse, |lse| 2^-24 of p: 5e-6 at |lse| = 80, 1e-3 where logits
+ * of 160 are divided by a temperature of 0.01.
  *   grad_logprob  [rows] f32 or NULL (zeros); grad_entropy [rows] f32 or NULL (zeros; entropy may be
  *                 NULL then); not both NULL
  *   grad_logits   [rows, V] logits_dt, row stride ld_g (written; bf16: rounded to nearest even).  It may be
