@@ -49,7 +49,7 @@ struct PromptParams {
     int64_t total_kv;
     int32_t B, total_q, max_q, max_kv, num_pages, table_len, page_shift;
     int32_t Hq, Hkv, G;
-    int32_t splits, tiles;   // parts of a tile's keys; bound of the row tiles of a KV head
+    int32_t splits;          // parts of a tile's keys
     uint32_t g_mul, g_shift; // of a division by G (by_g)
     uint32_t q_and, q_xor;   // on the bits of q: a negative scale is taken out of it, a zero one makes it zero
     float scale2;            // |sm_scale| * log2(e)
@@ -986,7 +986,6 @@ respec_status_t run(const char *name, PromptParams &p, const void *k, const void
     p.v = static_cast<const char *>(v);
     p.G = p.Hq / p.Hkv;
     p.splits = pl.splits;
-    p.tiles = (int32_t)pl.tiles;
     for (p.g_shift = 0; (1 << p.g_shift) < p.G; ++p.g_shift) {}
     p.g_mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << p.g_shift) - p.G)) / p.G + 1);
     p.g_shift = std::max(1u, p.g_shift);  // (G = 1 divides nothing)
