@@ -365,8 +365,8 @@ __device__ inline int best_of_groups(const Row<BF16> &r, const Deal &deal, int w
     return top;
 }
 
-// One work-group per part of a row.  1,024 rows of 151,936 bf16 logits take 64 us (4.9 TB/s), with 5 alternatives 69: the groups that are read
-// again and the ranks come after the pass.  8 rows with 20 alternatives are 64 parts each and take 9.5 us, latency, and 3.8 for the join.
+// One work-group per part of a row.  1,024 rows of 151,936 bf16 logits take 59 us (5.3 TB/s), with 5 alternatives 69: the groups that are read
+// again and the ranks come after the pass.  8 rows with 20 alternatives are 64 parts each and take 9.5 us, latency, and 3 to 4.5 for the join.
 template <bool BF16, bool TOP>
 __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobParams p) {
     using E = Elem<BF16>;
@@ -631,7 +631,7 @@ template <bool BF16, bool PIECES>
 __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradParams p) {
     using E = Elem<BF16>;
     // The last rows first, which the forward pass read last and left in the cache behind the L2s, and loads and stores that take no
-    // room there: forward and gradient of 2,048 rows of 151,936 bf16 logits take 298 us; 306 with ordinary loads, 314 with the
+    // room there: forward and gradient of 2,048 rows of 151,936 bf16 logits take 300 us; 306 with ordinary loads, 314 with the
     // rows in order as well, 356 with ordinary stores.
     const int row = p.rows - 1 - blockIdx.x / p.blocks_per_row, block = blockIdx.x % p.blocks_per_row;
     const Row<BF16> r(p.logits, row, p.ld, p.V);

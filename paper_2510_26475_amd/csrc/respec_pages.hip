@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kRankThreads) void resize_rank_kernel(ResizeParams 
         if (is_free[i]) p.fresh[rank++] = blockIdx.x * kPagesPerBlock + threadIdx.x * 4 + i;
 }
 
-// One work-group per sequence.  Both launches wait for a few loads that depend on one another: 3.1 and 4.1 us for 288 sequences.
+// One work-group per sequence.  Both launches wait for a few loads that depend on one another: 3.1 and 3.7 us for 288 sequences.
 __global__ __launch_bounds__(kThreads) void resize_apply_kernel(ResizeParams p) {
     __shared__ int lds[kThreads / 64];
     const int b = blockIdx.x, word = p.need[b], begin = p.begin[b];
@@ -248,8 +248,8 @@ __global__ __launch_bounds__(kThreads) void resize_apply_kernel(ResizeParams p) 
     resize_one<kThreads>(p, b, word, is_served(word, begin, n_free), p.fresh + begin, threadIdx.x, []() { __syncthreads(); });
 }
 
-// Few sequences and pages: all of it in one work-group, at the end a wave per sequence.  Replayed from a graph a resize of 8 sequences takes
-// 3.6 us, in two launches 5.6; of 32 sequences 5.9, and 6.7; of 64 7.4, and 6.6.  Enqueued one by one 6.1 and 9.0.
+// Few sequences and pages: all of it in one work-group, at the end a wave per sequence.  Replayed from a graph, a resize of 8 sequences in 4,096 pages
+// takes 4.1 us, in two launches 6.5; of 32 sequences 5.4, and 6.5; of 64 7.3, and 6.4.  Enqueued one by one 7.0 and 9.3.
 __global__ __launch_bounds__(kRankThreads) void resize_few_kernel(ResizeParams p) {
     __shared__ int lds[kRankThreads / 64];
     __shared__ int32_t fresh[kPagesPerBlock];
@@ -447,7 +447,8 @@ struct AppendParams {
 };
 constexpr int kAppendRows = 8;  // rows of a work-group
 
-// Bound by HBM: 4,096 tokens of 8 heads of 128 (33.6 MB read and written) take 8.0 us, 8.2 with two loads in flight.
+// Bound by memory: 4,096 tokens of 8 heads of 128 (33.6 MB read and written) take 7.7 us call after call, when the cache behind the L2s
+// holds them, and 11.5 before an attention that displaces them; two loads in flight instead of eight 2 % more.
 // A row's position follows from the length and the number of rows as they are given, whatever of them is left out: rows past max_q, and
 // those whose position the sequence's pages do not have.
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams p) {

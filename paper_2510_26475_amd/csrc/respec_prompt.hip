@@ -138,8 +138,8 @@ __device__ inline int bits_before(uint64_t mask) {  // set bits of lanes before 
 // The number-th tile of a batch of up to 64 sequences (one per lane), those that see most keys first, in steps of kOrderStep keys:
 // work-groups are given out in order, and a long one among the last would be waited for.  How many tiles see x keys or more is known
 // for every sequence without looking at its tiles, so the step is found by bisection.  (16 packed prompts of 65 to 2,048 tokens at
-// 28/4 heads take 143 us, in the order of the sequences 161; 8 chunks behind up to 8,192 tokens at 40/8 heads 332, and 362; in steps of 64
-// keys 144 and 338.)
+// 28/4 heads take 140 us, in the order of the sequences 160; 8 chunks behind up to 8,192 tokens at 40/8 heads with their append 332,
+// and 348; in steps of 64 keys no different.)
 constexpr int kOrderStep = 256, kInTurn = 32;
 template <bool PAGED, int ROWS>
 __device__ inline bool find_longest(const PromptParams &p, int number, Tile &out, int &tokens, int64_t &first) {
@@ -168,8 +168,8 @@ __device__ inline bool find_longest(const PromptParams &p, int number, Tile &out
     }
     const int more = p.B == 1 ? 0 : reach(over), mine = p.B == 1 ? tiles : reach(x) - more;  // (one sequence: its tiles from the last)
     // Among the tiles of a step one of every sequence in turn: an XCD, which is given every eighth work-group, then meets fewer sequences' keys
-    // at a time than with one sequence after the other (16 prompts of 1,024 tokens at 28/4 heads take 162 us, and 166).  Of many sequences
-    // that is too much for its L2, and one comes after the other (64 of 256 tokens 84 us, in turn 88).
+    // at a time than with one sequence after the other (16 prompts of 1,024 tokens at 28/4 heads take 161 us, and 166).  Of many sequences
+    // that is too much for its L2, and one comes after the other (64 of 256 tokens 82 us, in turn 84).
     int rest = number - (p.B == 1 ? 0 : n_over), turn = 0;
     uint64_t left = __ballot(mine > 0);
     int at;
@@ -194,7 +194,8 @@ __device__ inline bool find_longest(const PromptParams &p, int number, Tile &out
     return true;
 }
 
-// The number-th tile of row tiles, with its sequence's tokens and where they begin.
+// The number-th tile of row tiles, with its sequence's tokens and where they begin.  Batches of more than 64 sequences: one sequence after the
+// other, each from the tile that sees most.
 template <bool PAGED, int ROWS>
 __device__ inline bool find_rows(const PromptParams &p, int number, Tile &out, int &tokens, int64_t &first) {
     if (p.B <= 64) return find_longest<PAGED, ROWS>(p, number, out, tokens, first);
@@ -359,7 +360,7 @@ __device__ inline void finish(const PromptParams &p, const Job &j, const RowOf &
                 if (r.exists) *reinterpret_cast<floatx4 *>(p.part_o + slot * D + d * 32 + 2 * x + 4 * half) = floatx4{o[d][x], o[d][x + 1], o[d][x + 2], o[d][x + 3]};
     } else if constexpr (BF16) {
         // Through LDS, so that whole rows are written, sixteen bytes a lane: the wave's own 32 rows, pieces placed as K's are.  Past the caches,
-        // which K and V fill (32 prompts of 512 tokens at 28/4 heads 103 us, with ordinary stores 107).
+        // which K and V fill (32 prompts of 512 tokens at 28/4 heads 104 us, with ordinary stores 111).
         const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // (no visible key: zero; NaN stays)
         char *const mine = lds + wave * 32 * S::kRowBytes;
 #pragma unroll
@@ -600,7 +601,7 @@ __device__ __attribute__((always_inline)) inline void each(F &&f) {
 // for two steps is enough.  Four waves: two tiles of each and two work-groups per compute unit, K of t+2 and V of t+1, a
 // barrier per step.  The loop is written for as many steps as there are tiles in
 // LDS, so that a tile's place is a constant.
-// One prompt of 16,384 tokens at 16/2 heads of 128 takes 980 us (1.1 PFLOP/s): the matrix pipes are busy 59 % of the cycles, of a clock
+// One prompt of 16,384 tokens at 16/2 heads of 128 takes 970 to 1,020 us by the card (1.1 PFLOP/s): the matrix pipes are busy 59 % of the cycles, of a clock
 // that the power holds at 1.7 GHz.  16 prompts of 65 to 2,048 at 28/4 heads take 140 us: a work-group spends 14,000 of its 44,000
 // cycles on its rows, Q, the first keys and the output, half of it behind the other work-group of its compute unit.
 template <int D, int WAVES, bool PAGED>
@@ -873,10 +874,10 @@ PartBytes part_bytes(size_t slots, int32_t D) {
 // the groups are alike (many keys before the chunk) whole rounds of them, of which half is counted for several sequences, as those
 // are seldom of one length; parts cost a launch and their bytes.  The constants are fitted to 3,200 timings (1 to 64 prompts,
 // chunks of 1 to 4,000 tokens behind 0 to 30,000, six head layouts, D 64 and 128, both forms, 1 to 16 parts): the form picked is on
-// the mean 1.4 % behind the best of its shape.  8 chunks of 512 behind up to 8,192 at 40/8 heads: 337 us with eight waves, 375 with four.
-// Eight waves at 28/4 heads of 128: 8 prompts of 2,048 take 282 us, with four 295; 64 of 128 take 55 us, with four 44.
-// fp32 at 8/2 heads of 64: 4 prompts of 200 tokens take 13 us with four waves on 32 rows, 21 with 128; 32 of them 42 us, and 30.
-// One chunk of 40 tokens behind 8,000: 30 us in 16 parts; 512 behind 16,000, twice: 249 us in 2 parts, 309 in 3.
+// the mean 1.4 % behind the best of its shape.  8 chunks of 512 behind 7,680 at 40/8 heads: 660 us with eight waves, 701 with four.
+// Eight waves at 28/4 heads of 128: 8 prompts of 2,048 take 258 us, with four 272; 64 of 128 take 46 us, with four 37.
+// fp32 at 8/2 heads of 64: 4 prompts of 200 tokens take 12 us with four waves on 32 rows, 17 with 128; 32 of them 39 us, and 28.
+// One chunk of 40 tokens behind 8,000: 30 us in 16 parts, 33 in 8; 512 behind 16,000, twice: 245 us in 2 parts, 306 in 3, 376 whole.
 struct Cost {
     float step, lone, over, base;
 };
