@@ -18,7 +18,9 @@
  * same logits rows (Section 5.3), and respec_solver_pick, the Solver's table look-up (host code).
  * Around the verify step: respec_prompt_attention and respec_append_paged fill the cache before drafting
  * begins, respec_pages_* share, grow, free and move its pages, and respec_token_logprobs records
- * the log-probabilities of the emitted tokens (Algorithm 1), with their gradient.
+ * the log-probabilities of the emitted tokens (Algorithm 1), with their gradient.  respec_norm_rope_append_paged writes
+ * normalised and rotated heads into the cache, which may be one of 8 bits (respec_*_quantised), and
+ * respec_verify_attention_shared reads what the responses of a group share once for all of them.
  *
  * General rules
  *   - Every data pointer is a DEVICE pointer (HIP global memory) unless it says "host".
@@ -59,7 +61,11 @@ typedef enum {
     RESPEC_ERR_HIP = 4          /* the HIP runtime refused a launch                      */
 } respec_status_t;
 
-typedef enum { RESPEC_F32 = 0, RESPEC_BF16 = 1 } respec_dtype_t;
+typedef enum {
+    RESPEC_F32 = 0,
+    RESPEC_BF16 = 1,
+    RESPEC_E4M3 = 2 /* pools of the calls that say so: 8 bits with a scale per token and KV head (respec_norm_rope_append_paged) */
+} respec_dtype_t;
 
 /* Static strings; never NULL. */
 const char *respec_status_string(respec_status_t status);
@@ -403,6 +409,112 @@ respec_status_t respec_pages_compact(const int32_t *page_table, const int32_t *p
 respec_status_t respec_pages_copy(void *k_pages, void *v_pages, const int32_t *copy_src, const int32_t *copy_dst,
                                   int32_t n, int32_t num_pages, int32_t page_size, int32_t Hkv, int32_t D,
                                   respec_dtype_t dt, void *hip_stream);
+
+/*
+ * The heads of Q and K normalised and rotated, K and V written into the pages that the attention reads, in one pass over
+ * a projection's output (what a layer of the target's forward does before the attention of Figure 2).  For every head x of Q and K:
+ *     x' = x / sqrt(mean_d x[d]^2 + eps) * weight[d]                                       (weight NULL: x' = x)
+ *     (x'[a], x'[b]) -> (x'[a] cos t - x'[b] sin t, x'[b] cos t + x'[a] sin t),  t = position * inv_freq[i]
+ * for the pairs i in [0, rotary_dim/2) of its first rotary_dim entries: a = i, b = i + rotary_dim/2, or, interleaved, a = 2i, b = 2i + 1
+ * (inv_freq NULL: no rotation).  V is written as it is.  Everything is computed in fp32, angles in 64 bits, and rounded once.
+ * Row i of sequence b belongs to position kv_len[b]-R_b+i, where K and V go as in respec_append_paged: rows i >= max_q_per_seq are not
+ * processed; rows whose place the sequence's pages do not have write no K and V.  positions [total_q] int32, where not NULL, takes the place
+ * of that number in the rotation (a tree's rows lie at the depths of their nodes), not in where they go.
+ *   q       [total_q, Hq, D], k, v [total_q, Hkv, D]  dt, token strides ld_q, ld_k, ld_v elements (slices of one projection's output)
+ *   q_out   [total_q, Hq, D]  dt, token stride ld_q_out (written).  It may be q itself with its stride.  q and q_out NULL:
+ *           K and V only
+ *   q_weight, k_weight [D] f32 or NULL;  inv_freq [rotary_dim/2] f32 or NULL with rotary_dim = 0
+ *   pool_dt dt, with k_scale and v_scale NULL, or RESPEC_E4M3, a cache of 8 bits: k_pages, v_pages [num_pages, page_size, Hkv, D] hold
+ *           e4m3 codes (4 exponent and 3 mantissa bits, no infinities) and k_scale, v_scale [num_pages, Hkv, page_size] uint8 an exponent
+ *           byte for each token and head; code c under byte e stands for c 2^(e-127), which is a bf16 number exactly.  With top = the largest finite
+ *           |x| of the token's head (of what the formulas give, before any rounding) e is the least byte >= 1 with top <= 448 2^(e-127) and c is x / 2^(e-127)
+ *           rounded to nearest even; what is not finite becomes NaN.
+ *   D in {64, 128}; rotary_dim a multiple of 16 up to D; strides multiples of 16 bytes; q, k, v, q_out, pools and weights
+ *   16-byte aligned; a token's heads at most 2^24 bytes (RESPEC_ERR_UNSUPPORTED otherwise).
+ */
+respec_status_t respec_norm_rope_append_paged(const void *q, const void *k, const void *v, const float *q_weight, const float *k_weight,
+                                              const float *inv_freq, const int32_t *positions, void *q_out, void *k_pages, void *v_pages,
+                                              uint8_t *k_scale, uint8_t *v_scale, const int32_t *q_indptr, const int32_t *page_indptr,
+                                              const int32_t *page_table, const int32_t *kv_len, int32_t B, int32_t total_q, int32_t max_q_per_seq,
+                                              int32_t num_pages, int32_t page_table_len, int32_t page_size, int32_t Hq, int32_t Hkv, int32_t D,
+                                              int32_t rotary_dim, int32_t interleaved, int64_t ld_q, int64_t ld_k, int64_t ld_v, int64_t ld_q_out, float eps,
+                                              respec_dtype_t dt, respec_dtype_t pool_dt, void *hip_stream);
+
+/*
+ * Whole sequences out of a cache of 8 bits: what tokens 0 .. kv_len[b]-1 of sequence b stand for to rows kv_indptr[b] on of k_out and
+ * v_out, the layout that respec_prompt_attention reads (a prompt's next chunk is appended, read back with its earlier tokens and attended).
+ *   k_out, v_out [total_kv, Hkv, D] dt, contiguous, 16-byte aligned (written; bf16 and fp32 are both exact)
+ *   kv_indptr    [B+1] int64, not decreasing: as many tokens as fit between two entries are written; rows of no sequence, those of tokens past
+ *                max_kv_len and those of page ids outside [0, num_pages) are left as they were
+ * Pools, scales, tables and page_size as in respec_norm_rope_append_paged; scales 16-byte aligned.
+ */
+respec_status_t respec_read_paged_quantised(const void *k_pages, const void *v_pages, const uint8_t *k_scale, const uint8_t *v_scale,
+                                            const int32_t *page_indptr, const int32_t *page_table, const int32_t *kv_len, const int64_t *kv_indptr,
+                                            void *k_out, void *v_out, int32_t B, int64_t total_kv, int32_t max_kv_len, int32_t num_pages,
+                                            int32_t page_table_len, int32_t page_size, int32_t Hkv, int32_t D, respec_dtype_t dt, void *hip_stream);
+
+/* respec_commit_accepted_paged and respec_pages_copy for a cache of 8 bits: codes and scales are moved together. */
+respec_status_t respec_commit_accepted_paged_quantised(void *k_pages, void *v_pages, uint8_t *k_scale, uint8_t *v_scale, const int32_t *q_indptr,
+                                                       const int32_t *page_indptr, const int32_t *page_table, int32_t *kv_len, const int32_t *path,
+                                                       int32_t path_stride, const int32_t *num_accepted, int32_t B, int32_t total_q,
+                                                       int32_t max_q_per_seq, int32_t num_pages, int32_t page_table_len, int32_t page_size, int32_t Hkv,
+                                                       int32_t D, void *hip_stream);
+respec_status_t respec_pages_copy_quantised(void *k_pages, void *v_pages, uint8_t *k_scale, uint8_t *v_scale, const int32_t *copy_src,
+                                            const int32_t *copy_dst, int32_t n, int32_t num_pages, int32_t page_size, int32_t Hkv, int32_t D,
+                                            void *hip_stream);
+
+/*
+ * Verify attention of a batch whose sequences share their beginnings: the responses of a rollout group hold the pages of their
+ * prompt together (respec_pages_fork), and these are read once for all of them.  The result is that of respec_verify_attention_paged on
+ * every sequence's own tokens (with a tree_mask: on trees) up to rounding, also where sequences have no rows or no tokens: a row that sees no key
+ * gets zeros and lse = -inf.
+ *   group_indptr [num_groups+1] int32: group g is the sequences group_indptr[g] .. group_indptr[g+1]-1, no sequence in two groups.  Sequences of
+ *                no group are read alone.  NULL with num_groups = 0: no groups
+ *   shared_len   [num_groups] int32: so many tokens at the beginning are the same for all members of the group; they are read from the
+ *                pages of its first one.  Any number: what some member does not hold before its new tokens (kv_len[b]-R_b) counts as its own
+ *   k_pages, v_pages  of pool_dt, which is dt, with k_scale and v_scale NULL, or RESPEC_E4M3 (dt then RESPEC_BF16; as in
+ *                respec_norm_rope_append_paged, bytes 1 to 247): the attention over the bf16 numbers that the codes stand for
+ *   Everything else as in respec_verify_attention_paged; rows of no sequence are left as they were; B <= 65,535,
+ *   max_q_per_seq * Hq / Hkv <= 256 (trees: max_q_per_seq <= 64), total_q * Hq < 2^30 (RESPEC_ERR_UNSUPPORTED otherwise).
+ *   workspace    respec_verify_attention_shared_workspace_bytes(...) bytes, 256-byte aligned, scratch (nothing to prepare): calls that
+ *                overlap need one each, captured ones too
+ * A value of V that is not finite reaches only the rows that see its key.  Repeated calls give the same bits.
+ */
+size_t respec_verify_attention_shared_workspace_bytes(int32_t B, int32_t total_q, int32_t num_groups, int32_t max_q_per_seq, int32_t max_kv_len, int32_t Hq,
+                                                      int32_t Hkv, int32_t D, respec_dtype_t dt);
+respec_status_t respec_verify_attention_shared(const void *q, const void *k_pages, const void *v_pages, const uint8_t *k_scale, const uint8_t *v_scale,
+                                               const int32_t *q_indptr, const int32_t *page_indptr, const int32_t *page_table, const int32_t *kv_len,
+                                               const int32_t *group_indptr, const int32_t *shared_len, const uint64_t *tree_mask, void *out, float *lse,
+                                               int32_t B, int32_t total_q, int32_t num_groups, int32_t num_pages, int32_t page_table_len,
+                                               int32_t page_size, int32_t max_q_per_seq, int32_t max_kv_len, int32_t Hq, int32_t Hkv, int32_t D,
+                                               float sm_scale, respec_dtype_t dt, respec_dtype_t pool_dt, void *workspace, size_t workspace_bytes,
+                                               void *hip_stream);
+
+/*
+ * Another layer of the same forward, as respec_verify_attention_next_layer: `workspace` is the one of an earlier
+ * respec_verify_attention_shared call (or of a call of this function) on the same stream with the same contents of the index arrays and the
+ * same sizes and types, untouched since; the set-up it holds is reused.  Bit-equal to a full call.  With other sizes or types nothing is computed and out
+ * is left as it was.
+ */
+respec_status_t respec_verify_attention_shared_next_layer(const void *q, const void *k_pages, const void *v_pages, const uint8_t *k_scale,
+                                                          const uint8_t *v_scale, const int32_t *q_indptr, const int32_t *page_indptr,
+                                                          const int32_t *page_table, const int32_t *kv_len, const int32_t *group_indptr,
+                                                          const int32_t *shared_len, const uint64_t *tree_mask, void *out, float *lse, int32_t B,
+                                                          int32_t total_q, int32_t num_groups, int32_t num_pages, int32_t page_table_len,
+                                                          int32_t page_size, int32_t max_q_per_seq, int32_t max_kv_len, int32_t Hq, int32_t Hkv, int32_t D,
+                                                          float sm_scale, respec_dtype_t dt, respec_dtype_t pool_dt, void *workspace,
+                                                          size_t workspace_bytes, void *hip_stream);
+
+/*
+ * respec_verify_attention_paged over a cache of 8 bits: respec_verify_attention_shared without groups, with its workspace for num_groups = 0.
+ * Another layer: respec_verify_attention_shared_next_layer with num_groups = 0.
+ */
+respec_status_t respec_verify_attention_paged_quantised(const void *q, const void *k_pages, const void *v_pages, const uint8_t *k_scale,
+                                                        const uint8_t *v_scale, const int32_t *q_indptr, const int32_t *page_indptr,
+                                                        const int32_t *page_table, const int32_t *kv_len, const uint64_t *tree_mask, void *out, float *lse,
+                                                        int32_t B, int32_t total_q, int32_t num_pages, int32_t page_table_len, int32_t page_size,
+                                                        int32_t max_q_per_seq, int32_t max_kv_len, int32_t Hq, int32_t Hkv, int32_t D, float sm_scale,
+                                                        respec_dtype_t dt, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Profiling hook (benchmarks only; not for production callers).  One-shot: the calling

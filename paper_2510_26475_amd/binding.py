@@ -16,6 +16,7 @@ from . import build as _build
 
 RESPEC_F32 = 0
 RESPEC_BF16 = 1
+RESPEC_E4M3 = 2
 
 _lib = None
 
@@ -136,6 +137,14 @@ def load():
             ("respec_pages_fork", c.c_int, [ptr] * 7 + [i32] * 3 + [ptr]),
             ("respec_pages_compact", c.c_int, [ptr] * 7 + [i32] * 3 + [ptr, size, ptr]),
             ("respec_pages_copy", c.c_int, [ptr] * 4 + [i32] * 5 + [c.c_int, ptr]),
+            ("respec_norm_rope_append_paged", c.c_int, [ptr] * 16 + [i32] * 11 + [i64] * 4 + [f32, c.c_int, c.c_int, ptr]),
+            ("respec_read_paged_quantised", c.c_int, [ptr] * 10 + [i32, i64] + [i32] * 6 + [c.c_int, ptr]),
+            ("respec_commit_accepted_paged_quantised", c.c_int, [ptr] * 9 + [i32, ptr] + [i32] * 8 + [ptr]),
+            ("respec_pages_copy_quantised", c.c_int, [ptr] * 6 + [i32] * 5 + [ptr]),
+            ("respec_verify_attention_shared_workspace_bytes", size, [i32] * 8 + [c.c_int]),
+            ("respec_verify_attention_shared", c.c_int, [ptr] * 14 + [i32] * 11 + [f32, c.c_int, c.c_int, ptr, size, ptr]),
+            ("respec_verify_attention_shared_next_layer", c.c_int, [ptr] * 14 + [i32] * 11 + [f32, c.c_int, c.c_int, ptr, size, ptr]),
+            ("respec_verify_attention_paged_quantised", c.c_int, [ptr] * 12 + [i32] * 10 + [f32, c.c_int, ptr, size, ptr]),
             ("respec_token_logprobs_workspace_bytes", size, [i32] * 3 + [c.c_int]),
             ("respec_token_logprobs", c.c_int, [ptr] * 8 + [i32, i32, i64, i32, f32, c.c_int, ptr, size, ptr]),
             ("respec_token_logprobs_grad", c.c_int, [ptr] * 8 + [i32, i32, i64, i64, f32, c.c_int, ptr])):
@@ -165,6 +174,9 @@ EXPORTED_SYMBOLS = [
     "respec_prompt_attention_workspace_bytes", "respec_prompt_attention", "respec_prompt_attention_paged", "respec_append_paged",
     "respec_pages_workspace_bytes", "respec_pages_resize", "respec_pages_fork", "respec_pages_compact", "respec_pages_copy",
     "respec_token_logprobs_workspace_bytes", "respec_token_logprobs", "respec_token_logprobs_grad",
+    "respec_norm_rope_append_paged", "respec_read_paged_quantised", "respec_commit_accepted_paged_quantised", "respec_pages_copy_quantised",
+    "respec_verify_attention_shared_workspace_bytes", "respec_verify_attention_shared", "respec_verify_attention_shared_next_layer",
+    "respec_verify_attention_paged_quantised",
 ]
 
 
@@ -817,6 +829,183 @@ def respec_token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob, grad_
     _check(load().respec_token_logprobs_grad(
         logits.data_ptr(), tokens.data_ptr(), _ptr(row_temperature), lse.data_ptr(), _ptr(entropy), _ptr(grad_logprob),
         _ptr(grad_entropy), grad_logits.data_ptr(), rows, V, ld, ld_g, float(temperature), _dtype_code(logits), _stream_on(index, stream)))
+
+
+_E4M3_TYPES = (torch.float8_e4m3fn, torch.uint8)
+
+
+def _scaled_pools(k_pages, v_pages, k_scale, v_scale):
+    """Shape and type code of pools that may be of 8 bits: these come with scales [num_pages, Hkv, page_size]."""
+    num_pages, page_size, Hkv, D = shape = _pools(k_pages, v_pages)
+    if k_scale is None and v_scale is None:
+        return shape, _dtype_code(k_pages)
+    if k_pages.dtype not in _E4M3_TYPES:
+        raise TypeError("pools with scales must hold e4m3 codes (float8_e4m3fn or uint8)")
+    for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+        if t is None or t.dtype is not torch.uint8 or tuple(t.shape) != (num_pages, Hkv, page_size) or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous uint8 [num_pages, Hkv, page_size]")
+    return shape, RESPEC_E4M3
+
+
+def respec_norm_rope_append_paged(q, k, v, q_weight, k_weight, inv_freq, positions, q_out, k_pages, v_pages, k_scale, v_scale, q_indptr,
+                                  page_indptr, page_table, kv_len, max_q_per_seq, eps, interleaved=False, stream=None):
+    """q, q_out [total_q,Hq,D] (both None: K and V only), k, v [total_q,Hkv,D], each with a token stride of its own; weights [D] and inv_freq
+    [rotary_dim/2] float32 or None, positions [total_q] int32 or None; pools in k's dtype, or e4m3 codes with k_scale and v_scale."""
+    (num_pages, page_size, Hkv, D), pool = _scaled_pools(k_pages, v_pages, k_scale, v_scale)
+    total_q, H, Dk = shape = _three(k, "k")
+    B, dtype, Hq = q_indptr.numel() - 1, k.dtype, Hkv
+    index = _here(k, q, v, q_weight, k_weight, inv_freq, positions, q_out, k_pages, v_pages, k_scale, v_scale, q_indptr, page_indptr, page_table,
+                  kv_len)
+    _ints(B + 1, "q_indptr page_indptr", q_indptr, page_indptr)
+    _ints(B, "kv_len", kv_len)
+    _ints(None, "page_table", page_table)
+    if positions is not None:
+        _ints(total_q, "positions", positions)
+    _floats(D, "q_weight k_weight", q_weight, k_weight)
+    if v.dtype is not dtype or (pool != RESPEC_E4M3 and k_pages.dtype is not dtype):
+        raise TypeError("k, v and pools without scales must share one dtype")
+    if H != Hkv or Dk != D or v.shape != shape:
+        raise ValueError("k and v must be [total_q, Hkv, D]")
+    ld_q = ld_out = 0
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if q is not None:
+        n, Hq, Dq = _three(q, "q")
+        if n != total_q or Dq != D or q_out.shape != q.shape or q.dtype is not dtype or q_out.dtype is not dtype:
+            raise ValueError("q and q_out must be [total_q, Hq, D] in k's dtype")
+        ld_q, ld_out = _token_stride(q, n, Hq, D, "q"), _token_stride(q_out, n, Hq, D, "q_out")
+    rotary = 0
+    if inv_freq is not None:
+        rotary = 2 * inv_freq.numel()
+        _floats(rotary // 2, "inv_freq", inv_freq)
+    _check(load().respec_norm_rope_append_paged(
+        _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq), _ptr(positions), _ptr(q_out), k_pages.data_ptr(),
+        v_pages.data_ptr(), _ptr(k_scale), _ptr(v_scale), q_indptr.data_ptr(), page_indptr.data_ptr(), page_table.data_ptr(), kv_len.data_ptr(),
+        B, total_q, max_q_per_seq, num_pages, page_table.numel(), page_size, Hq, Hkv, D, rotary, int(interleaved), ld_q,
+        _token_stride(k, total_q, H, D, "k"), _token_stride(v, total_q, H, D, "v"), ld_out, float(eps), _dtype_code(k), pool,
+        _stream_on(index, stream)))
+
+
+def _quantised_pools(k_pages, v_pages, k_scale, v_scale):
+    if k_scale is None or v_scale is None:
+        raise ValueError("a cache of 8 bits has k_scale and v_scale")
+    return _scaled_pools(k_pages, v_pages, k_scale, v_scale)[0]
+
+
+def respec_read_paged_quantised(k_pages, v_pages, k_scale, v_scale, page_indptr, page_table, kv_len, kv_indptr, k_out, v_out, max_kv_len, stream=None):
+    """What the tokens of every sequence stand for to rows kv_indptr[b] on of k_out and v_out [total_kv, Hkv, D] (bf16 or float32)."""
+    num_pages, page_size, Hkv, D = _quantised_pools(k_pages, v_pages, k_scale, v_scale)
+    total_kv, H, Dk = shape = _three(k_out, "k_out")
+    B = page_indptr.numel() - 1
+    index = _here(k_pages, v_pages, k_scale, v_scale, page_indptr, page_table, kv_len, kv_indptr, k_out, v_out)
+    _ints(B, "kv_len", kv_len)
+    _ints(None, "page_indptr page_table", page_indptr, page_table)
+    if kv_indptr.dtype is not torch.int64 or kv_indptr.numel() != B + 1 or not kv_indptr.is_contiguous():
+        raise TypeError(f"kv_indptr must be contiguous int64 [{B + 1}]")
+    if H != Hkv or Dk != D or v_out.shape != shape or v_out.dtype is not k_out.dtype or not (k_out.is_contiguous() and v_out.is_contiguous()):
+        raise ValueError("k_out and v_out must be contiguous [total_kv, Hkv, D] of one dtype")
+    _check(load().respec_read_paged_quantised(
+        k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), page_indptr.data_ptr(), page_table.data_ptr(),
+        kv_len.data_ptr(), kv_indptr.data_ptr(), k_out.data_ptr(), v_out.data_ptr(), B, total_kv, max_kv_len, num_pages, page_table.numel(), page_size,
+        Hkv, D, _dtype_code(k_out), _stream_on(index, stream)))
+
+
+def respec_commit_accepted_paged_quantised(k_pages, v_pages, k_scale, v_scale, q_indptr, page_indptr, page_table, kv_len, num_accepted, total_q,
+                                           max_q_per_seq, path=None, stream=None):
+    """respec_commit_accepted_paged for a cache of 8 bits; pools, scales and kv_len are changed in place."""
+    num_pages, page_size, Hkv, D = _quantised_pools(k_pages, v_pages, k_scale, v_scale)
+    B = q_indptr.numel() - 1
+    index = _here(k_pages, v_pages, k_scale, v_scale, q_indptr, page_indptr, page_table, kv_len, num_accepted, path)
+    _ints(B + 1, "q_indptr page_indptr", q_indptr, page_indptr)
+    _ints(B, "kv_len num_accepted", kv_len, num_accepted)
+    _ints(None, "page_table", page_table)
+    stride = 0
+    if path is not None:
+        if path.dim() != 2 or path.shape[0] != B:
+            raise ValueError("path must be [B, stride]")
+        stride = path.shape[1]
+        _ints(None, "path", path)
+    _check(load().respec_commit_accepted_paged_quantised(
+        k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), q_indptr.data_ptr(), page_indptr.data_ptr(),
+        page_table.data_ptr(), kv_len.data_ptr(), _ptr(path), stride, num_accepted.data_ptr(), B, total_q, max_q_per_seq, num_pages,
+        page_table.numel(), page_size, Hkv, D, _stream_on(index, stream)))
+
+
+def respec_pages_copy_quantised(k_pages, v_pages, k_scale, v_scale, copy_src, copy_dst, stream=None):
+    """Pages copy_src[i] -> copy_dst[i] of one layer's codes and scales (-1: none)."""
+    num_pages, page_size, Hkv, D = _quantised_pools(k_pages, v_pages, k_scale, v_scale)
+    index = _here(k_pages, v_pages, k_scale, v_scale, copy_src, copy_dst)
+    _ints(None, "copy_src", copy_src)
+    _ints(copy_src.numel(), "copy_dst", copy_dst)
+    _check(load().respec_pages_copy_quantised(
+        k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), copy_src.numel(),
+        num_pages, page_size, Hkv, D, _stream_on(index, stream)))
+
+
+def respec_verify_attention_shared_workspace_bytes(B, total_q, num_groups, max_q_per_seq, max_kv_len, Hq, Hkv, D, dt) -> int:
+    return int(load().respec_verify_attention_shared_workspace_bytes(B, total_q, num_groups, max_q_per_seq, max_kv_len, Hq, Hkv, D, dt))
+
+
+def respec_verify_attention_shared(q, k_pages, v_pages, k_scale, v_scale, q_indptr, page_indptr, page_table, kv_len, group_indptr, shared_len,
+                                   tree_mask, out, lse, max_q_per_seq, max_kv_len, sm_scale, workspace, stream=None,
+                                   _entry="respec_verify_attention_shared"):
+    """q, out [total_q,Hq,D] contiguous, pools in q's dtype, or e4m3 codes with k_scale and v_scale (q bf16); group_indptr [num_groups+1] and shared_len
+    [num_groups] int32, or both None; tree_mask [total_q] int64 or None."""
+    (num_pages, page_size, Hkv, Dk), pool = _scaled_pools(k_pages, v_pages, k_scale, v_scale)
+    total_q, Hq, D = shape = _three(q, "q")
+    B, dtype = q_indptr.numel() - 1, q.dtype
+    index = _here(q, k_pages, v_pages, k_scale, v_scale, q_indptr, page_indptr, page_table, kv_len, group_indptr, shared_len, tree_mask, out, lse,
+                  workspace)
+    _ints(B + 1, "q_indptr page_indptr", q_indptr, page_indptr)
+    _ints(B, "kv_len", kv_len)
+    _ints(None, "page_table", page_table)
+    if (group_indptr is None) != (shared_len is None):
+        raise ValueError("group_indptr and shared_len go together")
+    groups = 0
+    if shared_len is not None:
+        groups = shared_len.numel()
+        _ints(groups, "shared_len", shared_len)
+        _ints(groups + 1, "group_indptr", group_indptr)
+    if tree_mask is not None and (tree_mask.dtype is not torch.int64 or tree_mask.numel() != total_q or not tree_mask.is_contiguous()):
+        raise TypeError("tree_mask must be contiguous int64 [total_q] (the bits of a uint64 per row)")
+    if out.dtype is not dtype or (pool != RESPEC_E4M3 and k_pages.dtype is not dtype):
+        raise TypeError("q, out and pools without scales must share one dtype")
+    if Dk != D or out.shape != shape or not (out.is_contiguous() and q.is_contiguous()):
+        raise ValueError("q and out must be contiguous [total_q, Hq, D] with the pools' D")
+    _floats(total_q * Hq, "lse", lse)
+    _check(getattr(load(), _entry)(
+        q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scale), _ptr(v_scale), q_indptr.data_ptr(), page_indptr.data_ptr(),
+        page_table.data_ptr(), kv_len.data_ptr(), _ptr(group_indptr), _ptr(shared_len), _ptr(tree_mask), out.data_ptr(), _ptr(lse), B, total_q, groups,
+        num_pages, page_table.numel(), page_size, max_q_per_seq, max_kv_len, Hq, Hkv, D, float(sm_scale), _dtype_code(q), pool, *_room(workspace),
+        _stream_on(index, stream)))
+
+
+def respec_verify_attention_shared_next_layer(*args, **kwargs):
+    """Another layer of the same forward: respec_verify_attention_shared with the set-up that its workspace holds."""
+    respec_verify_attention_shared(*args, **kwargs, _entry="respec_verify_attention_shared_next_layer")
+
+
+def respec_verify_attention_paged_quantised(q, k_pages, v_pages, k_scale, v_scale, q_indptr, page_indptr, page_table, kv_len, out, lse,
+                                            max_q_per_seq, max_kv_len, sm_scale, workspace, tree_mask=None, stream=None):
+    """respec_verify_attention_paged over a cache of 8 bits; the workspace is that of respec_verify_attention_shared without groups."""
+    num_pages, page_size, Hkv, Dk = _quantised_pools(k_pages, v_pages, k_scale, v_scale)
+    total_q, Hq, D = shape = _three(q, "q")
+    B = q_indptr.numel() - 1
+    index = _here(q, k_pages, v_pages, k_scale, v_scale, q_indptr, page_indptr, page_table, kv_len, tree_mask, out, lse, workspace)
+    _ints(B + 1, "q_indptr page_indptr", q_indptr, page_indptr)
+    _ints(B, "kv_len", kv_len)
+    _ints(None, "page_table", page_table)
+    if tree_mask is not None and (tree_mask.dtype is not torch.int64 or tree_mask.numel() != total_q or not tree_mask.is_contiguous()):
+        raise TypeError("tree_mask must be contiguous int64 [total_q] (the bits of a uint64 per row)")
+    if out.dtype is not q.dtype:
+        raise TypeError("q and out must share one dtype")
+    if Dk != D or out.shape != shape or not (out.is_contiguous() and q.is_contiguous()):
+        raise ValueError("q and out must be contiguous [total_q, Hq, D] with the pools' D")
+    _floats(total_q * Hq, "lse", lse)
+    _check(load().respec_verify_attention_paged_quantised(
+        q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), q_indptr.data_ptr(), page_indptr.data_ptr(),
+        page_table.data_ptr(), kv_len.data_ptr(), _ptr(tree_mask), out.data_ptr(), _ptr(lse), B, total_q, num_pages, page_table.numel(), page_size,
+        max_q_per_seq, max_kv_len, Hq, Hkv, D, float(sm_scale), _dtype_code(q), *_room(workspace), _stream_on(index, stream)))
 
 
 def respec_solver_pick(points, active_batch, draft_us_fixed, draft_us_per_seq):

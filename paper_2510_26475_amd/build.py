@@ -16,7 +16,8 @@ INCLUDE = os.path.join(_ROOT, "include")
 LIB_PATH = os.path.join(_HERE, "librespec.so")
 
 SOURCES = ["respec_common.hip", "respec_solver.hip", "respec_validate.hip", "respec_sampler.hip", "respec_tree_sampler.hip", "respec_kd.hip",
-           "respec_attention.hip", "respec_prompt.hip", "respec_pages.hip", "respec_logprobs.hip"]
+           "respec_attention.hip", "respec_prompt.hip", "respec_pages.hip", "respec_logprobs.hip", "respec_cache.hip",
+           "respec_shared.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
@@ -33,7 +34,8 @@ def _inputs():
     files = [os.path.join(CSRC, s) for s in SOURCES]
     files += [os.path.join(CSRC, "respec_common.hpp"), os.path.join(CSRC, "respec_sampler_rows.hpp"),
               os.path.join(CSRC, "respec_sampler_share.hpp"), os.path.join(CSRC, "respec_tree_candidate.hpp"),
-              os.path.join(CSRC, "respec_kd_absent.hpp"), os.path.join(CSRC, "respec_tiles.hpp"), os.path.join(INCLUDE, "respec.h")]
+              os.path.join(CSRC, "respec_kd_absent.hpp"), os.path.join(CSRC, "respec_tiles.hpp"),
+              os.path.join(CSRC, "respec_quantised.hpp"), os.path.join(INCLUDE, "respec.h")]
     return files
 
 
