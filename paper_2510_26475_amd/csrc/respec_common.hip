@@ -56,6 +56,9 @@ void read_knobs_locked() {
     g_knobs.kd_spin = env_long("RESPEC_KD_SPIN");
     g_knobs.prompt_waves = env_long("RESPEC_PROMPT_WAVES");
     g_knobs.prompt_splits = env_long("RESPEC_PROMPT_SPLITS");
+    g_knobs.shared_ranges = env_long("RESPEC_SHARED_RANGES");
+    g_knobs.shared_tiles = env_long("RESPEC_SHARED_TILES");
+    g_knobs.shared_cost = env_long("RESPEC_SHARED_COST");
     g_knobs_read = true;
 }
 

@@ -48,6 +48,9 @@ struct Knobs {
     long kd_spin;           // RESPEC_KD_SPIN: 10 ns ticks that a member's part of a row is waited for
     long prompt_waves;      // RESPEC_PROMPT_WAVES: waves that share a tile of keys in the prompt attention (bf16 4/8, fp32 1/4)
     long prompt_splits;     // RESPEC_PROMPT_SPLITS: parts (1-16) the keys of its row tiles are cut into
+    long shared_ranges;     // RESPEC_SHARED_RANGES: most ranges that either kind of work of the attention over shared pages is cut into
+    long shared_tiles;      // RESPEC_SHARED_TILES: fewest tiles of a sequence's own keys in a range of that attention
+    long shared_cost;       // RESPEC_SHARED_COST: what a work-group's step over a sequence's own keys costs, in percent of one over shared keys
     long get(long Knobs::*field, long fallback) const { return this->*field == kUnset ? fallback : this->*field; }
 };
 Knobs knobs();

@@ -16,6 +16,8 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
+#include <utility>
 
 namespace respec {
 namespace {
@@ -25,6 +27,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -33,10 +37,12 @@ typedef const __attribute__((address_space(4))) int32_t *ConstInts;  // (read th
 
 constexpr float kRescaleSlack = 8.f;  // log2 units
 constexpr int kWorkGroups = 512;      // two for each compute unit
-constexpr int kThreads = 256, kPrepThreads = 1024;
+constexpr int kThreads = 256, kPrepThreads = 512;
+constexpr int kPrepGroups = 8;        // work-groups that share the jobs out, each with a plan of its own
 constexpr int kColumns = 32;          // of a wave
 constexpr int kBlock = 4 * kColumns;  // columns of a work-group over shared keys
-constexpr int kMaxRanges = 4 * kWorkGroups;
+constexpr int kJobs = 4 * kWorkGroups;  // one for each wave, or for the waves that share one
+constexpr int kFewSeqs = 1024, kFewGroups = 256;  // whose plan is made in LDS
 
 struct SeqPlan {
     int64_t base;              // tiles of its own before this sequence's
@@ -48,15 +54,26 @@ struct GroupPlan {
     int64_t base;              // tiles of shared keys before this group's
     int32_t q0, rows, shared, e0;
     int32_t key_tiles, blocks; // tiles of keys, blocks of columns
+    int32_t first, end;        // its sequences
 };
-struct Start {                 // of a range: its place in the flat list
-    int64_t f;
-    int32_t outer, item, tile, block;
+enum Kind { kNone = 0, kShared = 1, kOwn = 2 };
+struct Job {                   // a range: where it begins and all that its work-group (own work: its wave) needs for that
+    uint64_t key;              // of the sizes that the plan was made for
+    int32_t kind, range, tiles;
+    int32_t outer, item, tile, block, pad;
+    SeqPlan s;
+    GroupPlan g;
+};
+// A flat list of `total` tiles cut into n even ranges: the first `more` of them have a tile more than the others.
+struct Cut {
+    int64_t total, each;
+    int32_t n, more;
 };
 struct Totals {
-    int64_t own, shared;       // tiles of an outer step of own work; of a head of shared work
-    int32_t shared_wgs, shared_ranges, own_ranges, pad;
-    uint64_t key;              // of the sizes that the plan was made for
+    Cut own, shared;
+    int64_t own_step, shared_step;  // tiles of an outer step of own work; of a head of shared work
+    int32_t shared_wgs, pad;
+    uint64_t key;                   // of the sizes that the plan was made for
 };
 
 struct SharedParams {
@@ -74,13 +91,15 @@ struct SharedParams {
     uint32_t q_and, q_xor;                  // on the bits of q: a negative scale is taken out of it, a zero one makes it zero
     float scale2;                           // |sm_scale| * log2(e)
     float shared_cost, own_cost;            // of a work-group's tile, in the same unit
+    int32_t max_ranges, min_tiles;
     uint64_t key;
     SeqPlan *seq;
     GroupPlan *grp;
-    Start *own_start, *shared_start;
+    Job *jobs;
     Totals *totals;
-    float *own_o, *own_ml, *shared_o, *shared_ml;                  // parts of ranges' ends
-    float *own_whole_o, *own_whole_ml, *shared_whole_o, *shared_whole_ml;  // [total_q * Hq]: parts that are a row's only one of their kind
+    // Parts of ranges' ends, and those that are a row's only one of their kind ([total_q * Hq]): outputs, and pairs of maximum and sum.
+    char *own_o, *shared_o, *own_whole_o, *shared_whole_o;
+    float *own_ml, *shared_ml, *own_whole_ml, *shared_whole_ml;
 };
 
 // x / G by a product: with s = ceil(log2 G) and g_mul = floor(2^32 (2^s - G) / G) + 1 this is exact for every x below 2^32.
@@ -103,7 +122,8 @@ struct Shape {
     static constexpr int kOwnKeys = 32, kOwnLoads = kOwnKeys / kLoadKeys, kOwnBytes = 2 * kOwnKeys * kRowBytes;
     static constexpr int kSharedKeys = kHalf ? 64 : 32, kWaveKeys = kSharedKeys / 4;
     static constexpr int kSharedLoads = kWaveKeys / kLoadKeys, kSharedBytes = 2 * kSharedKeys * kRowBytes;
-    static constexpr int kLdsBytes = 4 * kOwnBytes > 2 * kSharedBytes ? 4 * kOwnBytes : 2 * kSharedBytes;
+    static constexpr int kPlaces = kHalf ? 5 : 4;                 // for K or V of a tile of shared keys in LDS: three (two) of K, two of V
+    static constexpr int kLdsBytes = 4 * kOwnBytes > kPlaces * kSharedBytes / 2 ? 4 * kOwnBytes : kPlaces * kSharedBytes / 2;
     static_assert(kSharedLoads >= 1 && 16 % kLoadKeys == 0, "a wave's load lies in one page");
 };
 
@@ -135,23 +155,52 @@ __device__ inline void wave_sync() {  // (a wave's LDS operations run in order: 
 }
 
 // ------------------------------------------------------------------------------------------ the plan
-__device__ inline int64_t block_scan64(int64_t x, int64_t &total, int64_t *lds /* [16] */) {  // exclusive
+__device__ __attribute__((always_inline)) inline int64_t begin_of(const Cut &c, int r) { return r * c.each + min(r, c.more); }
+// a / b for a below 2^52: the quotient in floating point is off by one at most.
+__device__ inline int64_t quotient(int64_t a, int64_t b) {
+    if ((a | b) >> 31 == 0) return (uint32_t)a / (uint32_t)b;
+    int64_t x = (int64_t)((double)a / (double)b);
+    x -= x * b > a;
+    return x + ((x + 1) * b <= a);
+}
+__device__ inline Cut make_cut(int64_t total, int ranges) {
+    Cut c{};
+    c.total = total;
+    c.n = (int)min(total, (int64_t)ranges);
+    c.each = c.n == 0 ? 0 : quotient(total, c.n);
+    c.more = c.n == 0 ? 0 : (int)(total - c.each * c.n);
+    return c;
+}
+__device__ inline int range_of(const Cut &c, int64_t f) {  // the range that tile f lies in
+    const int64_t longer = c.more * (c.each + 1);
+    return (int)(f < longer ? quotient(f, c.each + 1) : c.more + quotient(f - longer, c.each));
+}
+
+// Exclusive sums over the threads of two numbers below 2^31, in one go: each as 13 low bits and the rest, whose sums over the threads fit 32 bits.
+__device__ inline void block_scan(int x, int y, int64_t &x_before, int64_t &y_before, int64_t &x_all, int64_t &y_all, int (*lds)[4]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t sum = x;
-    for (int step = 1; step < 64; step *= 2) {
-        const int64_t y = __shfl_up(sum, step);
-        if (lane >= step) sum += y;
-    }
-    if (lane == 63) lds[wave] = sum;
+    const int v[4] = {x & 8191, x >> 13, y & 8191, y >> 13};
+    int sum[4], all[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = wave_scan_add(v[i]);
+    if (lane == 63)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lds[wave][i] = sum[i];
     __syncthreads();
-    int64_t before = 0;
-    total = 0;
-    for (int w = 0; w < kPrepThreads / 64; ++w) {
-        before += w < wave ? lds[w] : 0;
-        total += lds[w];
-    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] -= v[i];
+#pragma unroll
+    for (int w = 0; w < kPrepThreads / 64; ++w)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            sum[i] += w < wave ? lds[w][i] : 0;
+            all[i] += lds[w][i];
+        }
     __syncthreads();
-    return before + sum - x;
+    x_before = sum[0] + ((int64_t)sum[1] << 13);
+    y_before = sum[2] + ((int64_t)sum[3] << 13);
+    x_all = all[0] + ((int64_t)all[1] << 13);
+    y_all = all[2] + ((int64_t)all[3] << 13);
 }
 
 // The place of `f` in the flat list: the last item whose base is not past it.
@@ -166,106 +215,157 @@ __device__ inline int find_item(const Item *items, int n, int64_t f) {
     return at;
 }
 
-// One work-group reads the index arrays and writes what every other one needs: what each sequence and group has to do, and where the ranges begin.
-template <int SHARED_KEYS>
+template <typename T>
+__device__ inline void copy_plan(T &to, const T &from) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 8); ++i) reinterpret_cast<uint64_t *>(&to)[i] = reinterpret_cast<const uint64_t *>(&from)[i];
+}
+
+// What each sequence and group has to do, and where the ranges begin.  Up to kFewSeqs sequences every work-group makes the plan for itself, in LDS, the first
+// one writes it down and all share the jobs out; for more there is one work-group.
+template <int SHARED_KEYS, bool FEW>
 __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams p) {
-    __shared__ int64_t lds[16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ int lds[kPrepThreads / 64][4];
+    __shared__ SeqPlan lds_seq[FEW ? kFewSeqs : 1];
+    __shared__ GroupPlan lds_grp[FEW ? kFewGroups : 1];
+    SeqPlan *const seq = FEW ? lds_seq : p.seq;
+    GroupPlan *const grp = FEW ? lds_grp : p.grp;
     for (int b = threadIdx.x; b < p.B; b += kPrepThreads) {
         SeqPlan s{};
-        s.q0 = max(0, min(p.q_indptr[b], p.total_q));
-        s.R = max(0, min(min(p.q_indptr[b + 1], p.total_q) - s.q0, p.max_q));
-        s.e0 = max(0, min(p.page_indptr[b], p.table_len));
-        const int64_t held = max(0, min(p.page_indptr[b + 1], p.table_len) - s.e0);
-        s.L = (int)max((int64_t)0, min(min((int64_t)p.kv_len[b], held << p.page_shift), (int64_t)p.max_kv));
+        const int q0 = p.q_indptr[b], q1 = p.q_indptr[b + 1], e0 = p.page_indptr[b], e1 = p.page_indptr[b + 1], length = p.kv_len[b];
+        s.q0 = max(0, min(q0, p.total_q));
+        s.R = max(0, min(min(q1, p.total_q) - s.q0, p.max_q));
+        s.e0 = max(0, min(e0, p.table_len));
+        const int64_t held = max(0, min(e1, p.table_len) - s.e0);
+        s.L = (int)max((int64_t)0, min(min((int64_t)length, held << p.page_shift), (int64_t)p.max_kv));
         s.group = -1;
-        p.seq[b] = s;
+        seq[b] = s;
     }
     __syncthreads();
-    for (int g = wave; g < p.groups; g += kPrepThreads / 64) {  // a wave per group: what all its members hold before their new tokens
+    // A group shares what all its members hold before their new tokens.
+    for (int g = threadIdx.x; g < p.groups; g += kPrepThreads) {
         const int first = max(0, min(p.group_indptr[g], p.B)), end = max(first, min(p.group_indptr[g + 1], p.B));
-        int shared = end - first < 2 ? 0 : p.shared_len[g];
-        for (int b = first + lane; b < end; b += 64) shared = min(shared, p.seq[b].L - p.seq[b].R);
-        for (int step = 1; step < 64; step *= 2) shared = min(shared, __shfl_xor(shared, step));
-        shared = max(0, shared);
         GroupPlan t{};
+        t.first = first;
+        t.end = end;
+        t.shared = end - first < 2 ? 0 : max(0, p.shared_len[g]);
+        grp[g] = t;
+    }
+    __syncthreads();
+    auto group_of = [&](int b) __attribute__((always_inline)) {  // the last one that begins at or before b, if b is in it
+        int at = 0;
+        for (int end = p.groups; end - at > 1;) {
+            const int mid = (at + end) / 2;
+            if (grp[mid].first <= b) at = mid;
+            else end = mid;
+        }
+        return p.groups > 0 && grp[at].first <= b && b < grp[at].end ? at : -1;
+    };
+    for (int b = threadIdx.x; b < p.B && p.groups > 0; b += kPrepThreads) {
+        const int g = group_of(b);
+        seq[b].group = g;
+        if (g >= 0) __hip_atomic_fetch_min(&grp[g].shared, max(0, seq[b].L - seq[b].R), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    }
+    __syncthreads();
+    for (int g = threadIdx.x; g < p.groups; g += kPrepThreads) {
+        const int shared = __hip_atomic_load(&grp[g].shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP), first = grp[g].first, end = grp[g].end;
+        GroupPlan t{};
+        t.first = first;
+        t.end = end;
         if (shared > 0) {
-            t.q0 = p.seq[first].q0;
-            t.rows = max(0, p.seq[end - 1].q0 + p.seq[end - 1].R - t.q0);
-            t.e0 = p.seq[first].e0;
+            t.q0 = seq[first].q0;
+            t.rows = max(0, seq[end - 1].q0 + seq[end - 1].R - t.q0);
+            t.e0 = seq[first].e0;
             t.shared = t.rows > 0 ? shared : 0;
             t.key_tiles = (t.shared + SHARED_KEYS - 1) / SHARED_KEYS;
             t.blocks = (int)(((int64_t)t.rows * p.G + kBlock - 1) / kBlock);
         }
-        if (lane == 0) p.grp[g] = t;
-        if (t.shared > 0)
-            for (int b = first + lane; b < end; b += 64) {
-                p.seq[b].shared = t.shared;
-                p.seq[b].group = g;
-            }
+        grp[g] = t;
     }
     __syncthreads();
-    int64_t own = 0, shared = 0, total;
-    for (int b0 = 0; b0 < p.B; b0 += kPrepThreads) {
-        const int b = b0 + threadIdx.x;
-        int tiles = 0;
-        if (b < p.B) {
-            const SeqPlan s = p.seq[b];
+    int64_t own = 0, shared = 0;
+    for (int i0 = 0; i0 < max(p.B, p.groups); i0 += kPrepThreads) {
+        const int i = i0 + threadIdx.x;
+        int tiles = 0, blocks = 0;
+        if (i < p.B) {
+            SeqPlan s = seq[i];
+            s.shared = s.group < 0 ? 0 : grp[s.group].shared;
+            seq[i].shared = s.shared;
             if (s.R > 0 && s.L > s.shared) tiles = (int)(((int64_t)s.L + 31) / 32) - s.shared / 32;
         }
-        const int64_t base = own + block_scan64(tiles, total, lds);
-        if (b < p.B) {
-            p.seq[b].base = base;
-            p.seq[b].tiles = tiles;
+        if (i < p.groups) blocks = grp[i].key_tiles * grp[i].blocks;
+        int64_t own_before, shared_before, own_more, shared_more;
+        block_scan(tiles, blocks, own_before, shared_before, own_more, shared_more, lds);
+        if (i < p.B) {
+            seq[i].base = own + own_before;
+            seq[i].tiles = tiles;
         }
-        own += total;
+        if (i < p.groups) grp[i].base = shared + shared_before;
+        own += own_more;
+        shared += shared_more;
     }
-    for (int g0 = 0; g0 < p.groups; g0 += kPrepThreads) {
-        const int g = g0 + threadIdx.x;
-        const int64_t n = g < p.groups ? (int64_t)p.grp[g].key_tiles * p.grp[g].blocks : 0;
-        const int64_t base = shared + block_scan64(n, total, lds);
-        if (g < p.groups) p.grp[g].base = base;
-        shared += total;
-    }
-    // Work-groups for each kind by what its tiles cost, whole eights of them (the XCDs take turns), at least a few tiles to a range.
-    const int64_t all_own = own * p.outer, all_shared = shared * p.Hkv;
-    const float cost_s = (float)all_shared * p.shared_cost, cost_o = (float)all_own / p.parts_wg * p.own_cost;
+    // Work-groups for each kind by what its tiles cost, whole eights of them (the XCDs take turns).
     Totals t{};
-    t.own = own;
-    t.shared = shared;
+    t.own_step = own;
+    t.shared_step = shared;
+    const int64_t all_own = own * p.outer, all_shared = shared * p.Hkv;
     if (all_shared > 0) {
+        const float cost_s = (float)all_shared * p.shared_cost, cost_o = (float)all_own / p.parts_wg * p.own_cost;
         const int even = (int)(kWorkGroups / 8 * (cost_s / (cost_s + cost_o)) + 0.5f) * 8;
         t.shared_wgs = all_own > 0 ? max(8, min(even, kWorkGroups - 8)) : kWorkGroups;
-        t.shared_ranges = (int)min((int64_t)t.shared_wgs, (all_shared + 1) / 2);
     }
-    t.own_ranges = (int)min((int64_t)(kWorkGroups - t.shared_wgs) * p.parts_wg, (all_own + 3) / 4);
+    t.shared = make_cut(all_shared, min(t.shared_wgs, p.max_ranges));
+    // (at least a few tiles to a range: parts have to be joined)
+    t.own = make_cut(all_own, (int)min((int64_t)min((kWorkGroups - t.shared_wgs) * p.parts_wg, p.max_ranges), (all_own + p.min_tiles - 1) / p.min_tiles));
     t.key = p.key;
-    if (threadIdx.x == 0) *p.totals = t;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.totals = t;
     __syncthreads();
-    for (int r = threadIdx.x; r <= t.own_ranges; r += kPrepThreads) {
-        Start s{};
-        s.f = t.own_ranges == 0 ? 0 : (int64_t)(((__int128)all_own * r) / t.own_ranges);
-        if (r < t.own_ranges) {
-            s.outer = (int)(s.f / own);
-            const int64_t rest = s.f - s.outer * own;
-            s.item = find_item(p.seq, p.B, rest);
-            s.tile = (int)(rest - p.seq[s.item].base);
+    for (int j = blockIdx.x * kPrepThreads + threadIdx.x; j < kWorkGroups * p.parts_wg; j += gridDim.x * kPrepThreads) {
+        const int wg = j / p.parts_wg;
+        Job &job = p.jobs[wg * 4 + j - wg * p.parts_wg];
+        int kind = kNone;
+        if (wg < t.shared_wgs) {
+            // consecutive ranges, which read the same keys for other columns, on one XCD (work-groups go to the XCDs in turn)
+            const int r = wg % 8 * (t.shared_wgs / 8) + wg / 8;
+            if (r < t.shared.n) {
+                const int64_t f = begin_of(t.shared, r);
+                kind = kShared;
+                job.range = r;
+                job.tiles = (int)(begin_of(t.shared, r + 1) - f);
+                const int outer = (int)quotient(f, shared);
+                const int64_t rest = f - outer * shared;
+                const int item = find_item(grp, p.groups, rest);
+                job.outer = outer;
+                const int key_tiles = grp[item].key_tiles;
+                const int64_t in = rest - grp[item].base;
+                const int block = (int)quotient(in, key_tiles);
+                job.item = item;
+                job.block = block;
+                job.tile = (int)(in - (int64_t)block * key_tiles);
+                copy_plan(job.g, grp[item]);
+            }
+        } else {
+            const int r = j - t.shared_wgs * p.parts_wg;
+            if (r < t.own.n) {
+                const int64_t f = begin_of(t.own, r);
+                kind = kOwn;
+                job.range = r;
+                job.tiles = (int)(begin_of(t.own, r + 1) - f);
+                const int outer = (int)quotient(f, own);
+                const int64_t rest = f - outer * own;
+                const int item = find_item(seq, p.B, rest);
+                job.outer = outer;
+                job.item = item;
+                job.tile = (int)(rest - seq[item].base);
+                copy_plan(job.s, seq[item]);
+            }
         }
-        p.own_start[r] = s;
+        job.kind = kind;
+        job.key = p.key;
     }
-    for (int r = threadIdx.x; r <= t.shared_ranges; r += kPrepThreads) {
-        Start s{};
-        s.f = t.shared_ranges == 0 ? 0 : (int64_t)(((__int128)all_shared * r) / t.shared_ranges);
-        if (r < t.shared_ranges) {
-            s.outer = (int)(s.f / shared);
-            const int64_t rest = s.f - s.outer * shared;
-            s.item = find_item(p.grp, p.groups, rest);
-            const GroupPlan g = p.grp[s.item];
-            const int64_t in = rest - g.base;
-            s.block = (int)(in / g.key_tiles);
-            s.tile = (int)(in - (int64_t)s.block * g.key_tiles);
-        }
-        p.shared_start[r] = s;
+    if (FEW && blockIdx.x == 0) {
+        for (int b = threadIdx.x; b < p.B; b += kPrepThreads) copy_plan(p.seq[b], seq[b]);
+        for (int g = threadIdx.x; g < p.groups; g += kPrepThreads) copy_plan(p.grp[g], grp[g]);
     }
 }
 
@@ -289,8 +389,12 @@ struct State {  // of a wave's 32 columns
 #pragma unroll
         for (int x = 0; x < S::kPieces / 2; ++x) {
             qf[x] = *reinterpret_cast<const u32x4 *>(from + x * 32);
-            for (int w = 0; w < 4; ++w) qf[x][w] = (qf[x][w] & p.q_and) ^ p.q_xor;
         }
+    }
+    __device__ void sign_q(const SharedParams &p) {  // (apart: the loads are not waited for where they are requested)
+#pragma unroll
+        for (int x = 0; x < S::kPieces / 2; ++x)
+            for (int w = 0; w < 4; ++w) qf[x][w] = (qf[x][w] & p.q_and) ^ p.q_xor;
     }
 };
 
@@ -299,19 +403,29 @@ template <Pool POOL, int D, int NB, typename Mask>
 __device__ __attribute__((always_inline)) inline void attend(const SharedParams &p, State<POOL, D> &st, const char *lds, int k, int v, int half, int col, Mask &&mask) {
     using S = Shape<POOL, D>;
     floatx16 s[NB];
+    // The place of a piece within its row is an exclusive or, so the x-th pair of pieces of K lies at k_at ^ 32 x and the d-th tile of V at v_at ^ 64 d.
+    int k_at = k + col * S::kRowBytes + k_piece<S::kHalf, D>(col, half) * 16;
+    asm volatile("" : "+v"(k_at));  // (the addresses that follow from it would not fit beside the tiles in flight)
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
         for (int x = 0; x < 16; ++x) s[b][x] = 0.f;
+        floatx16 other = s[b];  // (a second chain of products: a wave by itself waits for each)
 #pragma unroll
         for (int x = 0; x < S::kPieces / 2; ++x) {
-            const u32x4 a = *reinterpret_cast<const u32x4 *>(lds + k + (b * 32 + col) * S::kRowBytes + k_piece<S::kHalf, D>(col, 2 * x + half) * 16);
+            const u32x4 a = *reinterpret_cast<const u32x4 *>(lds + (k_at ^ (32 * x)) + b * 32 * S::kRowBytes);
             if constexpr (S::kHalf) {
-                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, st.qf[x]), s[b], 0, 0, 0);
+                floatx16 &to = x % 2 == 0 ? s[b] : other;
+                to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, st.qf[x]), to, 0, 0, 0);
             } else {
 #pragma unroll
-                for (int y = 0; y < 4; ++y) s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[y]), __uint_as_float(st.qf[x][y]), s[b], 0, 0, 0);
+                for (int y = 0; y < 4; ++y) {
+                    floatx16 &to = y % 2 == 0 ? s[b] : other;
+                    to = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[y]), __uint_as_float(st.qf[x][y]), to, 0, 0, 0);
+                }
             }
         }
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s[b][x] += other[x];
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) mask(s[b], b);
@@ -341,7 +455,8 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams 
     if constexpr (S::kHalf) {
         // V by transposing reads: sixteen lanes address four keys by sixteen d and receive one d of the four keys each.
         const int lane = half * 32 + col, i16 = lane & 15, v_key = half * 4 + (i16 >> 2), d0 = ((lane & 16) + 4 * (i16 & 3)) * 2;
-        const int v_at = v + v_key * S::kRowBytes + v_piece<true, D>(v_key, d0 >> 4) * 16 + (d0 & 15);
+        int v_at = v + v_key * S::kRowBytes + v_piece<true, D>(v_key, d0 >> 4) * 16 + (d0 & 15);
+        asm volatile("" : "+v"(v_at));
 #pragma unroll
         for (int g = 0; g < 2 * NB; ++g) {  // sixteen keys at a time: slot j is key 8 (j / 4) + 4 half + j % 4 of them; their probabilities rounded to bf16
             u32x4 pf;
@@ -376,13 +491,15 @@ enum Put { kAll = 0, kCut = 1, kSift = 2 };
 template <Pool POOL, int D, int LOADS>
 struct Mover {
     using S = Shape<POOL, D>;
+    static constexpr int kKeys = LOADS * S::kLoadKeys;  // 32 or fewer
     u32x4 k[LOADS], v[LOADS];
-    uint32_t ks[POOL == kE4m3 ? LOADS : 1], vs[POOL == kE4m3 ? LOADS : 1];
+    uint32_t scale;  // of K of key `lane`, of V of key `lane` - kKeys (and again past these)
     // Runs of `per_run` loads from key n0 on (a multiple of sixteen, or eight behind one), head h; the sequence's entries begin at e0, its last key is `last`.
     template <bool NT>
     __device__ __attribute__((always_inline)) inline void load(const SharedParams &p, int e0, int h, int n0, int last, int lane) {
         constexpr int kRun = (16 / S::kLoadKeys) < LOADS ? 16 / S::kLoadKeys : LOADS;
         const ConstInts table = (ConstInts)p.page_table;
+        const int scale_key = lane % kKeys;
         const int my_key = lane / S::kPoolPieces;
         const uint32_t piece = (uint32_t)(lane % S::kPoolPieces) * 16, token = (uint32_t)p.Hkv * D * S::kPoolSize;
 #pragma unroll
@@ -399,11 +516,10 @@ struct Mover {
                 const u32x4 *a = reinterpret_cast<const u32x4 *>(kp + off), *b = reinterpret_cast<const u32x4 *>(vp + off);
                 k[i] = NT ? __builtin_nontemporal_load(a) : *a;
                 v[i] = NT ? __builtin_nontemporal_load(b) : *b;
-                if constexpr (POOL == kE4m3) {
-                    const int64_t at = ((page * p.Hkv + h) << p.page_shift) + slot + key;
-                    ks[i] = p.k_scale[at];
-                    vs[i] = p.v_scale[at];
-                }
+            }
+            if constexpr (POOL == kE4m3) {
+                const int64_t at = ((page * p.Hkv + h) << p.page_shift) + slot;
+                if (scale_key / 16 == run || kKeys <= 16) scale = (lane / kKeys % 2 ? p.v_scale : p.k_scale)[at + min(scale_key % 16, left)];
             }
         }
     }
@@ -411,15 +527,18 @@ struct Mover {
     // carry a value of V that is not finite to it all the same, so such values count as zero here; they are added at the end to the rows that see them.
     template <Put SIFT>
     __device__ __attribute__((always_inline)) inline bool put(char *kt, char *vt, int key0, int lane, int n0, int begin, int end) {
-        const int my_key = lane / S::kPoolPieces, piece = lane % S::kPoolPieces;
+        constexpr int kOut = POOL == kE4m3 ? 2 : 1;  // pieces that a loaded one becomes
+        asm volatile("" : "+v"(lane));               // (as in attend)
+        const int my_key = lane / S::kPoolPieces, piece = lane % S::kPoolPieces * kOut, row = (key0 + my_key) * S::kRowBytes;
+        // (kLoadKeys keys on, the place of a piece of K differs by an exclusive or and that of V not at all)
+        const int k_at = row + k_piece<S::kHalf, D>(key0 + my_key, piece) * 16, v_at = row + v_piece<S::kHalf, D>(my_key, piece) * 16;
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int key = key0 + i * S::kLoadKeys + my_key;
-            constexpr int kOut = POOL == kE4m3 ? 2 : 1;
             u32x4 a[kOut], b[kOut];
             if constexpr (POOL == kE4m3) {
-                const float sk = scale_of((int)ks[i]), sv = scale_of((int)vs[i]);
+                const int of = i * S::kLoadKeys + my_key;
+                const float sk = scale_of(__shfl((int)scale, of)), sv = scale_of(__shfl((int)scale, of + kKeys));
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     uint32_t lo, hi;
@@ -448,172 +567,635 @@ struct Mover {
             }
 #pragma unroll
             for (int y = 0; y < kOut; ++y) {
-                *reinterpret_cast<u32x4 *>(kt + key * S::kRowBytes + k_piece<S::kHalf, D>(key, piece * kOut + y) * 16) = a[y];
-                *reinterpret_cast<u32x4 *>(vt + key * S::kRowBytes + v_piece<S::kHalf, D>(key, piece * kOut + y) * 16) = b[y];
+                constexpr int kStep = S::kLoadKeys * S::kRowBytes;
+                *reinterpret_cast<u32x4 *>(kt + (k_at ^ (k_piece<S::kHalf, D>(i * S::kLoadKeys, y) * 16)) + i * kStep) = a[y];
+                *reinterpret_cast<u32x4 *>(vt + (v_at ^ (16 * y)) + i * kStep) = b[y];
             }
         }
         return bad;
     }
 };
 
-// A wave's columns as a part: unnormalised output, maximum and sum.  `o`, `ml`: of the lane's column.
-template <Pool POOL, int D>
-__device__ inline void write_part(const State<POOL, D> &st, float l, float *o, float *ml, bool exists, int half) {
-    if (!exists) return;
-    if (half == 0) *reinterpret_cast<floatx2 *>(ml) = floatx2{st.m, l};
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int x = 0; x < 16; x += 4)
-            *reinterpret_cast<floatx4 *>(o + d * 32 + 2 * x + 4 * half) = floatx4{st.o[d][x], st.o[d][x + 1], st.o[d][x + 2], st.o[d][x + 3]};
-}
-
-// ------------------------------------------------------------------------------------------ keys that a group shares
-// Every wave has 32 of the work-group's 128 columns; the four stage a tile of keys together, into one of two places in LDS while the other is read.
-template <Pool POOL, int D>
-__device__ __attribute__((always_inline)) inline void shared_work(const SharedParams &p, char *lds, int r) {
+// A wave's accumulators times `factor` as rows of D, in bf16 (OUT) or in fp16 (parts), through LDS so that whole rows are written: COLS columns at a
+// time, the rows' pieces placed as K's are.  to(c): where column c goes, or nullptr.
+template <Pool POOL, int D, int COLS, bool OUT, typename To>
+__device__ __attribute__((always_inline)) inline void write_rows(const State<POOL, D> &st, float factor, char *area, int half, int col, To &&to) {
     using S = Shape<POOL, D>;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int half = lane >> 5, col = lane & 31;
-    Start at = p.shared_start[r];
-    const int64_t f0 = at.f, f1 = p.shared_start[r + 1].f;
-    if (f0 >= f1) return;
-    GroupPlan g = p.grp[at.item];
-    State<POOL, D> st;
-    Mover<POOL, D, S::kSharedLoads> mover;
-    auto fetch = [&]() __attribute__((always_inline)) {
-        mover.template load<false>(p, g.e0, at.outer, at.tile * S::kSharedKeys + wave * S::kWaveKeys, g.shared - 1, lane);
-    };
-    auto put = [&](int place) __attribute__((always_inline)) {
-        const int n0 = at.tile * S::kSharedKeys;
-        char *const kt = lds + place * S::kSharedBytes, *const vt = kt + S::kSharedBytes / 2;
-        // (all rows see all keys: what is not finite goes where it belongs, only what lies past the keys is left out)
-        if (n0 + S::kSharedKeys <= g.shared) mover.template put<kAll>(kt, vt, wave * S::kWaveKeys, lane, 0, 0, 0);
-        else mover.template put<kCut>(kt, vt, wave * S::kWaveKeys, lane, n0 + wave * S::kWaveKeys, 0, g.shared);
-    };
-    fetch();
-    put(0);
-    int place = 0;
-    bool fresh = true, first = true;
-    int64_t row = 0;
-    int head = 0, column = 0;
-    bool exists = false;
-    for (int64_t f = f0; f < f1; ++f) {
-        const Start now = at;
-        const GroupPlan gn = g;
-        if (fresh) {
-            column = now.block * kBlock + wave * kColumns + col;
-            exists = column < gn.rows * p.G;
-            const int c = min(column, gn.rows * p.G - 1), i = by_g(p, c);
-            row = gn.q0 + i;
-            head = now.outer * p.G + c - i * p.G;
-            st.clear();
-            st.load_q(p, row, head, half);
-            fresh = false;
-        }
-        if (++at.tile == g.key_tiles) {  // the next tile's place
-            at.tile = 0;
-            if (++at.block == g.blocks) {
-                at.block = 0;
-                if (f + 1 < f1) {
-                    do {
-                        if (++at.item == p.groups) {
-                            at.item = 0;
-                            ++at.outer;
-                        }
-                    } while (p.grp[at.item].key_tiles == 0);
-                    g = p.grp[at.item];
-                }
-            }
-            fresh = true;
-        }
-        if (f + 1 < f1) fetch();
-        __syncthreads();  // (this tile is there, and the other place has been read)
-        if (now.block * kBlock + wave * kColumns < gn.rows * p.G) {
-            const int n0 = now.tile * S::kSharedKeys;
-            const bool cut = n0 + S::kSharedKeys > gn.shared;
-            attend<POOL, D, S::kSharedKeys / 32>(p, st, lds, place * S::kSharedBytes, place * S::kSharedBytes + S::kSharedBytes / 2, half, col,
-                                                 [&](floatx16 &s, int b) __attribute__((always_inline)) {
-                                                     if (!cut) return;
+    constexpr int kRows = 64 / S::kPieces;  // that a wave moves at a time
+    int lane = half * 32 + col;
+    asm volatile("" : "+v"(lane));  // (as in attend)
+    half = lane >> 5;
+    col = lane & 31;
+    const int piece = lane % S::kPieces;
 #pragma unroll
-                                                     for (int x = 0; x < 16; ++x)
-                                                         if (n0 + b * 32 + 8 * (x / 4) + 4 * half + x % 4 >= gn.shared) s[x] = -INFINITY;
-                                                 });
+    for (int round = 0; round < kColumns / COLS; ++round) {
+        wave_sync();
+        if (COLS == kColumns || col / COLS == round) {
+            const int c = col % COLS;
+#pragma unroll
+            for (int d = 0; d < S::kDTiles; ++d)
+#pragma unroll
+                for (int x = 0; x < 16; x += 4) {  // four d in a row
+                    const floatx2 a = {st.o[d][x] * factor, st.o[d][x + 1] * factor}, b = {st.o[d][x + 2] * factor, st.o[d][x + 3] * factor};
+                    const u32x2 y = OUT ? u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(a, bf16x2)), __builtin_bit_cast(uint32_t, __builtin_convertvector(b, bf16x2))}
+                                        : u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(a, halfx2)), __builtin_bit_cast(uint32_t, __builtin_convertvector(b, halfx2))};
+                    *reinterpret_cast<u32x2 *>(area + c * S::kRowBytes + k_piece<true, D>(c, d * 4 + x / 4) * 16 + 8 * half) = y;
+                }
         }
-        place ^= 1;
-        if (f + 1 < f1) put(place);
-        if (fresh || f + 1 == f1) {
-            const bool whole = now.tile + 1 == gn.key_tiles && f - now.tile >= f0;
-            const float l = sum_of_halves(st.l);
-            const int64_t index = whole ? row * p.Hq + head : ((int64_t)2 * r + !first) * kBlock + wave * kColumns + col;
-            write_part<POOL, D>(st, l, (whole ? p.shared_whole_o : p.shared_o) + index * D, (whole ? p.shared_whole_ml : p.shared_ml) + index * 2, exists, half);
-            first = false;
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < COLS / kRows; ++i) {
+            const int c = i * kRows + lane / S::kPieces;
+            const u32x4 y = *reinterpret_cast<const u32x4 *>(area + c * S::kRowBytes + k_piece<true, D>(c, piece) * 16);
+            char *const at = to(round * COLS + c);
+            if (at && OUT) __builtin_nontemporal_store(y, reinterpret_cast<u32x4 *>(at + piece * 16));
+            else if (at) *reinterpret_cast<u32x4 *>(at + piece * 16) = y;  // (read soon)
         }
     }
 }
 
-// ------------------------------------------------------------------------------------------ keys of a sequence by itself
-// Every wave walks a range of its own, without barriers: tiles of 32 keys, the next one on its way into registers while this one is read from the
-// wave's part of LDS.  Neighbouring waves have neighbouring KV heads of the same keys.
-template <Pool POOL, int D>
-__device__ __attribute__((always_inline)) inline void own_work(const SharedParams &p, char *lds, int wg) {
+// A wave's columns as a part: unnormalised output, maximum and sum, to rows to(c) of `o` and `ml` (negative: there is no column c).  Outputs of bf16
+// products are written in fp16, relative to their largest: (m, l, o) and (m + e, l 2^-e, o 2^-e) are the same part, and with all o 2^-e below 1 the rounding is
+// 2^-12 of each and 2^-25 of the largest, against 2^-9 of the probabilities before and of the result after (half the bytes: 256 sequences of 512 to 4,096
+// tokens at 28/4 heads over 8 bits leave 20 MB).  What is not finite stays so.
+template <Pool POOL, int D, int COLS, typename To>
+__device__ __attribute__((always_inline)) inline void write_part(const State<POOL, D> &st, float l, char *o, float *ml, char *area, int half, int col, To &&to) {
     using S = Shape<POOL, D>;
+    float m = st.m, factor = 1.f;
+    if constexpr (S::kHalf) {
+        float top = 0.f;
+#pragma unroll
+        for (int d = 0; d < S::kDTiles; ++d)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) top = fmaxf(top, fabsf(st.o[d][x]));
+        if (__ballot(top == INFINITY) != 0) {  // (NaN is passed over, infinities are here)
+            top = 0.f;
+#pragma unroll
+            for (int d = 0; d < S::kDTiles; ++d)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) top = fmaxf(top, fabsf(st.o[d][x]) < INFINITY ? fabsf(st.o[d][x]) : 0.f);
+        }
+        const int e = max(-100, min((int)(__float_as_uint(max_of_halves(top)) >> 23) - 126, 126));  // top < 2^e
+        factor = __uint_as_float((uint32_t)(127 - e) << 23);
+        m += (float)e;
+        l *= factor;
+    }
+    const int64_t mine = to(col);
+    if (half == 0 && mine >= 0) *reinterpret_cast<floatx2 *>(ml + mine * 2) = floatx2{m, l};
+    if constexpr (S::kHalf) {
+        write_rows<POOL, D, COLS, false>(st, factor, area, half, col, [&](int c) __attribute__((always_inline)) {
+            const int64_t at = to(c);
+            return at < 0 ? nullptr : o + at * (D * 2);
+        });
+    } else if (mine >= 0) {
+#pragma unroll
+        for (int d = 0; d < S::kDTiles; ++d)
+#pragma unroll
+            for (int x = 0; x < 16; x += 4)
+                *reinterpret_cast<floatx4 *>(o + (mine * D + d * 32 + 2 * x + 4 * half) * 4) = floatx4{st.o[d][x], st.o[d][x + 1], st.o[d][x + 2], st.o[d][x + 3]};
+    }
+}
+
+// ------------------------------------------------------------------------------------------ keys that a group shares
+// f(0), f(1) ... f(N-1), each with its number as a type.
+template <int N, typename F, int... I>
+__device__ __attribute__((always_inline)) inline void each_of(F &&f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __attribute__((always_inline)) inline void each(F &&f) {
+    each_of<N>(f, std::make_integer_sequence<int, N>{});
+}
+
+typedef __attribute__((address_space(3))) void *LdsTo;
+typedef const __attribute__((address_space(1))) void *GlobalFrom;
+
+// K or V of a tile of shared keys on its way from the pool into LDS: each wave moves a quarter of the keys, which lie in one page.  bf16: straight into
+// LDS, each lane asking for the piece that belongs where its sixteen bytes land.  8 bits: K through registers and V through LDS as it is (`to`), where each lane
+// finds again what it has asked for, to be turned into bf16; there would not be registers for both.  fp32: through registers.
+template <Pool POOL, int D, bool V>
+struct Stage {
+    using S = Shape<POOL, D>;
+    static constexpr bool kDirect = POOL == kBf16, kRaw = POOL == kE4m3 && V;
+    static constexpr int kLoads = S::kSharedLoads;
+    u32x4 x[kDirect || kRaw ? 1 : kLoads];
+    uint32_t scale;  // of the wave's key `lane`
+    __device__ __attribute__((always_inline)) inline void load(const SharedParams &p, const GroupPlan &g, int h, int tile, int wave, int lane, char *to) {
+        const int last = g.shared - 1, n = min(tile * S::kSharedKeys + wave * S::kWaveKeys, last), left = last - n;
+        const int64_t page = max(0, min(((ConstInts)p.page_table)[g.e0 + (n >> p.page_shift)], p.num_pages - 1));
+        const int slot = n & ((1 << p.page_shift) - 1);
+        const char *from = (V ? p.v : p.k) + (((page << p.page_shift) + slot) * p.Hkv + h) * (D * S::kPoolSize);
+        const uint32_t token = (uint32_t)p.Hkv * D * S::kPoolSize;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int in_wave = i * S::kLoadKeys + lane / S::kPoolPieces, key = wave * S::kWaveKeys + in_wave, at = lane % S::kPoolPieces;
+            const int piece = !kDirect ? at : V ? v_piece<S::kHalf, D>(key, at) : k_piece<S::kHalf, D>(key, at);  // (an exclusive or: its own inverse)
+            const char *mine = from + ((uint32_t)min(in_wave, left) * token + (uint32_t)piece * 16);
+            if constexpr (kDirect)
+                __builtin_amdgcn_global_load_lds((GlobalFrom)mine, (LdsTo)(to + (wave * S::kWaveKeys + i * S::kLoadKeys) * S::kRowBytes), 16, 0, 0);
+            else if constexpr (kRaw)
+                __builtin_amdgcn_global_load_lds((GlobalFrom)mine, (LdsTo)(to + (wave * kLoads + i) * 1024), 16, 0, 0);
+            else
+                x[i] = *reinterpret_cast<const u32x4 *>(mine);
+        }
+        if constexpr (kRaw) asm volatile("" ::: "memory");  // (the scale is asked for last: put() goes by that)
+        if constexpr (POOL == kE4m3) scale = (V ? p.v_scale : p.k_scale)[((page * p.Hkv + h) << p.page_shift) + slot + min(lane % S::kWaveKeys, left)];
+    }
+    // What load() has asked for, into the tile (straight ones are there).  Of V, what lies past the shared keys is zero: `end` keys of the tile are shared.
+    __device__ __attribute__((always_inline)) inline void put(char *tile, int wave, int lane, int end, const char *raw = nullptr) const {
+        asm volatile("" : "+v"(lane));
+        // (loads come back in order: with the scale, which was asked for last, the codes are there)
+        if constexpr (kRaw) asm volatile("" ::"v"(scale) : "memory");
+        if constexpr (kDirect) {
+            if (V && end < S::kSharedKeys)
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i)
+                    if (wave * S::kWaveKeys + i * S::kLoadKeys + lane / S::kPieces >= end)
+                        *reinterpret_cast<u32x4 *>(tile + (wave * S::kWaveKeys + i * S::kLoadKeys) * S::kRowBytes + lane * 16) = u32x4{0, 0, 0, 0};
+        } else {
+            constexpr int kOut = POOL == kE4m3 ? 2 : 1;
+            const int my_key = wave * S::kWaveKeys + lane / S::kPoolPieces, piece = lane % S::kPoolPieces * kOut;
+            const int at = my_key * S::kRowBytes + (V ? v_piece<S::kHalf, D>(my_key, piece) : k_piece<S::kHalf, D>(my_key, piece)) * 16;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                u32x4 a[kOut];
+                if constexpr (POOL == kE4m3) {
+                    u32x4 codes;
+                    if constexpr (kRaw) codes = *reinterpret_cast<const u32x4 *>(raw + (wave * kLoads + i) * 1024 + lane * 16);
+                    else codes = x[i];
+                    const float step = scale_of(__shfl((int)scale, i * S::kLoadKeys + lane / S::kPoolPieces));
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        uint32_t lo, hi;
+                        values_of(codes[w], step, lo, hi);
+                        a[w / 2][w % 2 * 2] = lo;
+                        a[w / 2][w % 2 * 2 + 1] = hi;
+                    }
+                } else {
+                    a[0] = x[i];
+                }
+                if (V && end < S::kSharedKeys) {
+#pragma unroll
+                    for (int y = 0; y < kOut; ++y)
+                        for (int w = 0; w < 4; ++w) a[y][w] &= my_key + i * S::kLoadKeys < end ? ~0u : 0u;
+                }
+#pragma unroll
+                for (int y = 0; y < kOut; ++y)
+                    *reinterpret_cast<u32x4 *>(tile + (at ^ (V ? 16 * y : k_piece<S::kHalf, D>(i * S::kLoadKeys, y) * 16)) + i * S::kLoadKeys * S::kRowBytes) = a[y];
+            }
+        }
+    }
+};
+
+// Scores of keys past the shared ones are masked.
+template <int NB>
+__device__ __attribute__((always_inline)) inline void mask_past(floatx16 (&s)[NB], int n0, int half, int end) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+            if (n0 + b * 32 + 8 * (x / 4) + 4 * half + x % 4 >= end) s[b][x] = -INFINITY;
+}
+
+// The waves of the work-group meet: what they have written to LDS is there, and all but the `kLeft` loads that each has asked for last.
+template <int kLeft>
+__device__ __attribute__((always_inline)) inline void meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (kLeft & 15) | (kLeft >> 4) << 14);  // vmcnt(kLeft) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// fp32: tiles t0 .. t1-1 one after the other, one of them read while the next is on its way.
+template <int D>
+__device__ __attribute__((always_inline)) inline void shared_tiles(const SharedParams &p, char *lds, const GroupPlan &g, int h, int t0, int t1, bool active, State<kF32, D> &st) {
+    using S = Shape<kF32, D>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
+    Stage<kF32, D, false> k;
+    Stage<kF32, D, true> v;
+    k.load(p, g, h, t0, wave, lane, nullptr);
+    v.load(p, g, h, t0, wave, lane, nullptr);
+    st.sign_q(p);
+    for (int t = t0; t < t1; ++t) {
+        const int at = (t - t0) % 2 * S::kSharedBytes, n0 = t * S::kSharedKeys;
+        k.put(lds + at, wave, lane, S::kSharedKeys);
+        v.put(lds + at + S::kSharedBytes / 2, wave, lane, g.shared - n0);
+        if (t + 1 < t1) {
+            k.load(p, g, h, t + 1, wave, lane, nullptr);
+            v.load(p, g, h, t + 1, wave, lane, nullptr);
+        }
+        __syncthreads();  // (this tile is there, and the one before the last has been read)
+        if (active)
+            attend<kF32, D, 1>(p, st, lds, at, at + S::kSharedBytes / 2, half, col, [&](floatx16 &s, int) __attribute__((always_inline)) {
+                if (n0 + S::kSharedKeys <= g.shared) return;
+                floatx16 x[1] = {s};
+                mask_past(x, n0, half, g.shared);
+                s = x[0];
+            });
+    }
+    __syncthreads();
+}
+
+// bf16 products: the scores of tile t+1 are multiplied while the exponentials of tile t are computed, so step t reads K of t+1 and V of t.  LDS holds
+// three (8 bits: two) tiles of K and two of V.  bf16: step t asks for K of t+3 and V of t+1, whose places were read a step before; K is waited for two
+// steps on.  8 bits: it puts K of t+2 and V of t+1 in their places and asks for K of t+4 and V of t+3 (a step is shorter than the memory's latency).  Written in the
+// order it is to run in: a product, an LDS read kReads products before its use, and a share of the rest.
+template <Pool POOL, int D>
+__device__ __attribute__((always_inline)) inline void shared_tiles(const SharedParams &p, char *lds, const GroupPlan &g, int h, int t0, int t1, bool active, State<POOL, D> &st) {
+    using S = Shape<POOL, D>;
+    typedef Stage<POOL, D, false> StageK;
+    typedef Stage<POOL, D, true> StageV;
+    constexpr bool kDirect = StageK::kDirect;
+    constexpr int kTile = S::kSharedBytes / 2, kBlocks = S::kSharedKeys / 32;  // of K or V; of 32 keys
+    constexpr int kRing = kDirect ? 3 : 2, kV = kRing * kTile;                 // places of K; where V's begin
+    constexpr int kFirst = kBlocks * S::kPieces / 2, kSecond = 2 * kBlocks * S::kDTiles, kReads = 4;
+    constexpr int kPairs = 16 * kBlocks / 2, kEarly = kPairs * 5 / 8;          // pairs of probabilities; those along with the first products
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
+    const int last_tile = t1 - 1;
+    StageK k[kDirect ? 1 : 2];
+    StageV v[kDirect ? 1 : 2];
+    char *const raw = lds + 4 * kTile;  // two tiles of codes of V
+    auto v_end = [&](int t) __attribute__((always_inline)) { return g.shared - t * S::kSharedKeys; };
+    // Tiles t0, t0+1 (and t0+2) of K and t0 (and t0+1) of V.
+    auto fetch_k = [&](StageK &x, int t, char *to) __attribute__((always_inline)) { x.load(p, g, h, min(t, last_tile), wave, lane, to); };  // (past the last tile: not read)
+    auto fetch_v = [&](StageV &x, int t, char *to) __attribute__((always_inline)) { x.load(p, g, h, min(t, last_tile), wave, lane, to); };
+    if constexpr (kDirect) {
+        fetch_k(k[0], t0, lds);
+        fetch_v(v[0], t0, lds + kV);
+        fetch_k(k[0], t0 + 1, lds + kTile);
+        fetch_k(k[0], t0 + 2, lds + 2 * kTile);
+    } else {
+        fetch_k(k[0], t0, nullptr);
+        fetch_v(v[0], t0, raw);
+        fetch_k(k[1], t0 + 1, nullptr);
+        fetch_v(v[1], t0 + 1, raw + kTile / 2);
+        k[0].put(lds, wave, lane, S::kSharedKeys);
+        fetch_k(k[0], t0 + 2, nullptr);
+        v[0].put(lds + kV, wave, lane, v_end(t0), raw);
+        fetch_v(v[0], t0 + 2, raw);
+        k[1].put(lds + kTile, wave, lane, S::kSharedKeys);
+        fetch_k(k[1], t0 + 3, nullptr);
+    }
+    // The place of a piece within its row is an exclusive or, so the x-th pair of pieces of K lies at k_at ^ 32 x and the d-th tile of V at v_at ^ 64 d.
+    int k_at = col * S::kRowBytes + k_piece<true, D>(col, half) * 16;
+    const int i16 = lane & 15, v_key = half * 4 + (i16 >> 2), d0 = ((lane & 16) + 4 * (i16 & 3)) * 2;
+    int v_at = kV + v_key * S::kRowBytes + v_piece<true, D>(v_key, d0 >> 4) * 16 + (d0 & 15);
+
+    auto rescale = [&](float top) __attribute__((always_inline)) {  // with the largest score that this lane has
+        top = max_of_halves(top) * p.scale2;
+        if (__ballot(top > st.m + kRescaleSlack) == 0) return;  // (m = -inf: any finite score)
+        const float m_new = top > st.m + kRescaleSlack ? top : st.m;
+        const float f = st.m == m_new ? 1.f : __builtin_amdgcn_exp2f(st.m - m_new);
+        st.m = m_new;
+        st.ref = m_new == -INFINITY ? 0.f : m_new;
+        st.l *= f;
+#pragma unroll
+        for (int d = 0; d < S::kDTiles; ++d)
+            for (int x = 0; x < 16; ++x) st.o[d][x] *= f;
+    };
+    auto largest = [&](const floatx16(&s)[kBlocks]) __attribute__((always_inline)) {
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int x = b == 0; x < 16; ++x) top = fmaxf(top, s[b][x]);
+        return top;
+    };
+    // Two probabilities of sixteen keys' B operand, the n-th pair of all: slot j is key 8 (j / 4) + 4 half + j % 4 of them.  Rounded to bf16 for the
+    // second product (2^-9 each, averaging over the keys); the sum is that of the unrounded ones.
+    auto pair = [&](auto n_, const floatx16(&s)[kBlocks], u32x4(&pf)[2 * kBlocks]) __attribute__((always_inline)) {
+        constexpr int n = decltype(n_)::value, i = n / 4, j = n % 4 * 2;
+        const float a = __builtin_amdgcn_exp2f(fmaf(s[i / 2][i % 2 * 8 + j], p.scale2, -st.ref));
+        const float c = __builtin_amdgcn_exp2f(fmaf(s[i / 2][i % 2 * 8 + j + 1], p.scale2, -st.ref));
+        st.l += a;
+        st.l += c;
+        asm volatile("" : "+v"(st.l));  // (added now: later, the sixteen pairs would have to be kept)
+        pf[i][j / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{a, c}, bf16x2));
+    };
+    auto read_v = [&](int i, int d, int tile) __attribute__((always_inline)) {
+        s16x4 vt[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) vt[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTr)(lds + (v_at ^ (64 * d)) + (tile + (i * 16 + j * 8) * S::kRowBytes)));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(vt[0], vt[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    // Step t (not the last), whose scores are in s with their maximum taken into account.  KPLACE, VPLACE: (t - t0) modulo the places of K and of V.
+    auto step = [&](auto k_place, auto v_place, int t, floatx16(&s)[kBlocks], floatx16(&next)[kBlocks]) __attribute__((always_inline)) {
+        constexpr int kPlace = decltype(k_place)::value, vPlace = decltype(v_place)::value;
+        char *const v_to = lds + kV + (vPlace ^ 1) * kTile;
+        if constexpr (kDirect) {
+            fetch_v(v[0], t + 1, v_to);
+            fetch_k(k[0], t + 3, lds + kPlace * kTile);
+        }
+        asm volatile("" : "+v"(k_at), "+v"(v_at));  // (the addresses that follow from them would not fit beside the tiles)
+        if (active) {
+            __builtin_amdgcn_sched_barrier(0);
+            bf16x8 ahead[kReads];
+            u32x4 pf[2 * kBlocks];
+            auto read = [&](auto i_) __attribute__((always_inline)) {
+                constexpr int i = decltype(i_)::value;
+                if constexpr (i < kFirst) {
+                    constexpr int b = i % kBlocks, x = i / kBlocks;
+                    ahead[i % kReads] = *reinterpret_cast<const bf16x8 *>(lds + (k_at ^ (32 * x)) + ((kPlace + 1) % kRing * kTile + b * 32 * S::kRowBytes));
+                } else if constexpr (i < kFirst + kSecond) {
+                    ahead[i % kReads] = read_v((i - kFirst) / S::kDTiles, (i - kFirst) % S::kDTiles, vPlace * kTile);
+                }
+            };
+            float top = -INFINITY;
+            each<kReads>([&](auto i) __attribute__((always_inline)) { read(i); });
+            __builtin_amdgcn_sched_barrier(0);
+            each<kFirst + kSecond>([&](auto i_) __attribute__((always_inline)) {
+                constexpr int i = decltype(i_)::value;
+                if constexpr (!kDirect && i == kFirst) {
+                    k[vPlace].put(lds + kPlace * kTile, wave, lane, S::kSharedKeys);
+                    fetch_k(k[vPlace], t + 4, nullptr);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if constexpr (i < kFirst) {
+                    constexpr int b = i % kBlocks, x = i / kBlocks;
+                    const floatx16 none{};
+                    next[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[i % kReads], __builtin_bit_cast(bf16x8, st.qf[x]), x == 0 ? none : next[b], 0, 0, 0);
+                } else {
+                    constexpr int e = (i - kFirst) / S::kDTiles, d = (i - kFirst) % S::kDTiles;
+                    st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[i % kReads], __builtin_bit_cast(bf16x8, pf[e]), st.o[d], 0, 0, 0);
+                }
+                read(std::integral_constant<int, i + kReads>{});
+                if constexpr (i < kFirst) {
+                    constexpr int from = i * kEarly / kFirst, to = (i + 1) * kEarly / kFirst;
+                    each<to - from>([&](auto n) __attribute__((always_inline)) { pair(std::integral_constant<int, from + decltype(n)::value>{}, s, pf); });
+                } else {  // the other pairs, none later than the products before its own, then the maximum
+                    constexpr int n = kEarly + i - kFirst, at = i - kFirst - (kPairs - kEarly), kRest = kSecond - (kPairs - kEarly);
+                    if constexpr (n < kPairs) pair(std::integral_constant<int, n>{}, s, pf);
+                    else
+#pragma unroll
+                        for (int x = 16 * kBlocks * at / kRest; x < 16 * kBlocks * (at + 1) / kRest; ++x) top = fmaxf(top, next[x / 16][x % 16]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            if ((t + 2) * S::kSharedKeys > g.shared) {  // (uniform)
+                mask_past(next, (t + 1) * S::kSharedKeys, half, g.shared);
+                top = largest(next);
+            }
+            rescale(top);
+        } else if constexpr (!kDirect) {
+            k[vPlace].put(lds + kPlace * kTile, wave, lane, S::kSharedKeys);
+            fetch_k(k[vPlace], t + 4, nullptr);
+        }
+        if constexpr (kDirect) {
+            if (v_end(t + 1) < S::kSharedKeys) {  // (uniform)
+                __builtin_amdgcn_s_waitcnt(0x0070);
+                v[0].put(v_to, wave, lane, v_end(t + 1));
+            }
+            meet<StageK::kLoads>();  // (V of t+1 and K of t+2)
+        } else {
+            v[vPlace ^ 1].put(v_to, wave, lane, v_end(t + 1), raw + (vPlace ^ 1) * (kTile / 2));
+            fetch_v(v[vPlace ^ 1], t + 3, raw + (vPlace ^ 1) * (kTile / 2));
+            meet<63>();
+        }
+    };
+
+    floatx16 even[kBlocks], odd[kBlocks];
+    st.sign_q(p);
+    if constexpr (kDirect) {
+        if (v_end(t0) < S::kSharedKeys) {
+            __builtin_amdgcn_s_waitcnt(0x0070);
+            v[0].put(lds + kV, wave, lane, v_end(t0));
+        }
+        meet<StageK::kLoads>();  // (all but the third tile of K)
+    } else {
+        meet<63>();
+    }
+    if (active) {
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int x = 0; x < S::kPieces / 2; ++x) {
+                const bf16x8 a = *reinterpret_cast<const bf16x8 *>(lds + (k_at ^ (32 * x)) + b * 32 * S::kRowBytes);
+                const floatx16 none{};
+                even[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, st.qf[x]), x == 0 ? none : even[b], 0, 0, 0);
+            }
+        if ((t0 + 1) * S::kSharedKeys > g.shared) mask_past(even, t0 * S::kSharedKeys, half, g.shared);
+        rescale(largest(even));
+    }
+    meet<kDirect ? StageK::kLoads : 63>();  // (the first tile's K is read by all before it is written over)
+    // As many steps in a row as bring both kinds of places around, so that they are constants.
+    constexpr int kRound = kRing == 3 ? 6 : 2;
+    int t = t0, done = 0;
+    for (bool more = t + 1 < t1; more;) {
+        each<kRound>([&](auto i_) __attribute__((always_inline)) {
+            constexpr int i = decltype(i_)::value;
+            if (t + 1 < t1) {
+                if constexpr (i % 2 == 0) step(std::integral_constant<int, i % kRing>{}, std::integral_constant<int, i % 2>{}, t, even, odd);
+                else step(std::integral_constant<int, i % kRing>{}, std::integral_constant<int, i % 2>{}, t, odd, even);
+                ++t;
+                done = (i + 1) % 2;
+            }
+        });
+        more = t + 1 < t1;
+    }
+    if (active) {  // the last tile's exponentials and second product
+        if (done == 1)
+            for (int b = 0; b < kBlocks; ++b) even[b] = odd[b];
+        u32x4 pf[2 * kBlocks];
+        each<kPairs>([&](auto n) __attribute__((always_inline)) { pair(n, even, pf); });
+#pragma unroll
+        for (int i = 0; i < 2 * kBlocks; ++i)
+#pragma unroll
+            for (int d = 0; d < S::kDTiles; ++d)
+                st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v(i, d, done * kTile), __builtin_bit_cast(bf16x8, pf[i]), st.o[d], 0, 0, 0);
+    }
+    meet<0>();  // (LDS is free)
+}
+
+// A range of the tiles over shared keys, group after group and block of columns after block: every wave has 32 of the work-group's 128 columns, and the four
+// stage the tiles together.
+template <Pool POOL, int D>
+__device__ __attribute__((always_inline)) inline void shared_work(const SharedParams &p, char *lds, const Job &job) {
+    using S = Shape<POOL, D>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
+    int left = job.tiles, tile = job.tile, block = job.block, item = job.item, h = job.outer;
+    GroupPlan g = job.g;
+    bool first = true;
+    for (;;) {
+        const int t1 = min(g.key_tiles, tile + left), last = g.rows * p.G - 1, column0 = block * kBlock + wave * kColumns;
+        State<POOL, D> st;
+        {
+            const int c = min(column0 + col, last), i = by_g(p, c);
+            st.clear();
+            st.load_q(p, (int64_t)g.q0 + i, h * p.G + c - i * p.G, half);
+        }
+        shared_tiles(p, lds, g, h, tile, t1, column0 <= last, st);
+        const bool whole = tile == 0 && t1 == g.key_tiles;
+        if (column0 <= last)
+            write_part<POOL, D, kColumns>(st, sum_of_halves(st.l), whole ? p.shared_whole_o : p.shared_o, whole ? p.shared_whole_ml : p.shared_ml,
+                                          lds + wave * (kColumns * S::kRowBytes), half, col, [&](int c) __attribute__((always_inline)) {
+                                              const int packed = column0 + c;
+                                              if (packed > last) return (int64_t)-1;
+                                              if (!whole) return ((int64_t)2 * job.range + !first) * kBlock + wave * kColumns + c;
+                                              const int i = by_g(p, packed);
+                                              return ((int64_t)g.q0 + i) * p.Hq + h * p.G + packed - i * p.G;
+                                          });
+        first = false;
+        left -= t1 - tile;
+        if (left == 0) break;
+        tile = 0;
+        if (++block == g.blocks) {
+            block = 0;
+            do {
+                if (++item == p.groups) {
+                    item = 0;
+                    ++h;
+                }
+            } while (p.grp[item].key_tiles == 0);
+            g = p.grp[item];
+        }
+        meet<63>();  // (the rows have been read)
+    }
+}
+
+// ------------------------------------------------------------------------------------------ keys of a sequence by itself
+struct OwnPart {
+    int32_t kv_head, packed0, begin_tile, n0, half, col;  // n0: first key of its last tile
+    bool whole, final, bad;  // whole: all own keys of the sequence; final: and it shares none; bad: values of V were left out
+    int64_t slot;            // of its first column
+};
+
+// A wave's columns over the own keys of a sequence, or a part of them: to the output, or to where the parts are joined.
+template <Pool POOL, int D>
+__device__ __attribute__((always_inline)) inline void own_finish(const SharedParams &p, const State<POOL, D> &st, const SeqPlan &sn, const OwnPart &w, char *area) {
+    using S = Shape<POOL, D>;
+    const int lane = w.half * 32 + w.col, half = w.half;
+    const float l = sum_of_halves(st.l);
+    auto row_of = [&](int c) __attribute__((always_inline)) {  // the row and head of column c, as a row of the output
+        const int packed = w.packed0 + c, i = by_g(p, packed);
+        return packed >= sn.R * p.G ? (int64_t)-1 : ((int64_t)sn.q0 + i) * p.Hq + w.kv_head * p.G + packed - i * p.G;
+    };
+    char *const part_o = w.whole ? p.own_whole_o : p.own_o;
+    if (w.final) {
+        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // (no visible key: zero; NaN stays)
+        const int64_t mine = row_of(w.col);
+        if (p.lse && half == 0 && mine >= 0) p.lse[mine] = l == 0.f ? -INFINITY : st.m * 0.693147180559945309f + logf(l);
+        if constexpr (S::kHalf) {
+            write_rows<POOL, D, kColumns, true>(st, inv, area, half, w.col, [&](int c) __attribute__((always_inline)) {
+                const int64_t at = row_of(c);
+                return at < 0 ? nullptr : p.out + at * S::kRowBytes;
+            });
+        } else if (mine >= 0) {
+#pragma unroll
+            for (int d = 0; d < S::kDTiles; ++d)
+#pragma unroll
+                for (int x = 0; x < 16; x += 4)
+                    *reinterpret_cast<floatx4 *>(p.out + mine * S::kRowBytes + (d * 32 + 2 * x + 4 * half) * 4) =
+                        floatx4{st.o[d][x] * inv, st.o[d][x + 1] * inv, st.o[d][x + 2] * inv, st.o[d][x + 3] * inv};
+        }
+    } else {
+        write_part<POOL, D, kColumns>(st, l, part_o, w.whole ? p.own_whole_ml : p.own_ml, area, half, w.col, [&](int c) __attribute__((always_inline)) {
+            const int64_t at = row_of(c);
+            return at < 0 || w.whole ? at : w.slot + c;
+        });
+    }
+    if (!w.bad) return;
+    // The values that put() left out, added to what this wave has written: a column and a d of it per lane.
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    __builtin_amdgcn_wave_barrier();
+    // (in the tile that the shared keys end in, and from the first one on that some row does not see all of)
+    const int before = sn.L - sn.R, first_key = (sn.shared / 32 + w.begin_tile) * 32, end_key = min(w.n0 + 32, sn.L);
+    const int next = first_key < sn.shared ? first_key + 32 : first_key, masked = max(next, max(before, 0) / 32 * 32);
+    for (int e = lane; e < kColumns * D; e += 64) {
+        const int c = w.packed0 + e / D, d = e % D;
+        if (c >= sn.R * p.G) break;
+        const int i = by_g(p, c);
+        const uint64_t bits = p.tree_mask ? p.tree_mask[sn.q0 + i] : 0;
+        float sum = 0.f;
+        for (int n = first_key < sn.shared ? sn.shared : masked; n < end_key; n = n + 1 == next ? masked : n + 1) {
+            const bool sees = p.tree_mask ? n < before || (n - before < 64 && (bits >> (n - before) & 1)) : n <= before + i;
+            if (!sees) continue;
+            const int64_t page = max(0, min(p.page_table[sn.e0 + (n >> p.page_shift)], p.num_pages - 1));
+            const int slot = n & ((1 << p.page_shift) - 1);
+            const int64_t el = (((page << p.page_shift) + slot) * p.Hkv + w.kv_head) * D + d;
+            float x;
+            if constexpr (POOL == kF32) x = reinterpret_cast<const float *>(p.v)[el];
+            else if constexpr (POOL == kBf16) x = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p.v)[el] << 16);
+            else {
+                uint32_t lo, hi;
+                values_of(reinterpret_cast<const uint8_t *>(p.v)[el], scale_of(p.v_scale[((page * p.Hkv + w.kv_head) << p.page_shift) + slot]), lo, hi);
+                x = __uint_as_float(lo << 16);
+            }
+            if (!(fabsf(x) < INFINITY)) sum += x;
+        }
+        if (sum == 0.f) continue;  // (nothing but infinities and NaN is added)
+        const int64_t row = row_of(e / D);
+        char *const to = w.final ? p.out + (row * D + d) * S::kSize : part_o + ((w.whole ? row : w.slot + e / D) * D + d) * S::kSize;
+        if constexpr (!S::kHalf) *reinterpret_cast<float *>(to) += sum;
+        else if (w.final) *reinterpret_cast<__bf16 *>(to) = (__bf16)((float)*reinterpret_cast<__bf16 *>(to) + sum);
+        else *reinterpret_cast<_Float16 *>(to) = (_Float16)((float)*reinterpret_cast<_Float16 *>(to) + sum);
+    }
+}
+
+// A place in the list of own work, and the sequence that it is in.
+struct OwnPlace {
+    int32_t outer, item, tile;
+    SeqPlan s;
+    __device__ __attribute__((always_inline)) inline bool next(const SharedParams &p, bool more) {  // whether the tile was its sequence's last; `more`: there is a next one
+        if (++tile < s.tiles) return false;
+        tile = 0;
+        if (more) {
+            do {
+                if (++item == p.B) {
+                    item = 0;
+                    ++outer;
+                }
+            } while (p.seq[item].tiles == 0);
+            s = p.seq[item];
+        }
+        return true;
+    }
+    __device__ int first_key() const { return (s.shared / 32 + tile) * 32; }
+};
+
+// Every wave walks a range of its own, without barriers: tiles of 32 keys, the next kAhead of them on their way into registers while this one is read from
+// the wave's part of LDS.  Neighbouring waves have neighbouring KV heads of the same keys.
+template <Pool POOL, int D>
+__device__ __attribute__((always_inline)) inline void own_work(const SharedParams &p, char *lds, const Job &job) {
+    using S = Shape<POOL, D>;
+    constexpr int kAhead = POOL == kE4m3 ? 2 : 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int half = lane >> 5, col = lane & 31;
-    const int cw = wave % p.col_waves, hi = wave / p.col_waves % p.heads_wg, part = wave / (p.col_waves * p.heads_wg);
-    const int r = wg * p.parts_wg + part;
-    if (r >= p.totals->own_ranges) return;
-    Start at = p.own_start[r];
-    const int64_t f0 = at.f, f1 = p.own_start[r + 1].f;
-    if (f0 >= f1) return;
+    const int cw = wave % p.col_waves, hi = wave / p.col_waves % p.heads_wg, n_tiles = job.tiles;
     const int head_groups = p.Hkv / p.heads_wg;
     char *const kt = lds + wave * S::kOwnBytes, *const vt = kt + S::kOwnBytes / 2;
-    SeqPlan s = p.seq[at.item];
+    OwnPlace now{job.outer, job.item, job.tile, job.s}, ahead = now;
     State<POOL, D> st;
-    Mover<POOL, D, S::kOwnLoads> mover;
-    auto fetch = [&]() __attribute__((always_inline)) {
-        mover.template load<true>(p, s.e0, at.outer % head_groups * p.heads_wg + hi, (s.shared / 32 + at.tile) * 32, s.L - 1, lane);
+    Mover<POOL, D, S::kOwnLoads> mover[kAhead];
+    auto fetch = [&](Mover<POOL, D, S::kOwnLoads> &m, int f) __attribute__((always_inline)) {  // the tile that is f-th of this range
+        m.template load<true>(p, ahead.s.e0, ahead.outer % head_groups * p.heads_wg + hi, ahead.first_key(), ahead.s.L - 1, lane);
+        ahead.next(p, f + 1 < n_tiles);
     };
-    fetch();
-    bool fresh = true, first = true, bad = false, exists = false;
-    int64_t row = 0;
-    int head = 0, lim = 0, packed0 = 0, begin_tile = 0;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (i < n_tiles) fetch(mover[i], i);
+    bool fresh = true, first = true, bad = false;
+    int lim = 0, packed0 = 0, begin_tile = 0;
     uint64_t bits = 0;
-    for (int64_t f = f0; f < f1; ++f) {
-        const Start now = at;
-        const SeqPlan sn = s;
+    auto step = [&](Mover<POOL, D, S::kOwnLoads> &m, int f) __attribute__((always_inline)) {
+        const SeqPlan sn = now.s;
+        const int tile = now.tile;
         const int kv_head = now.outer % head_groups * p.heads_wg + hi;
-        const int n0 = (sn.shared / 32 + now.tile) * 32, before = sn.L - sn.R;  // keys before the new tokens (negative: the first rows see none)
+        const int n0 = now.first_key(), before = sn.L - sn.R;  // keys before the new tokens (negative: the first rows see none)
         const bool special = n0 < sn.shared || n0 + 32 > before + (p.tree_mask ? 0 : 1);
-        if (special) bad |= mover.template put<kSift>(kt, vt, 0, lane, n0, sn.shared, sn.L);
-        else mover.template put<kAll>(kt, vt, 0, lane, 0, 0, 0);
         if (fresh) {
             packed0 = (now.outer / head_groups * p.col_waves + cw) * kColumns;
-            begin_tile = now.tile;
+            begin_tile = tile;
             const int last = sn.R * p.G - 1, c = min(packed0 + col, last), i = by_g(p, c);
-            exists = packed0 + col <= last;
-            row = sn.q0 + i;
-            head = kv_head * p.G + c - i * p.G;
             lim = before + i + 1;
-            if (p.tree_mask) bits = p.tree_mask[row];
+            if (p.tree_mask) bits = p.tree_mask[sn.q0 + i];
             st.clear();
-            st.load_q(p, row, head, half);
-            fresh = false;
+            st.load_q(p, (int64_t)sn.q0 + i, kv_head * p.G + c - i * p.G, half);
         }
-        if (++at.tile == s.tiles) {
-            at.tile = 0;
-            if (f + 1 < f1) {
-                do {
-                    if (++at.item == p.B) {
-                        at.item = 0;
-                        ++at.outer;
-                    }
-                } while (p.seq[at.item].tiles == 0);
-                s = p.seq[at.item];
-            }
-            fresh = true;
-        }
-        if (f + 1 < f1) fetch();
+        if (special) bad |= m.template put<kSift>(kt, vt, 0, lane, n0, sn.shared, sn.L);
+        else m.template put<kAll>(kt, vt, 0, lane, 0, 0, 0);
+        if (fresh) st.sign_q(p);
+        if (f + kAhead < n_tiles) fetch(m, f + kAhead);
+        fresh = now.next(p, f + 1 < n_tiles);
         wave_sync();
         if (packed0 < sn.R * p.G)  // (uniform)
             attend<POOL, D, 1>(p, st, lds, wave * S::kOwnBytes, wave * S::kOwnBytes + S::kOwnBytes / 2, half, col, [&](floatx16 &sc, int) __attribute__((always_inline)) {
@@ -626,162 +1208,168 @@ __device__ __attribute__((always_inline)) inline void own_work(const SharedParam
                 }
             });
         wave_sync();
-        if (!fresh && f + 1 < f1) continue;
-        const bool whole = begin_tile == 0 && now.tile + 1 == sn.tiles, final = whole && sn.shared == 0;
-        const float l = sum_of_halves(st.l);
-        const int64_t index = whole ? row * p.Hq + head : (((int64_t)2 * r + !first) * (4 / p.parts_wg) + hi * p.col_waves + cw) * kColumns + col;
-        float *const part_o = (whole ? p.own_whole_o : p.own_o) + index * D, *const part_ml = (whole ? p.own_whole_ml : p.own_ml) + index * 2;
-        if (final) {  // all that the row sees
-            const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // (no visible key: zero; NaN stays)
-            char *const to = p.out + (row * p.Hq + head) * (int64_t)S::kRowBytes;
-            if (exists) {
-                if (p.lse && half == 0) p.lse[row * p.Hq + head] = l == 0.f ? -INFINITY : st.m * 0.693147180559945309f + logf(l);
+        if (!fresh && f + 1 < n_tiles) return;
+        const bool whole = begin_tile == 0 && tile + 1 == sn.tiles;
+        if (packed0 < sn.R * p.G)
+            own_finish<POOL, D>(p, st, sn, OwnPart{kv_head, packed0, begin_tile, n0, half, col, whole, whole && sn.shared == 0, __ballot(bad) != 0,
+                                                   (((int64_t)2 * job.range + !first) * (4 / p.parts_wg) + hi * p.col_waves + cw) * kColumns}, kt);
+        bad = first = false;
+    };
+    for (int f = 0; f < n_tiles; f += kAhead) {
 #pragma unroll
-                for (int d = 0; d < S::kDTiles; ++d)
-#pragma unroll
-                    for (int x = 0; x < 16; x += 4) {
-                        const floatx4 y = {st.o[d][x] * inv, st.o[d][x + 1] * inv, st.o[d][x + 2] * inv, st.o[d][x + 3] * inv};
-                        if constexpr (S::kHalf) {
-                            const bf16x2 a = __builtin_convertvector(floatx2{y[0], y[1]}, bf16x2), b = __builtin_convertvector(floatx2{y[2], y[3]}, bf16x2);
-                            *reinterpret_cast<u32x2 *>(to + (d * 32 + 2 * x + 4 * half) * 2) = u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
-                        } else {
-                            *reinterpret_cast<floatx4 *>(to + (d * 32 + 2 * x + 4 * half) * 4) = y;
-                        }
-                    }
-            }
-        } else {
-            write_part<POOL, D>(st, l, part_o, part_ml, exists, half);
-        }
-        first = false;
-        if (__ballot(bad) != 0) {
-            // The values that put() left out, added to what this wave has written: a column and a d of it per lane.
-            bad = false;
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-            __builtin_amdgcn_wave_barrier();
-            // (in the tile that the shared keys end in, and from the first one on that some row does not see all of)
-            const int first_key = (sn.shared / 32 + begin_tile) * 32, end_key = min(n0 + 32, sn.L);
-            const int next = first_key < sn.shared ? first_key + 32 : first_key, masked = max(next, max(before, 0) / 32 * 32);
-            for (int e = lane; e < kColumns * D; e += 64) {
-                const int c = packed0 + e / D, d = e % D;
-                if (c >= sn.R * p.G) break;
-                const int i = by_g(p, c);
-                const uint64_t own_bits = p.tree_mask ? p.tree_mask[sn.q0 + i] : 0;
-                float sum = 0.f;
-                for (int n = first_key < sn.shared ? sn.shared : masked; n < end_key; n = n + 1 == next ? masked : n + 1) {
-                    const bool sees = p.tree_mask ? n < before || (n - before < 64 && (own_bits >> (n - before) & 1)) : n <= before + i;
-                    if (!sees) continue;
-                    const int64_t page = max(0, min(p.page_table[sn.e0 + (n >> p.page_shift)], p.num_pages - 1));
-                    const int slot = n & ((1 << p.page_shift) - 1);
-                    const int64_t el = (((page << p.page_shift) + slot) * p.Hkv + kv_head) * D + d;
-                    float x;
-                    if constexpr (POOL == kF32) x = reinterpret_cast<const float *>(p.v)[el];
-                    else if constexpr (POOL == kBf16) x = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p.v)[el] << 16);
-                    else {
-                        uint32_t lo, hi;
-                        values_of(reinterpret_cast<const uint8_t *>(p.v)[el], scale_of(p.v_scale[((page * p.Hkv + kv_head) << p.page_shift) + slot]), lo, hi);
-                        x = __uint_as_float(lo << 16);
-                    }
-                    if (!(fabsf(x) < INFINITY)) sum += x;
-                }
-                if (sum == 0.f) continue;
-                const int64_t q_row = sn.q0 + i, q_head = kv_head * p.G + c - i * p.G;
-                if (final) {
-                    char *const to = p.out + ((q_row * p.Hq + q_head) * D + d) * S::kSize;
-                    if constexpr (S::kHalf) *reinterpret_cast<uint16_t *>(to) = __builtin_bit_cast(uint16_t, (__bf16)(__uint_as_float((uint32_t)*reinterpret_cast<uint16_t *>(to) << 16) + sum));
-                    else *reinterpret_cast<float *>(to) += sum;
-                } else {
-                    const int64_t at_col = whole ? q_row * p.Hq + q_head : index - col + e / D;
-                    (whole ? p.own_whole_o : p.own_o)[at_col * D + d] += sum;
-                }
-            }
-        }
+        for (int i = 0; i < kAhead; ++i)
+            if (f + i < n_tiles) step(mover[i], f + i);
     }
 }
 
 template <Pool POOL, int D>
 __global__ __launch_bounds__(kThreads, POOL == kF32 ? 1 : 2) void shared_attention_kernel(SharedParams p) {
     extern __shared__ __align__(16) char lds[];
-    if (p.totals->key != p.key) return;  // (no plan of these sizes)
-    const int wgs = __builtin_amdgcn_readfirstlane(p.totals->shared_wgs), wg = blockIdx.x;
-    if (wg < wgs) {
-        // consecutive ranges, which read the same keys for other columns, on one XCD (work-groups go to the XCDs in turn)
-        const int r = wg % 8 * (wgs / 8) + wg / 8;
-        if (r < p.totals->shared_ranges) shared_work<POOL, D>(p, lds, r);
-    } else {
-        own_work<POOL, D>(p, lds, wg - wgs);
-    }
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Job &job = p.jobs[blockIdx.x * 4 + wave / (4 / p.parts_wg)];
+    if (job.key != p.key) return;  // (no plan of these sizes)
+    if (job.kind == kShared) shared_work<POOL, D>(p, lds, job);
+    else if (job.kind == kOwn) own_work<POOL, D>(p, lds, job);
 }
 
 // ------------------------------------------------------------------------------------------ joining the parts
-// The range whose tiles include f.
-__device__ inline int range_of(const Start *start, int n, int64_t total, int64_t f) {
-    int r = max(0, min(n - 1, (int)((double)f * n / (double)total)));
-    while (r > 0 && start[r].f > f) --r;
-    while (r + 1 < n && start[r + 1].f <= f) ++r;
-    return r;
-}
-
-// D / 4 lanes for each row and head of a sequence.
-template <bool HALF, int D>
+// D / 8 lanes for each row and head of a sequence; SPLIT: in each of the work-group's waves, which share the parts out and add up through LDS what they found.
+// Each lane looks at the maximum and sum of another part; the outputs are then weighted and summed in the parts' order, those of shared keys first, without
+// one load waiting for another.
+template <bool HALF, int D, bool SPLIT>
 __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
-    constexpr int kQuads = D / 4, kPer = kThreads / kQuads;
+    constexpr int kLanes = D / 8, kWaves = kThreads / 64, kPer = (SPLIT ? 64 : kThreads) / kLanes;
+    __shared__ float lds[SPLIT ? kWaves * kPer * (D + 4) : 1];
     const Totals t = *p.totals;
-    if (t.key != p.key) return;
     const SeqPlan s = p.seq[blockIdx.y];
-    const int item = blockIdx.x * kPer + threadIdx.x / kQuads, quad = threadIdx.x % kQuads;
-    if (item >= s.R * p.Hq) return;
-    const int i = item / p.Hq, head = item % p.Hq, kv_head = head / p.G, c = i * p.G + head % p.G;
+    const int wave = threadIdx.x >> 6, part = threadIdx.x % kLanes, sub = (SPLIT ? threadIdx.x & 63 : threadIdx.x) / kLanes;
+    const int last = s.R * p.Hq - 1, item = min((int)blockIdx.x * kPer + sub, last);
+    if (t.key != p.key || (int)blockIdx.x * kPer > last) return;
+    const bool exists = (int)blockIdx.x * kPer + sub <= last;
+    const int i = item / p.Hq, head = item - i * p.Hq, kv_head = head / p.G, g_head = head - kv_head * p.G, c = i * p.G + g_head;
     const int64_t row = s.q0 + i, at = row * p.Hq + head;
-    float m = -INFINITY, l = 0.f;
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    auto add = [&](const float *part_o, const float *part_ml, int64_t index) __attribute__((always_inline)) {
-        const floatx2 ml = *reinterpret_cast<const floatx2 *>(part_ml + index * 2);
-        const floatx4 x = *reinterpret_cast<const floatx4 *>(part_o + index * D + quad * 4);
-        if (ml[1] == 0.f) return;  // (no key of this part is seen)
-        const float m_new = fmaxf(m, ml[0]);
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new), e = __builtin_amdgcn_exp2f(ml[0] - m_new);
-        l = l * f + ml[1] * e;
-        for (int j = 0; j < 4; ++j) o[j] = o[j] * f + x[j] * e;
-        m = m_new;
-    };
+    int n_shared = 0, n_own = 0;
+    // Where the parts of each kind lie, in rows of D (and pairs of maximum and sum): the first one, and how far apart they are.
+    const char *shared_o = p.shared_whole_o, *own_o = p.own_whole_o;
+    const float *shared_ml = p.shared_whole_ml, *own_ml = p.own_whole_ml;
+    int64_t shared_at = at, own_at = at;
+    int shared_late = 0, own_late = 0;  // rows further where the first part is its range's last one, not its first
+    constexpr int kSharedStep = 2 * kBlock;
+    const int own_step = 2 * p.heads_wg * p.col_waves * kColumns;
     if (s.shared > 0) {
         const GroupPlan g = p.grp[s.group];
-        const int packed = max(0, min((int)(row - g.q0) * p.G + head % p.G, g.rows * p.G - 1)), block = packed / kBlock;
-        const int64_t all = t.shared * p.Hkv, b = t.shared * kv_head + g.base + (int64_t)block * g.key_tiles, e = b + g.key_tiles - 1;
-        const int r0 = range_of(p.shared_start, t.shared_ranges, all, b), r1 = range_of(p.shared_start, t.shared_ranges, all, e);
-        if (r0 == r1) add(p.shared_whole_o, p.shared_whole_ml, at);
-        else
-            for (int r = r0; r <= r1; ++r) add(p.shared_o, p.shared_ml, ((int64_t)2 * r + (r == r0 && p.shared_start[r].f < b)) * kBlock + packed % kBlock);
-    }
-    if (s.tiles > 0) {
-        const int cols = p.col_waves * kColumns, hi = kv_head % p.heads_wg, outer = c / cols * (p.Hkv / p.heads_wg) + kv_head / p.heads_wg;
-        const int64_t all = t.own * p.outer, b = t.own * outer + s.base, e = b + s.tiles - 1;
-        const int r0 = range_of(p.own_start, t.own_ranges, all, b), r1 = range_of(p.own_start, t.own_ranges, all, e);
-        if (r0 == r1) {
-            if (s.shared == 0) return;  // (written already)
-            add(p.own_whole_o, p.own_whole_ml, at);
-        } else {
-            for (int r = r0; r <= r1; ++r)
-                add(p.own_o, p.own_ml, (((int64_t)2 * r + (r == r0 && p.own_start[r].f < b)) * (4 / p.parts_wg) + hi * p.col_waves + c % cols / kColumns) * kColumns + c % kColumns);
+        const int packed = max(0, min((int)(row - g.q0) * p.G + g_head, g.rows * p.G - 1));
+        const int64_t b = t.shared_step * kv_head + g.base + (int64_t)(packed / kBlock) * g.key_tiles;
+        const int r = range_of(t.shared, b);
+        n_shared = range_of(t.shared, b + g.key_tiles - 1) - r + 1;
+        if (n_shared > 1) {
+            shared_o = p.shared_o;
+            shared_ml = p.shared_ml;
+            shared_at = (int64_t)r * kSharedStep + packed % kBlock;
+            shared_late = begin_of(t.shared, r) < b ? kSharedStep / 2 : 0;
         }
     }
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-    for (int j = 0; j < 4; ++j) o[j] *= inv;
-    if constexpr (HALF) {
-        const bf16x2 a = __builtin_convertvector(floatx2{o[0], o[1]}, bf16x2), b = __builtin_convertvector(floatx2{o[2], o[3]}, bf16x2);
-        *reinterpret_cast<u32x2 *>(p.out + (at * D + quad * 4) * 2) = u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
-    } else {
-        *reinterpret_cast<floatx4 *>(p.out + (at * D + quad * 4) * 4) = o;
+    if (s.tiles > 0) {
+        const int cols = p.col_waves * kColumns, c_block = c / cols, c_in = c - c_block * cols, head_block = kv_head / p.heads_wg;
+        const int64_t b = t.own_step * (c_block * (p.Hkv / p.heads_wg) + head_block) + s.base;
+        const int r = range_of(t.own, b);
+        n_own = range_of(t.own, b + s.tiles - 1) - r + 1;
+        if (n_own > 1) {
+            own_o = p.own_o;
+            own_ml = p.own_ml;
+            own_at = (int64_t)r * own_step + (kv_head - head_block * p.heads_wg) * cols + c_in;
+            own_late = begin_of(t.own, r) < b ? own_step / 2 : 0;
+        }
     }
-    if (p.lse && quad == 0) p.lse[at] = l == 0.f ? -INFINITY : m * 0.693147180559945309f + logf(l);
+    const bool written = n_own == 1 && n_shared == 0;  // (already)
+    float m = -INFINITY, l = 0.f;
+    float o[8] = {};
+    constexpr int kRowBytes = D * (HALF ? 2 : 4);
+    const int n = written ? 0 : n_shared + n_own, share = SPLIT ? (n + kWaves - 1) / kWaves : n;
+    const int begin = SPLIT ? min(n, wave * share) : 0, end = SPLIT ? min(n, begin + share) : n;
+    for (int j0 = begin; j0 < end; j0 += kLanes) {
+        const int mine = j0 + part, in_own = mine - n_shared;
+        floatx2 ml = {-INFINITY, 0.f};
+        if (mine < end)
+            ml = in_own < 0 ? reinterpret_cast<const floatx2 *>(shared_ml)[shared_at + (int64_t)mine * kSharedStep + (mine == 0 ? shared_late : 0)]
+                            : reinterpret_cast<const floatx2 *>(own_ml)[own_at + (int64_t)in_own * own_step + (in_own == 0 ? own_late : 0)];
+        if (ml[1] == 0.f) ml[0] = -INFINITY;  // (no key of this part is seen)
+        float top = ml[0];
+#pragma unroll
+        for (int step = 1; step < kLanes; step *= 2) top = fmaxf(top, __shfl_xor(top, step));
+        const float m_new = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+        const float e = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m_new);
+        float sum = ml[1] * e;
+#pragma unroll
+        for (int step = 1; step < kLanes; step *= 2) sum += __shfl_xor(sum, step);
+        l = l * f + sum;
+        for (int x = 0; x < 8; ++x) o[x] *= f;
+        m = m_new;
+        const int to = min(end, j0 + kLanes), lane0 = (int)(threadIdx.x & 63) / kLanes * kLanes;
+        // kBatch parts at a time, all asked for before the first is waited for (one behind the other they take 0.8 us each).
+        constexpr int kBatch = HALF ? 8 : 4;
+        for (int j = j0; j < to; j += kBatch) {
+            u32x4 x[kBatch][HALF ? 1 : 2];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int at_part = min(j + i, to - 1), in_own = at_part - n_shared;
+                const char *from = in_own < 0 ? shared_o + (shared_at + (int64_t)at_part * kSharedStep + (at_part == 0 ? shared_late : 0)) * kRowBytes
+                                              : own_o + (own_at + (int64_t)in_own * own_step + (in_own == 0 ? own_late : 0)) * kRowBytes;
+#pragma unroll
+                for (int y = 0; y < (HALF ? 1 : 2); ++y) x[i][y] = *reinterpret_cast<const u32x4 *>(from + part * (HALF ? 16 : 32) + 16 * y);
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const float w = __shfl(e, lane0 + min(j + i, to - 1) - j0);
+                if (j + i >= to)
+#pragma unroll
+                    for (int y = 0; y < (HALF ? 1 : 2); ++y) x[i][y] = u32x4{0, 0, 0, 0};
+                if constexpr (HALF) {
+                    const halfx8 h = __builtin_bit_cast(halfx8, x[i][0]);
+                    for (int y = 0; y < 8; ++y) o[y] = fmaf((float)h[y], w, o[y]);
+                } else {
+                    const floatx4 a = __builtin_bit_cast(floatx4, x[i][0]), b = __builtin_bit_cast(floatx4, x[i][HALF ? 0 : 1]);
+                    for (int y = 0; y < 8; ++y) o[y] = fmaf(y < 4 ? a[y % 4] : b[y % 4], w, o[y]);
+                }
+            }
+        }
+    }
+    if constexpr (SPLIT) {
+        float *const mine = lds + (wave * kPer + sub) * (D + 4);
+        for (int y = 0; y < 8; ++y) mine[y * kLanes + part] = o[y];
+        if (part == 0) *reinterpret_cast<floatx2 *>(mine + D) = floatx2{m, l};
+        __syncthreads();
+        if (wave != 0) return;
+        for (int w = 1; w < kWaves; ++w) {
+            const float *other = lds + (w * kPer + sub) * (D + 4);
+            const floatx2 ml = *reinterpret_cast<const floatx2 *>(other + D);
+            const float m_new = fmaxf(m, ml[0]);
+            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new), e = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m_new);
+            l = l * f + ml[1] * e;
+            for (int y = 0; y < 8; ++y) o[y] = o[y] * f + other[y * kLanes + part] * e;
+            m = m_new;
+        }
+    }
+    if (written || !exists) return;
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+    for (int j = 0; j < 8; ++j) o[j] *= inv;
+    if constexpr (HALF) {
+        u32x4 y;
+        for (int j = 0; j < 4; ++j) y[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{o[2 * j], o[2 * j + 1]}, bf16x2));
+        __builtin_nontemporal_store(y, reinterpret_cast<u32x4 *>(p.out + at * kRowBytes + part * 16));
+    } else {
+        *reinterpret_cast<floatx4 *>(p.out + at * kRowBytes + part * 32) = floatx4{o[0], o[1], o[2], o[3]};
+        *reinterpret_cast<floatx4 *>(p.out + at * kRowBytes + part * 32 + 16) = floatx4{o[4], o[5], o[6], o[7]};
+    }
+    if (p.lse && part == 0) p.lse[at] = l == 0.f ? -INFINITY : m * 0.693147180559945309f + logf(l);
 }
 
 // ------------------------------------------------------------------------------------------ host side
 // The workspace, piece by piece, each at a multiple of 256 bytes.
 struct Layout {
-    size_t seq, grp, own_start, shared_start, totals, own_o, own_ml, shared_o, shared_ml, own_whole_o, own_whole_ml, shared_whole_o, shared_whole_ml, bytes;
+    size_t seq, grp, jobs, totals, own_o, own_ml, shared_o, shared_ml, own_whole_o, own_whole_ml, shared_whole_o, shared_whole_ml, bytes;
 };
-Layout layout(int32_t B, int32_t total_q, int32_t groups, int32_t Hq, int32_t D) {
+Layout layout(int32_t B, int32_t total_q, int32_t groups, int32_t Hq, int32_t D, respec_dtype_t dt) {
     Layout w{};
     size_t at = 0;
     auto take = [&](size_t n) {
@@ -789,22 +1377,20 @@ Layout layout(int32_t B, int32_t total_q, int32_t groups, int32_t Hq, int32_t D)
         at += round_up(n, 256);
         return here;
     };
-    const size_t f = sizeof(float), rows = (size_t)total_q * Hq, own = (size_t)kWorkGroups * 8 * kColumns, shared = groups > 0 ? (size_t)kWorkGroups * 2 * kBlock : 0;
+    const size_t ml = 2 * sizeof(float), o = (size_t)D * (dt == RESPEC_BF16 ? 2 : 4);
+    const size_t rows = groups > 0 ? (size_t)total_q * Hq : 0, own = (size_t)kWorkGroups * 8 * kColumns, shared = groups > 0 ? (size_t)kWorkGroups * 2 * kBlock : 0;
     w.seq = take((size_t)B * sizeof(SeqPlan));
     w.grp = take((size_t)groups * sizeof(GroupPlan));
-    w.own_start = take((kMaxRanges + 1) * sizeof(Start));
-    w.shared_start = take((kWorkGroups + 1) * sizeof(Start));
+    w.jobs = take(kJobs * sizeof(Job));
     w.totals = take(sizeof(Totals));
-    w.own_ml = take(own * 2 * f);
-    w.own_o = take(own * D * f);
-    w.shared_ml = take(shared * 2 * f);
-    w.shared_o = take(shared * D * f);
-    if (groups > 0) {
-        w.own_whole_ml = take(rows * 2 * f);
-        w.own_whole_o = take(rows * D * f);
-        w.shared_whole_ml = take(rows * 2 * f);
-        w.shared_whole_o = take(rows * D * f);
-    }
+    w.own_ml = take(own * ml);
+    w.own_o = take(own * o);
+    w.shared_ml = take(shared * ml);
+    w.shared_o = take(shared * o);
+    w.own_whole_ml = take(rows * ml);
+    w.own_whole_o = take(rows * o);
+    w.shared_whole_ml = take(rows * ml);
+    w.shared_whole_o = take(rows * o);
     w.bytes = at;
     return w;
 }
@@ -818,15 +1404,22 @@ bool sizes_fit(int32_t B, int32_t total_q, int32_t groups, int32_t max_q, int32_
 template <Pool POOL, int D>
 hipError_t launch(const SharedParams &p, bool prepared, hipStream_t stream) {
     using S = Shape<POOL, D>;
-    if (!prepared) hipLaunchKernelGGL(shared_prep_kernel<S::kSharedKeys>, dim3(1), dim3(kPrepThreads), 0, stream, p);
+    if (!prepared && p.B <= kFewSeqs && p.groups <= kFewGroups)
+        hipLaunchKernelGGL((shared_prep_kernel<S::kSharedKeys, true>), dim3(kPrepGroups), dim3(kPrepThreads), 0, stream, p);
+    else if (!prepared)
+        hipLaunchKernelGGL((shared_prep_kernel<S::kSharedKeys, false>), dim3(1), dim3(kPrepThreads), 0, stream, p);
     auto *kernel = &shared_attention_kernel<POOL, D>;
     if (S::kLdsBytes > 65536) {
         const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLdsBytes);
         if (err != hipSuccess) return err;
     }
     hipLaunchKernelGGL(kernel, dim3(kWorkGroups), dim3(kThreads), S::kLdsBytes, stream, p);
-    constexpr int kPer = kThreads / (D / 4);
-    hipLaunchKernelGGL((shared_join_kernel<S::kHalf, D>), dim3((unsigned)((p.max_q * p.Hq + kPer - 1) / kPer), (unsigned)p.B), dim3(kThreads), 0, stream, p);
+    // Few rows have many parts each, which four waves share out.
+    const bool split = (int64_t)p.total_q * p.Hq <= 4096;
+    const int per = (split ? 64 : kThreads) / (D / 8);
+    const dim3 grid((unsigned)((p.max_q * p.Hq + per - 1) / per), (unsigned)p.B);
+    if (split) hipLaunchKernelGGL((shared_join_kernel<S::kHalf, D, true>), grid, dim3(kThreads), 0, stream, p);
+    else hipLaunchKernelGGL((shared_join_kernel<S::kHalf, D, false>), grid, dim3(kThreads), 0, stream, p);
     return hipGetLastError();
 }
 
@@ -852,18 +1445,22 @@ respec_status_t run(const char *name, SharedParams &p, int32_t D, int32_t page_s
     if (p.tree_mask && p.max_q > 64) return fail(RESPEC_ERR_UNSUPPORTED, "%s: a tree has at most 64 rows", name);
     if (!aligned_to(p.q, 16) || !aligned_to(p.k, 16) || !aligned_to(p.v, 16) || !aligned_to(p.out, 16))
         return fail(RESPEC_ERR_INVALID_ARG, "%s: data pointers must be 16-byte aligned", name);
-    const Layout w = layout(p.B, p.total_q, p.groups, p.Hq, D);
+    const Layout w = layout(p.B, p.total_q, p.groups, p.Hq, D, dt);
     if (!workspace || workspace_bytes < w.bytes || !aligned_to(workspace, 256))
         return fail(RESPEC_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) needed, got %zu", name, w.bytes, workspace ? workspace_bytes : (size_t)0);
     char *const base = static_cast<char *>(workspace);
     p.seq = reinterpret_cast<SeqPlan *>(base + w.seq);
     p.grp = reinterpret_cast<GroupPlan *>(base + w.grp);
-    p.own_start = reinterpret_cast<Start *>(base + w.own_start);
-    p.shared_start = reinterpret_cast<Start *>(base + w.shared_start);
+    p.jobs = reinterpret_cast<Job *>(base + w.jobs);
     p.totals = reinterpret_cast<Totals *>(base + w.totals);
-    for (const auto &[to, at] : {std::pair<float **, size_t>{&p.own_o, w.own_o}, {&p.own_ml, w.own_ml}, {&p.shared_o, w.shared_o}, {&p.shared_ml, w.shared_ml},
-                                 {&p.own_whole_o, w.own_whole_o}, {&p.own_whole_ml, w.own_whole_ml}, {&p.shared_whole_o, w.shared_whole_o}, {&p.shared_whole_ml, w.shared_whole_ml}})
-        *to = reinterpret_cast<float *>(base + at);
+    p.own_o = base + w.own_o;
+    p.shared_o = base + w.shared_o;
+    p.own_whole_o = base + w.own_whole_o;
+    p.shared_whole_o = base + w.shared_whole_o;
+    p.own_ml = reinterpret_cast<float *>(base + w.own_ml);
+    p.shared_ml = reinterpret_cast<float *>(base + w.shared_ml);
+    p.own_whole_ml = reinterpret_cast<float *>(base + w.own_whole_ml);
+    p.shared_whole_ml = reinterpret_cast<float *>(base + w.shared_whole_ml);
     p.page_shift = __builtin_ctz((unsigned)page_size);
     p.G = p.Hq / p.Hkv;
     for (p.col_waves = 1; p.col_waves < 4 && p.col_waves * kColumns < p.G * p.max_q; p.col_waves *= 2) {}
@@ -881,8 +1478,11 @@ respec_status_t run(const char *name, SharedParams &p, int32_t D, int32_t page_s
     for (const int64_t x : {(int64_t)p.B, (int64_t)p.groups, (int64_t)p.total_q, (int64_t)p.max_q, (int64_t)p.max_kv, (int64_t)p.num_pages, (int64_t)p.table_len,
                             (int64_t)page_size, (int64_t)p.Hq, (int64_t)p.Hkv, (int64_t)D, (int64_t)dt, (int64_t)pool_dt})
         p.key = (p.key ^ (uint64_t)x) * 0x100000001b3u;
+    const Knobs kn = knobs();
     p.shared_cost = 1.f;
-    p.own_cost = pool_dt == RESPEC_E4M3 ? 0.7f : 1.f;
+    p.own_cost = kn.get(&Knobs::shared_cost, dt == RESPEC_BF16 ? 200 : 100) / 100.f;
+    p.min_tiles = (int)std::max(1L, kn.get(&Knobs::shared_tiles, 2));
+    p.max_ranges = (int)std::max(1L, std::min(kn.get(&Knobs::shared_ranges, kJobs), (long)kJobs));
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     hipError_t err;
     if (pool_dt == RESPEC_E4M3) err = D == 128 ? launch<kE4m3, 128>(p, prepared, stream) : launch<kE4m3, 64>(p, prepared, stream);
@@ -933,7 +1533,7 @@ size_t respec_verify_attention_shared_workspace_bytes(int32_t B, int32_t total_q
                                                       int32_t Hkv, int32_t D, respec_dtype_t dt) {
     using namespace respec;
     if (!sizes_fit(B, total_q, num_groups, std::min(max_q_per_seq, total_q), max_kv_len, Hq, Hkv, D, dt)) return 0;
-    return layout(B, total_q, num_groups, Hq, D).bytes;
+    return layout(B, total_q, num_groups, Hq, D, dt).bytes;
 }
 
 respec_status_t respec_verify_attention_shared(const void *q, const void *k_pages, const void *v_pages, const uint8_t *k_scale, const uint8_t *v_scale,
