@@ -33,6 +33,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef s16x4 __attribute__((address_space(3))) *LdsTr;
+typedef __attribute__((address_space(3))) void *LdsTo;
+typedef const __attribute__((address_space(1))) void *GlobalFrom;
 typedef const __attribute__((address_space(4))) int32_t *ConstInts;  // (read through the scalar cache; nothing writes it meanwhile)
 
 constexpr float kRescaleSlack = 8.f;  // log2 units
@@ -119,11 +121,17 @@ struct Shape {
     static constexpr int kPoolPieces = D * kPoolSize / 16;        // of a key in the pool
     static constexpr int kLoadKeys = 64 / kPoolPieces;            // keys of a wave's load
     static constexpr int kDTiles = D / 32;
-    static constexpr int kOwnKeys = 32, kOwnLoads = kOwnKeys / kLoadKeys, kOwnBytes = 2 * kOwnKeys * kRowBytes;
+    static constexpr int kOwnKeys = 32, kOwnLoads = kOwnKeys / kLoadKeys;
+    static constexpr int kCodeBytes = kOwnKeys * D;               // 8 bits: K or V of a tile as it is, two of each to a wave, and its scales
+    static constexpr int kOwnBytes = POOL == kE4m3 ? 4 * kCodeBytes + 2 * kOwnKeys * 4 : 2 * kOwnKeys * kRowBytes;
     static constexpr int kSharedKeys = kHalf ? 64 : 32, kWaveKeys = kSharedKeys / 4;
     static constexpr int kSharedLoads = kWaveKeys / kLoadKeys, kSharedBytes = 2 * kSharedKeys * kRowBytes;
     static constexpr int kPlaces = kHalf ? 5 : 4;                 // for K or V of a tile of shared keys in LDS: three (two) of K, two of V
-    static constexpr int kLdsBytes = 4 * kOwnBytes > kPlaces * kSharedBytes / 2 ? 4 * kOwnBytes : kPlaces * kSharedBytes / 2;
+    static constexpr int kTileBytes = 2 * kOwnKeys * D * kPoolSize;  // of K and V as they are in the pool
+    static constexpr int kPairedRing = 4, kPairedHeads = POOL == kE4m3 ? 2 : 1;  // tiles in LDS where waves share them; KV heads at most
+    static constexpr int kPairedBytes = kHalf ? kPairedHeads * kPairedRing * (kTileBytes + 64 + 16) + 4 * 2 * kOwnKeys * 4 : 0;
+    static constexpr int most(int a, int b) { return a > b ? a : b; }
+    static constexpr int kLdsBytes = most(most(4 * kOwnBytes, kPlaces * kSharedBytes / 2), kPairedBytes);
     static_assert(kSharedLoads >= 1 && 16 % kLoadKeys == 0, "a wave's load lies in one page");
 };
 
@@ -383,13 +391,42 @@ struct State {  // of a wave's 32 columns
         m = -INFINITY;
         ref = l = 0.f;
     }
-    // Q^T as the B operand: a lane's column is its row, its contraction slots the pieces 2x + half of the row.
-    __device__ void load_q(const SharedParams &p, int64_t row, int head, int half) {
-        const char *from = p.q + (row * p.Hq + head) * (int64_t)S::kRowBytes + half * 16;
+    // The scores of a tile to probabilities: the maximum moves where it grows by more than 2^8, the sum is theirs before any rounding.
+    template <int NB>
+    __device__ __attribute__((always_inline)) inline void exponentials(const SharedParams &p, floatx16 (&s)[NB]) {
+        float top = s[0][0];
 #pragma unroll
-        for (int x = 0; x < S::kPieces / 2; ++x) {
-            qf[x] = *reinterpret_cast<const u32x4 *>(from + x * 32);
-        }
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int x = b == 0; x < 16; ++x) top = fmaxf(top, s[b][x]);
+        rescale(p, top);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                s[b][x] = __builtin_amdgcn_exp2f(fmaf(s[b][x], p.scale2, -ref));
+                l += s[b][x];
+            }
+    }
+    __device__ __attribute__((always_inline)) inline void rescale(const SharedParams &p, float top) {  // with the largest score that this lane has
+        top = max_of_halves(top) * p.scale2;
+        if (__ballot(top > m + kRescaleSlack) == 0) return;  // (m = -inf: any finite score)
+        const float m_new = top > m + kRescaleSlack ? top : m;
+        const float f = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        ref = m_new == -INFINITY ? 0.f : m_new;
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < S::kDTiles; ++d)
+            for (int x = 0; x < 16; ++x) o[d][x] *= f;
+    }
+    // Q^T as the B operand: a lane's column is its row, its contraction slots the pieces 2x + half of the row (CODES: as sixteen codes of K lie together,
+    // the pieces 4 (x / 2) + 2 half + x % 2).
+    template <bool CODES = false>
+    __device__ void load_q(const SharedParams &p, int64_t row, int head, int half) {
+        const char *from = p.q + (row * p.Hq + head) * (int64_t)S::kRowBytes + half * (CODES ? 32 : 16);
+#pragma unroll
+        for (int x = 0; x < S::kPieces / 2; ++x) qf[x] = *reinterpret_cast<const u32x4 *>(from + (CODES ? x / 2 * 64 + x % 2 * 16 : x * 32));
     }
     __device__ void sign_q(const SharedParams &p) {  // (apart: the loads are not waited for where they are requested)
 #pragma unroll
@@ -429,29 +466,7 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams 
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) mask(s[b], b);
-    float top = s[0][0];
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int x = 0; x < 16; ++x) top = fmaxf(top, s[b][x]);
-    top = max_of_halves(top) * p.scale2;
-    if (__ballot(top > st.m + kRescaleSlack) != 0) {  // (m = -inf: any finite score)
-        const float m_new = top > st.m + kRescaleSlack ? top : st.m;
-        const float f = st.m == m_new ? 1.f : __builtin_amdgcn_exp2f(st.m - m_new);
-        st.m = m_new;
-        st.ref = m_new == -INFINITY ? 0.f : m_new;
-        st.l *= f;
-#pragma unroll
-        for (int d = 0; d < S::kDTiles; ++d)
-            for (int x = 0; x < 16; ++x) st.o[d][x] *= f;
-    }
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-            s[b][x] = __builtin_amdgcn_exp2f(fmaf(s[b][x], p.scale2, -st.ref));
-            st.l += s[b][x];
-        }
+    st.exponentials(p, s);
     if constexpr (S::kHalf) {
         // V by transposing reads: sixteen lanes address four keys by sixteen d and receive one d of the four keys each.
         const int lane = half * 32 + col, i16 = lane & 15, v_key = half * 4 + (i16 >> 2), d0 = ((lane & 16) + 4 * (i16 & 3)) * 2;
@@ -485,141 +500,106 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams 
     }
 }
 
-// A wave's keys on their way from the pools through registers into LDS.  Its loads cover aligned runs of sixteen keys, each within a page; what
-// differs between lanes is a 32-bit offset.  Keys past the last one (`left` behind a run's first) are the last one's: they are never seen.
-enum Put { kAll = 0, kCut = 1, kSift = 2 };
-template <Pool POOL, int D, int LOADS>
+// Where sixteen keys of a sequence lie that begin at key n (a multiple of eight), all in one page: keys past the last one are the last one's, as they are
+// never seen.  The entry of the page table is asked for a step before it is needed: waited for at once it takes a sixth of a step.
+struct Run {
+    int32_t entry, slot, left;  // slot: of the first; left: keys behind it
+    __device__ __attribute__((always_inline)) inline Run(const SharedParams &p, int e0, int n, int last) {
+        n = min(n, last);
+        entry = ((ConstInts)p.page_table)[e0 + (n >> p.page_shift)];
+        slot = n & ((1 << p.page_shift) - 1);
+        left = last - n;
+    }
+    __device__ int64_t page(const SharedParams &p) const { return max(0, min(entry, p.num_pages - 1)); }
+    __device__ int64_t row(const SharedParams &p, int h) const { return ((page(p) << p.page_shift) + slot) * p.Hkv + h; }
+    __device__ int64_t scale(const SharedParams &p, int h) const { return ((page(p) * p.Hkv + h) << p.page_shift) + slot; }
+};
+struct Runs {  // of 32 keys
+    Run a, b;
+    __device__ __attribute__((always_inline)) inline Runs(const SharedParams &p, int e0, int n, int last) : a(p, e0, n, last), b(p, e0, n + 16, last) {}
+    __device__ const Run &operator[](int i) const { return i == 0 ? a : b; }
+};
+
+// A wave's 32 keys on their way from the pools through registers into LDS (fp32 and bf16).  What differs between lanes is a 32-bit offset.
+template <Pool POOL, int D>
 struct Mover {
     using S = Shape<POOL, D>;
-    static constexpr int kKeys = LOADS * S::kLoadKeys;  // 32 or fewer
-    u32x4 k[LOADS], v[LOADS];
-    uint32_t scale;  // of K of key `lane`, of V of key `lane` - kKeys (and again past these)
-    // Runs of `per_run` loads from key n0 on (a multiple of sixteen, or eight behind one), head h; the sequence's entries begin at e0, its last key is `last`.
-    template <bool NT>
-    __device__ __attribute__((always_inline)) inline void load(const SharedParams &p, int e0, int h, int n0, int last, int lane) {
-        constexpr int kRun = (16 / S::kLoadKeys) < LOADS ? 16 / S::kLoadKeys : LOADS;
-        const ConstInts table = (ConstInts)p.page_table;
-        const int scale_key = lane % kKeys;
+    static constexpr int kLoads = S::kOwnLoads, kRun = 16 / S::kLoadKeys;
+    u32x4 k[kLoads], v[kLoads];
+    __device__ __attribute__((always_inline)) inline void load(const SharedParams &p, const Runs &runs, int h, int lane) {
         const int my_key = lane / S::kPoolPieces;
         const uint32_t piece = (uint32_t)(lane % S::kPoolPieces) * 16, token = (uint32_t)p.Hkv * D * S::kPoolSize;
 #pragma unroll
-        for (int run = 0; run < LOADS / kRun; ++run) {
-            const int n = min(n0 + run * 16, last);
-            const int64_t page = max(0, min(table[e0 + (n >> p.page_shift)], p.num_pages - 1));
-            const int slot = n & ((1 << p.page_shift) - 1), left = last - n;
-            const int64_t row = ((page << p.page_shift) + slot) * p.Hkv + h;
-            const char *kp = p.k + row * (D * S::kPoolSize), *vp = p.v + row * (D * S::kPoolSize);
+        for (int run = 0; run < kLoads / kRun; ++run) {
+            const Run &r = runs[run];
+            const char *kp = p.k + r.row(p, h) * (D * S::kPoolSize), *vp = p.v + r.row(p, h) * (D * S::kPoolSize);
 #pragma unroll
             for (int j = 0; j < kRun; ++j) {
-                const int i = run * kRun + j, key = min(j * S::kLoadKeys + my_key, left);
-                const uint32_t off = (uint32_t)key * token + piece;
-                const u32x4 *a = reinterpret_cast<const u32x4 *>(kp + off), *b = reinterpret_cast<const u32x4 *>(vp + off);
-                k[i] = NT ? __builtin_nontemporal_load(a) : *a;
-                v[i] = NT ? __builtin_nontemporal_load(b) : *b;
-            }
-            if constexpr (POOL == kE4m3) {
-                const int64_t at = ((page * p.Hkv + h) << p.page_shift) + slot;
-                if (scale_key / 16 == run || kKeys <= 16) scale = (lane / kKeys % 2 ? p.v_scale : p.k_scale)[at + min(scale_key % 16, left)];
+                const uint32_t off = (uint32_t)min(j * S::kLoadKeys + my_key, r.left) * token + piece;
+                k[run * kRun + j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kp + off));  // (read once)
+                v[run * kRun + j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(vp + off));
             }
         }
     }
-    // Into the rows `key0` on of a tile.  kCut: V of keys outside [begin, end) is zero.  kSift: also, some row does not see all of these keys.  A product would
-    // carry a value of V that is not finite to it all the same, so such values count as zero here; they are added at the end to the rows that see them.
-    template <Put SIFT>
-    __device__ __attribute__((always_inline)) inline bool put(char *kt, char *vt, int key0, int lane, int n0, int begin, int end) {
-        constexpr int kOut = POOL == kE4m3 ? 2 : 1;  // pieces that a loaded one becomes
-        asm volatile("" : "+v"(lane));               // (as in attend)
-        const int my_key = lane / S::kPoolPieces, piece = lane % S::kPoolPieces * kOut, row = (key0 + my_key) * S::kRowBytes;
+    // Into a tile.  SIFT: some row does not see all of these keys.  A product would carry a value of V that is not finite to it all the same, so such values
+    // count as zero here (they are added at the end to the rows that see them), as do all of keys outside [begin, end).
+    template <bool SIFT>
+    __device__ __attribute__((always_inline)) inline bool put(char *kt, char *vt, int lane, int n0, int begin, int end) {
+        asm volatile("" : "+v"(lane));  // (as in attend)
+        const int my_key = lane / S::kPoolPieces, piece = lane % S::kPoolPieces, row = my_key * S::kRowBytes;
         // (kLoadKeys keys on, the place of a piece of K differs by an exclusive or and that of V not at all)
-        const int k_at = row + k_piece<S::kHalf, D>(key0 + my_key, piece) * 16, v_at = row + v_piece<S::kHalf, D>(my_key, piece) * 16;
+        const int k_at = row + k_piece<S::kHalf, D>(my_key, piece) * 16, v_at = row + v_piece<S::kHalf, D>(my_key, piece) * 16;
         bool bad = false;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            u32x4 a[kOut], b[kOut];
-            if constexpr (POOL == kE4m3) {
-                const int of = i * S::kLoadKeys + my_key;
-                const float sk = scale_of(__shfl((int)scale, of)), sv = scale_of(__shfl((int)scale, of + kKeys));
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    uint32_t lo, hi;
-                    values_of(k[i][w], sk, lo, hi);
-                    a[w / 2][w % 2 * 2] = lo;
-                    a[w / 2][w % 2 * 2 + 1] = hi;
-                    values_of(v[i][w], sv, lo, hi);
-                    b[w / 2][w % 2 * 2] = lo;
-                    b[w / 2][w % 2 * 2 + 1] = hi;
-                }
-            } else {
-                a[0] = k[i];
-                b[0] = v[i];
-            }
-            if constexpr (SIFT != kAll) {
+        for (int i = 0; i < kLoads; ++i) {
+            u32x4 b = v[i];
+            if constexpr (SIFT) {
                 const int n = n0 + i * S::kLoadKeys + my_key;
                 const bool none = n < begin || n >= end;
 #pragma unroll
-                for (int y = 0; y < kOut; ++y)
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const bool hi = SIFT == kSift && (b[y][w] & 0x7f800000u) == 0x7f800000u, lo = SIFT == kSift && S::kHalf && (b[y][w] & 0x7f80u) == 0x7f80u;
-                        bad |= (hi || lo) && !none;
-                        b[y][w] &= none ? 0u : (hi ? (S::kHalf ? 0xffffu : 0u) : ~0u) & (lo ? 0xffff0000u : ~0u);
-                    }
+                for (int w = 0; w < 4; ++w) {
+                    const bool hi = (b[w] & 0x7f800000u) == 0x7f800000u, lo = S::kHalf && (b[w] & 0x7f80u) == 0x7f80u;
+                    bad |= (hi || lo) && !none;
+                    b[w] &= none ? 0u : (hi ? (S::kHalf ? 0xffffu : 0u) : ~0u) & (lo ? 0xffff0000u : ~0u);
+                }
             }
-#pragma unroll
-            for (int y = 0; y < kOut; ++y) {
-                constexpr int kStep = S::kLoadKeys * S::kRowBytes;
-                *reinterpret_cast<u32x4 *>(kt + (k_at ^ (k_piece<S::kHalf, D>(i * S::kLoadKeys, y) * 16)) + i * kStep) = a[y];
-                *reinterpret_cast<u32x4 *>(vt + (v_at ^ (16 * y)) + i * kStep) = b[y];
-            }
+            constexpr int kStep = S::kLoadKeys * S::kRowBytes;
+            *reinterpret_cast<u32x4 *>(kt + (k_at ^ (k_piece<S::kHalf, D>(i * S::kLoadKeys, 0) * 16)) + i * kStep) = k[i];
+            *reinterpret_cast<u32x4 *>(vt + v_at + i * kStep) = b;
         }
         return bad;
     }
 };
 
-// A wave's accumulators times `factor` as rows of D, in bf16 (OUT) or in fp16 (parts), through LDS so that whole rows are written: COLS columns at a
-// time, the rows' pieces placed as K's are.  to(c): where column c goes, or nullptr.
-template <Pool POOL, int D, int COLS, bool OUT, typename To>
-__device__ __attribute__((always_inline)) inline void write_rows(const State<POOL, D> &st, float factor, char *area, int half, int col, To &&to) {
+// A wave's column times `factor` to `to`, a row of D in bf16 (OUT) or in fp16 (parts); nullptr: there is no such column.  The halves of the wave trade four of
+// eight d each, so that a lane writes sixteen bytes.
+template <Pool POOL, int D, bool OUT>
+__device__ __attribute__((always_inline)) inline void write_row(const State<POOL, D> &st, float factor, char *to, int half) {
     using S = Shape<POOL, D>;
-    constexpr int kRows = 64 / S::kPieces;  // that a wave moves at a time
-    int lane = half * 32 + col;
-    asm volatile("" : "+v"(lane));  // (as in attend)
-    half = lane >> 5;
-    col = lane & 31;
-    const int piece = lane % S::kPieces;
 #pragma unroll
-    for (int round = 0; round < kColumns / COLS; ++round) {
-        wave_sync();
-        if (COLS == kColumns || col / COLS == round) {
-            const int c = col % COLS;
+    for (int d = 0; d < S::kDTiles; ++d)
 #pragma unroll
-            for (int d = 0; d < S::kDTiles; ++d)
+        for (int x = 0; x < 16; x += 8) {
+            uint32_t y[4];
 #pragma unroll
-                for (int x = 0; x < 16; x += 4) {  // four d in a row
-                    const floatx2 a = {st.o[d][x] * factor, st.o[d][x + 1] * factor}, b = {st.o[d][x + 2] * factor, st.o[d][x + 3] * factor};
-                    const u32x2 y = OUT ? u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(a, bf16x2)), __builtin_bit_cast(uint32_t, __builtin_convertvector(b, bf16x2))}
-                                        : u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(a, halfx2)), __builtin_bit_cast(uint32_t, __builtin_convertvector(b, halfx2))};
-                    *reinterpret_cast<u32x2 *>(area + c * S::kRowBytes + k_piece<true, D>(c, d * 4 + x / 4) * 16 + 8 * half) = y;
-                }
+            for (int j = 0; j < 4; ++j) {
+                const floatx2 a = {st.o[d][x + 2 * j] * factor, st.o[d][x + 2 * j + 1] * factor};
+                y[j] = OUT ? __builtin_bit_cast(uint32_t, __builtin_convertvector(a, bf16x2)) : __builtin_bit_cast(uint32_t, __builtin_convertvector(a, halfx2));
+            }
+            const auto lo = __builtin_amdgcn_permlane32_swap(y[0], y[2], false, false), hi = __builtin_amdgcn_permlane32_swap(y[1], y[3], false, false);
+            const u32x4 z = {lo[0], hi[0], lo[1], hi[1]};
+            u32x4 *const at = reinterpret_cast<u32x4 *>(to + (32 * d + 2 * x + 8 * half) * 2);
+            if (to && OUT) __builtin_nontemporal_store(z, at);
+            else if (to) *at = z;  // (read soon)
         }
-        wave_sync();
-#pragma unroll
-        for (int i = 0; i < COLS / kRows; ++i) {
-            const int c = i * kRows + lane / S::kPieces;
-            const u32x4 y = *reinterpret_cast<const u32x4 *>(area + c * S::kRowBytes + k_piece<true, D>(c, piece) * 16);
-            char *const at = to(round * COLS + c);
-            if (at && OUT) __builtin_nontemporal_store(y, reinterpret_cast<u32x4 *>(at + piece * 16));
-            else if (at) *reinterpret_cast<u32x4 *>(at + piece * 16) = y;  // (read soon)
-        }
-    }
 }
 
-// A wave's columns as a part: unnormalised output, maximum and sum, to rows to(c) of `o` and `ml` (negative: there is no column c).  Outputs of bf16
+// A wave's column as a part: unnormalised output, maximum and sum, to row `to` of `o` and `ml` (negative: there is no such column).  Outputs of bf16
 // products are written in fp16, relative to their largest: (m, l, o) and (m + e, l 2^-e, o 2^-e) are the same part, and with all o 2^-e below 1 the rounding is
 // 2^-12 of each and 2^-25 of the largest, against 2^-9 of the probabilities before and of the result after (half the bytes: 256 sequences of 512 to 4,096
 // tokens at 28/4 heads over 8 bits leave 20 MB).  What is not finite stays so.
-template <Pool POOL, int D, int COLS, typename To>
-__device__ __attribute__((always_inline)) inline void write_part(const State<POOL, D> &st, float l, char *o, float *ml, char *area, int half, int col, To &&to) {
+template <Pool POOL, int D>
+__device__ __attribute__((always_inline)) inline void write_part(const State<POOL, D> &st, float l, char *o, float *ml, int half, int64_t to) {
     using S = Shape<POOL, D>;
     float m = st.m, factor = 1.f;
     if constexpr (S::kHalf) {
@@ -640,19 +620,15 @@ __device__ __attribute__((always_inline)) inline void write_part(const State<POO
         m += (float)e;
         l *= factor;
     }
-    const int64_t mine = to(col);
-    if (half == 0 && mine >= 0) *reinterpret_cast<floatx2 *>(ml + mine * 2) = floatx2{m, l};
+    if (half == 0 && to >= 0) *reinterpret_cast<floatx2 *>(ml + to * 2) = floatx2{m, l};
     if constexpr (S::kHalf) {
-        write_rows<POOL, D, COLS, false>(st, factor, area, half, col, [&](int c) __attribute__((always_inline)) {
-            const int64_t at = to(c);
-            return at < 0 ? nullptr : o + at * (D * 2);
-        });
-    } else if (mine >= 0) {
+        write_row<POOL, D, false>(st, factor, to < 0 ? nullptr : o + to * (D * 2), half);
+    } else if (to >= 0) {
 #pragma unroll
         for (int d = 0; d < S::kDTiles; ++d)
 #pragma unroll
             for (int x = 0; x < 16; x += 4)
-                *reinterpret_cast<floatx4 *>(o + (mine * D + d * 32 + 2 * x + 4 * half) * 4) = floatx4{st.o[d][x], st.o[d][x + 1], st.o[d][x + 2], st.o[d][x + 3]};
+                *reinterpret_cast<floatx4 *>(o + (to * D + d * 32 + 2 * x + 4 * half) * 4) = floatx4{st.o[d][x], st.o[d][x + 1], st.o[d][x + 2], st.o[d][x + 3]};
     }
 }
 
@@ -667,9 +643,6 @@ __device__ __attribute__((always_inline)) inline void each(F &&f) {
     each_of<N>(f, std::make_integer_sequence<int, N>{});
 }
 
-typedef __attribute__((address_space(3))) void *LdsTo;
-typedef const __attribute__((address_space(1))) void *GlobalFrom;
-
 // K or V of a tile of shared keys on its way from the pool into LDS: each wave moves a quarter of the keys, which lie in one page.  bf16: straight into
 // LDS, each lane asking for the piece that belongs where its sixteen bytes land.  8 bits: K through registers and V through LDS as it is (`to`), where each lane
 // finds again what it has asked for, to be turned into bf16; there would not be registers for both.  fp32: through registers.
@@ -681,16 +654,14 @@ struct Stage {
     u32x4 x[kDirect || kRaw ? 1 : kLoads];
     uint32_t scale;  // of the wave's key `lane`
     __device__ __attribute__((always_inline)) inline void load(const SharedParams &p, const GroupPlan &g, int h, int tile, int wave, int lane, char *to) {
-        const int last = g.shared - 1, n = min(tile * S::kSharedKeys + wave * S::kWaveKeys, last), left = last - n;
-        const int64_t page = max(0, min(((ConstInts)p.page_table)[g.e0 + (n >> p.page_shift)], p.num_pages - 1));
-        const int slot = n & ((1 << p.page_shift) - 1);
-        const char *from = (V ? p.v : p.k) + (((page << p.page_shift) + slot) * p.Hkv + h) * (D * S::kPoolSize);
+        const Run r(p, g.e0, tile * S::kSharedKeys + wave * S::kWaveKeys, g.shared - 1);
+        const char *from = (V ? p.v : p.k) + r.row(p, h) * (D * S::kPoolSize);
         const uint32_t token = (uint32_t)p.Hkv * D * S::kPoolSize;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int in_wave = i * S::kLoadKeys + lane / S::kPoolPieces, key = wave * S::kWaveKeys + in_wave, at = lane % S::kPoolPieces;
             const int piece = !kDirect ? at : V ? v_piece<S::kHalf, D>(key, at) : k_piece<S::kHalf, D>(key, at);  // (an exclusive or: its own inverse)
-            const char *mine = from + ((uint32_t)min(in_wave, left) * token + (uint32_t)piece * 16);
+            const char *mine = from + ((uint32_t)min(in_wave, r.left) * token + (uint32_t)piece * 16);
             if constexpr (kDirect)
                 __builtin_amdgcn_global_load_lds((GlobalFrom)mine, (LdsTo)(to + (wave * S::kWaveKeys + i * S::kLoadKeys) * S::kRowBytes), 16, 0, 0);
             else if constexpr (kRaw)
@@ -699,7 +670,7 @@ struct Stage {
                 x[i] = *reinterpret_cast<const u32x4 *>(mine);
         }
         if constexpr (kRaw) asm volatile("" ::: "memory");  // (the scale is asked for last: put() goes by that)
-        if constexpr (POOL == kE4m3) scale = (V ? p.v_scale : p.k_scale)[((page * p.Hkv + h) << p.page_shift) + slot + min(lane % S::kWaveKeys, left)];
+        if constexpr (POOL == kE4m3) scale = (V ? p.v_scale : p.k_scale)[r.scale(p, h) + min(lane % S::kWaveKeys, r.left)];
     }
     // What load() has asked for, into the tile (straight ones are there).  Of V, what lies past the shared keys is zero: `end` keys of the tile are shared.
     __device__ __attribute__((always_inline)) inline void put(char *tile, int wave, int lane, int end, const char *raw = nullptr) const {
@@ -758,6 +729,10 @@ __device__ __attribute__((always_inline)) inline void mask_past(floatx16 (&s)[NB
 }
 
 // The waves of the work-group meet: what they have written to LDS is there, and all but the `kLeft` loads that each has asked for last.
+template <int kLeft>
+__device__ __attribute__((always_inline)) inline void wait_for() {
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (kLeft & 15) | (kLeft >> 4) << 14);  // vmcnt(kLeft)
+}
 template <int kLeft>
 __device__ __attribute__((always_inline)) inline void meet() {
     asm volatile("" ::: "memory");
@@ -841,18 +816,6 @@ __device__ __attribute__((always_inline)) inline void shared_tiles(const SharedP
     const int i16 = lane & 15, v_key = half * 4 + (i16 >> 2), d0 = ((lane & 16) + 4 * (i16 & 3)) * 2;
     int v_at = kV + v_key * S::kRowBytes + v_piece<true, D>(v_key, d0 >> 4) * 16 + (d0 & 15);
 
-    auto rescale = [&](float top) __attribute__((always_inline)) {  // with the largest score that this lane has
-        top = max_of_halves(top) * p.scale2;
-        if (__ballot(top > st.m + kRescaleSlack) == 0) return;  // (m = -inf: any finite score)
-        const float m_new = top > st.m + kRescaleSlack ? top : st.m;
-        const float f = st.m == m_new ? 1.f : __builtin_amdgcn_exp2f(st.m - m_new);
-        st.m = m_new;
-        st.ref = m_new == -INFINITY ? 0.f : m_new;
-        st.l *= f;
-#pragma unroll
-        for (int d = 0; d < S::kDTiles; ++d)
-            for (int x = 0; x < 16; ++x) st.o[d][x] *= f;
-    };
     auto largest = [&](const floatx16(&s)[kBlocks]) __attribute__((always_inline)) {
         float top = s[0][0];
 #pragma unroll
@@ -935,7 +898,7 @@ __device__ __attribute__((always_inline)) inline void shared_tiles(const SharedP
                 mask_past(next, (t + 1) * S::kSharedKeys, half, g.shared);
                 top = largest(next);
             }
-            rescale(top);
+            st.rescale(p, top);
         } else if constexpr (!kDirect) {
             k[vPlace].put(lds + kPlace * kTile, wave, lane, S::kSharedKeys);
             fetch_k(k[vPlace], t + 4, nullptr);
@@ -974,7 +937,7 @@ __device__ __attribute__((always_inline)) inline void shared_tiles(const SharedP
                 even[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, st.qf[x]), x == 0 ? none : even[b], 0, 0, 0);
             }
         if ((t0 + 1) * S::kSharedKeys > g.shared) mask_past(even, t0 * S::kSharedKeys, half, g.shared);
-        rescale(largest(even));
+        st.rescale(p, largest(even));
     }
     meet<kDirect ? StageK::kLoads : 63>();  // (the first tile's K is read by all before it is written over)
     // As many steps in a row as bring both kinds of places around, so that they are constants.
@@ -1025,15 +988,13 @@ __device__ __attribute__((always_inline)) inline void shared_work(const SharedPa
         }
         shared_tiles(p, lds, g, h, tile, t1, column0 <= last, st);
         const bool whole = tile == 0 && t1 == g.key_tiles;
-        if (column0 <= last)
-            write_part<POOL, D, kColumns>(st, sum_of_halves(st.l), whole ? p.shared_whole_o : p.shared_o, whole ? p.shared_whole_ml : p.shared_ml,
-                                          lds + wave * (kColumns * S::kRowBytes), half, col, [&](int c) __attribute__((always_inline)) {
-                                              const int packed = column0 + c;
-                                              if (packed > last) return (int64_t)-1;
-                                              if (!whole) return ((int64_t)2 * job.range + !first) * kBlock + wave * kColumns + c;
-                                              const int i = by_g(p, packed);
-                                              return ((int64_t)g.q0 + i) * p.Hq + h * p.G + packed - i * p.G;
-                                          });
+        if (column0 <= last) {
+            int half = lane >> 5, col = lane & 31;
+            asm volatile("" : "+v"(half), "+v"(col));  // (as in attend)
+            const int packed = column0 + col, i = by_g(p, packed);
+            const int64_t to = whole ? ((int64_t)g.q0 + i) * p.Hq + h * p.G + packed - i * p.G : ((int64_t)2 * job.range + !first) * kBlock + wave * kColumns + col;
+            write_part(st, sum_of_halves(st.l), whole ? p.shared_whole_o : p.shared_o, whole ? p.shared_whole_ml : p.shared_ml, half, packed > last ? -1 : to);
+        }
         first = false;
         left -= t1 - tile;
         if (left == 0) break;
@@ -1048,7 +1009,6 @@ __device__ __attribute__((always_inline)) inline void shared_work(const SharedPa
             } while (p.grp[item].key_tiles == 0);
             g = p.grp[item];
         }
-        meet<63>();  // (the rows have been read)
     }
 }
 
@@ -1061,9 +1021,11 @@ struct OwnPart {
 
 // A wave's columns over the own keys of a sequence, or a part of them: to the output, or to where the parts are joined.
 template <Pool POOL, int D>
-__device__ __attribute__((always_inline)) inline void own_finish(const SharedParams &p, const State<POOL, D> &st, const SeqPlan &sn, const OwnPart &w, char *area) {
+__device__ __attribute__((always_inline)) inline void own_finish(const SharedParams &p, const State<POOL, D> &st, const SeqPlan &sn, const OwnPart &w) {
     using S = Shape<POOL, D>;
-    const int lane = w.half * 32 + w.col, half = w.half;
+    int half = w.half, col = w.col;
+    asm volatile("" : "+v"(half), "+v"(col));  // (as in attend)
+    const int lane = half * 32 + col;
     const float l = sum_of_halves(st.l);
     auto row_of = [&](int c) __attribute__((always_inline)) {  // the row and head of column c, as a row of the output
         const int packed = w.packed0 + c, i = by_g(p, packed);
@@ -1072,13 +1034,10 @@ __device__ __attribute__((always_inline)) inline void own_finish(const SharedPar
     char *const part_o = w.whole ? p.own_whole_o : p.own_o;
     if (w.final) {
         const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // (no visible key: zero; NaN stays)
-        const int64_t mine = row_of(w.col);
+        const int64_t mine = row_of(col);
         if (p.lse && half == 0 && mine >= 0) p.lse[mine] = l == 0.f ? -INFINITY : st.m * 0.693147180559945309f + logf(l);
         if constexpr (S::kHalf) {
-            write_rows<POOL, D, kColumns, true>(st, inv, area, half, w.col, [&](int c) __attribute__((always_inline)) {
-                const int64_t at = row_of(c);
-                return at < 0 ? nullptr : p.out + at * S::kRowBytes;
-            });
+            write_row<POOL, D, true>(st, inv, mine < 0 ? nullptr : p.out + mine * S::kRowBytes, half);
         } else if (mine >= 0) {
 #pragma unroll
             for (int d = 0; d < S::kDTiles; ++d)
@@ -1088,10 +1047,8 @@ __device__ __attribute__((always_inline)) inline void own_finish(const SharedPar
                         floatx4{st.o[d][x] * inv, st.o[d][x + 1] * inv, st.o[d][x + 2] * inv, st.o[d][x + 3] * inv};
         }
     } else {
-        write_part<POOL, D, kColumns>(st, l, part_o, w.whole ? p.own_whole_ml : p.own_ml, area, half, w.col, [&](int c) __attribute__((always_inline)) {
-            const int64_t at = row_of(c);
-            return at < 0 || w.whole ? at : w.slot + c;
-        });
+        const int64_t at = row_of(col);
+        write_part(st, l, part_o, w.whole ? p.own_whole_ml : p.own_ml, half, at < 0 || w.whole ? at : w.slot + col);
     }
     if (!w.bad) return;
     // The values that put() left out, added to what this wave has written: a column and a d of it per lane.
@@ -1152,73 +1109,376 @@ struct OwnPlace {
     __device__ int first_key() const { return (s.shared / 32 + tile) * 32; }
 };
 
-// Every wave walks a range of its own, without barriers: tiles of 32 keys, the next kAhead of them on their way into registers while this one is read from
-// the wave's part of LDS.  Neighbouring waves have neighbouring KV heads of the same keys.
+// A wave's columns in a sequence, and what each sees of the new tokens.
+struct OwnColumns {
+    int32_t packed0, begin_tile, lim;
+    uint64_t bits;  // (trees)
+    template <bool CODES, Pool POOL, int D>
+    __device__ __attribute__((always_inline)) inline void begin(const SharedParams &p, const OwnPlace &at, int packed, int kv_head, int half, int col, State<POOL, D> &st) {
+        packed0 = packed;
+        begin_tile = at.tile;
+        const int last = at.s.R * p.G - 1, c = min(packed0 + col, last), i = by_g(p, c);
+        lim = at.s.L - at.s.R + i + 1;
+        if (p.tree_mask) bits = p.tree_mask[at.s.q0 + i];
+        st.clear();
+        st.template load_q<CODES>(p, (int64_t)at.s.q0 + i, kv_head * p.G + c - i * p.G, half);
+    }
+    // Score x of a tile is key n0 + 8 (x / 4) + 4 half + x % 4.
+    __device__ __attribute__((always_inline)) inline void mask(const SharedParams &p, const SeqPlan &s, int n0, int half, floatx16 &sc) const {
+        const int before = s.L - s.R;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            const int n = n0 + 8 * (x / 4) + 4 * half + x % 4;
+            const bool sees = p.tree_mask ? n < before || (n < s.L && n - before < 64 && (bits >> (n - before) & 1)) : n < lim;
+            if (n < s.shared || !sees) sc[x] = -INFINITY;
+        }
+    }
+};
+
+// 8 bits: K and V of two tiles at a time are on their way into a wave's part of LDS as they are, each lane asking for the piece that belongs where its sixteen
+// bytes land.  They are turned into bf16 behind the reads that the products take them by: sixteen codes of a key's K, and by the transposing read of bytes
+// (sixteen lanes address eight keys by sixteen d and receive one d of the eight keys each) eight of V, whose scales go to the probabilities.  So neither
+// the registers nor LDS hold a tile twice: 96 sequences of 256 to 8,192 tokens with trees of seven rows at 40/8 heads take 178 us by registers and bf16 in LDS.
+template <int D>
+struct Codes {
+    using S = Shape<kE4m3, D>;
+    static constexpr int kLoads = S::kOwnLoads, kRun = 16 / S::kLoadKeys;
+    static __device__ int place(int key, int piece) { return D == 128 ? piece ^ ((key >> 1) & 7) : piece ^ ((key >> 2) & 3); }  // (its own inverse)
+    template <bool V>
+    static __device__ __attribute__((always_inline)) inline void load(const SharedParams &p, const Runs &runs, int h, int lane, char *to) {
+        const uint32_t token = (uint32_t)p.Hkv * D;
+#pragma unroll
+        for (int run = 0; run < kLoads / kRun; ++run) {
+            const Run &r = runs[run];
+            const char *from = (V ? p.v : p.k) + r.row(p, h) * D;
+#pragma unroll
+            for (int j = 0; j < kRun; ++j) {
+                const int in_run = j * S::kLoadKeys + lane / S::kPoolPieces;
+                const uint32_t off = (uint32_t)min(in_run, r.left) * token + (uint32_t)place(run * 16 + in_run, lane % S::kPoolPieces) * 16;
+                __builtin_amdgcn_global_load_lds((GlobalFrom)(from + off), (LdsTo)(to + (run * kRun + j) * 1024), 16, 0, 2);  // (past the caches: read once)
+            }
+        }
+    }
+    // The scale bytes of K of key `lane`, of V of key `lane` - 32.
+    static __device__ __attribute__((always_inline)) inline uint32_t load_scale(const SharedParams &p, const Runs &r, int h, int lane) {
+        const int key = lane & 31;
+        const int64_t at = key < 16 ? r.a.scale(p, h) + min(key, r.a.left) : r.b.scale(p, h) + min(key - 16, r.b.left);
+        return (lane < 32 ? p.k_scale : p.v_scale)[at];
+    }
+};
+
+// Sixteen bytes of V in LDS where some row does not see all keys: what is not finite counts as zero (it is added at the end to the rows that see it), as does all
+// of a key that is no row's (`none`).  Whether there was something not finite.
+template <bool CODES>
+__device__ inline bool sift(char *at, bool none) {
+    u32x4 x = *reinterpret_cast<const u32x4 *>(at);
+    bool bad = false;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        // (codes: a one for each byte that is 0x7f or 0xff)
+        const uint32_t nan = CODES ? ((((x[w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu
+                                   : ((x[w] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u) | ((x[w] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u);
+        bad |= nan != 0 && !none;
+        x[w] &= none ? 0u : ~nan;
+    }
+    *reinterpret_cast<u32x4 *>(at) = x;
+    return bad;
+}
+
+__device__ inline bf16x8 eight_of(uint32_t lo, uint32_t hi, float scale) {
+    u32x4 y;
+    uint32_t a, b;
+    values_of(lo, scale, a, b);
+    y[0] = a;
+    y[1] = b;
+    values_of(hi, scale, a, b);
+    y[2] = a;
+    y[3] = b;
+    return __builtin_bit_cast(bf16x8, y);
+}
+__device__ inline void lds_read() {  // what the wave has asked LDS for is there
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    asm volatile("" ::: "memory");
+}
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef i32x2 __attribute__((address_space(3))) *LdsTrBytes;
+
+// A tile of 32 keys as codes (K at `k` of `lds`, V at `v`; `scales` of K's keys, then of V's) into the state; between() once K has been read.
+template <int D, typename Between, typename Mask>
+__device__ __attribute__((always_inline)) inline void attend_codes(const SharedParams &p, State<kE4m3, D> &st, char *lds, int k, int v, const float *scales, bool active,
+                                                                   int half, int col, Between &&between, Mask &&mask) {
+    using S = Shape<kE4m3, D>;
+    typedef Codes<D> C;
+    const int lane = half * 32 + col;
+    // Where this lane reads: a key's K; of V, the row of its pair of lanes, eight bytes of the sixteen that its group receives.
+    const int v_key = 8 * ((lane & 15) >> 3) + 4 * half + ((lane & 15) >> 1) % 4;
+    int k_at = k + col * D + C::place(col, half) * 16, v_at = v + v_key * D + (lane & 1) * 8;
+    asm volatile("" : "+v"(k_at), "+v"(v_at));
+    floatx16 s[1];
+    if (active) {
+        const float k_scale = scales[col];
+        floatx16 other;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s[0][x] = other[x] = 0.f;
+#pragma unroll
+        for (int y = 0; y < D / 32; ++y) {
+            const u32x4 a = *reinterpret_cast<const u32x4 *>(lds + (k_at ^ (32 * y)));
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_of(a[0], a[1], k_scale), __builtin_bit_cast(bf16x8, st.qf[2 * y]), s[0], 0, 0, 0);
+            other = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_of(a[2], a[3], k_scale), __builtin_bit_cast(bf16x8, st.qf[2 * y + 1]), other, 0, 0, 0);
+        }
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s[0][x] += other[x];
+    }
+    between();
+    if (!active) return;
+    mask(s[0]);
+    st.exponentials(p, s);
+    u32x4 pf[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // (a power of two: nothing but the exponent moves)
+        const floatx4 vs = *reinterpret_cast<const floatx4 *>(scales + 32 + 8 * i + 4 * half);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            pf[i / 2][i % 2 * 2 + j] =
+                __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{s[0][4 * i + 2 * j] * vs[2 * j], s[0][4 * i + 2 * j + 1] * vs[2 * j + 1]}, bf16x2));
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int d = 0; d < S::kDTiles; ++d) {
+            const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LdsTrBytes)(lds + v_at + i * 16 * D + C::place(i * 16 + v_key, 2 * d + ((lane >> 4) & 1)) * 16));
+            st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_of((uint32_t)c[0], (uint32_t)c[1], 1.f), __builtin_bit_cast(bf16x8, pf[i]), st.o[d], 0, 0, 0);
+        }
+}
+
+// Every wave walks a range of its own, without barriers, in tiles of 32 keys.  Neighbouring waves have neighbouring KV heads of the same keys.
 template <Pool POOL, int D>
 __device__ __attribute__((always_inline)) inline void own_work(const SharedParams &p, char *lds, const Job &job) {
     using S = Shape<POOL, D>;
-    constexpr int kAhead = POOL == kE4m3 ? 2 : 1;
+    constexpr bool kCodes = POOL == kE4m3;
+    constexpr int kAhead = kCodes ? 2 : 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int half = lane >> 5, col = lane & 31;
     const int cw = wave % p.col_waves, hi = wave / p.col_waves % p.heads_wg, n_tiles = job.tiles;
     const int head_groups = p.Hkv / p.heads_wg;
-    char *const kt = lds + wave * S::kOwnBytes, *const vt = kt + S::kOwnBytes / 2;
+    const int at0 = wave * S::kOwnBytes;  // of the wave's part of LDS
+    char *const mine = lds + at0;
     OwnPlace now{job.outer, job.item, job.tile, job.s}, ahead = now;
     State<POOL, D> st;
-    Mover<POOL, D, S::kOwnLoads> mover[kAhead];
-    auto fetch = [&](Mover<POOL, D, S::kOwnLoads> &m, int f) __attribute__((always_inline)) {  // the tile that is f-th of this range
-        m.template load<true>(p, ahead.s.e0, ahead.outer % head_groups * p.heads_wg + hi, ahead.first_key(), ahead.s.L - 1, lane);
-        ahead.next(p, f + 1 < n_tiles);
-    };
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-        if (i < n_tiles) fetch(mover[i], i);
+    OwnColumns cols{};
     bool fresh = true, first = true, bad = false;
-    int lim = 0, packed0 = 0, begin_tile = 0;
-    uint64_t bits = 0;
-    auto step = [&](Mover<POOL, D, S::kOwnLoads> &m, int f) __attribute__((always_inline)) {
-        const SeqPlan sn = now.s;
-        const int tile = now.tile;
-        const int kv_head = now.outer % head_groups * p.heads_wg + hi;
-        const int n0 = now.first_key(), before = sn.L - sn.R;  // keys before the new tokens (negative: the first rows see none)
-        const bool special = n0 < sn.shared || n0 + 32 > before + (p.tree_mask ? 0 : 1);
-        if (fresh) {
-            packed0 = (now.outer / head_groups * p.col_waves + cw) * kColumns;
-            begin_tile = tile;
-            const int last = sn.R * p.G - 1, c = min(packed0 + col, last), i = by_g(p, c);
-            lim = before + i + 1;
-            if (p.tree_mask) bits = p.tree_mask[sn.q0 + i];
-            st.clear();
-            st.load_q(p, (int64_t)sn.q0 + i, kv_head * p.G + c - i * p.G, half);
-        }
-        if (special) bad |= m.template put<kSift>(kt, vt, 0, lane, n0, sn.shared, sn.L);
-        else m.template put<kAll>(kt, vt, 0, lane, 0, 0, 0);
-        if (fresh) st.sign_q(p);
-        if (f + kAhead < n_tiles) fetch(m, f + kAhead);
-        fresh = now.next(p, f + 1 < n_tiles);
-        wave_sync();
-        if (packed0 < sn.R * p.G)  // (uniform)
-            attend<POOL, D, 1>(p, st, lds, wave * S::kOwnBytes, wave * S::kOwnBytes + S::kOwnBytes / 2, half, col, [&](floatx16 &sc, int) __attribute__((always_inline)) {
-                if (!special) return;
-#pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    const int n = n0 + 8 * (x / 4) + 4 * half + x % 4;
-                    const bool sees = p.tree_mask ? n < before || (n < sn.L && n - before < 64 && (bits >> (n - before) & 1)) : n < lim;
-                    if (n < sn.shared || !sees) sc[x] = -INFINITY;
-                }
-            });
-        wave_sync();
-        if (!fresh && f + 1 < n_tiles) return;
-        const bool whole = begin_tile == 0 && tile + 1 == sn.tiles;
-        if (packed0 < sn.R * p.G)
-            own_finish<POOL, D>(p, st, sn, OwnPart{kv_head, packed0, begin_tile, n0, half, col, whole, whole && sn.shared == 0, __ballot(bad) != 0,
-                                                   (((int64_t)2 * job.range + !first) * (4 / p.parts_wg) + hi * p.col_waves + cw) * kColumns}, kt);
+    auto head_of = [&](const OwnPlace &x) __attribute__((always_inline)) { return x.outer % head_groups * p.heads_wg + hi; };
+    auto look = [&]() __attribute__((always_inline)) { return Runs(p, ahead.s.e0, ahead.first_key(), ahead.s.L - 1); };
+    Runs runs = look();  // of the next tile to fetch
+    auto begin = [&]() __attribute__((always_inline)) {
+        cols.template begin<kCodes>(p, now, (now.outer / head_groups * p.col_waves + cw) * kColumns, head_of(now), half, col, st);
+    };
+    auto finish = [&](const SeqPlan &sn, int tile, int n0, int kv_head) __attribute__((always_inline)) {  // after the sequence's or the range's last tile
+        const bool whole = cols.begin_tile == 0 && tile + 1 == sn.tiles;
+        if (cols.packed0 < sn.R * p.G)
+            own_finish<POOL, D>(p, st, sn, OwnPart{kv_head, cols.packed0, cols.begin_tile, n0, half, col, whole, whole && sn.shared == 0, __ballot(bad) != 0,
+                                                   (((int64_t)2 * job.range + !first) * (4 / p.parts_wg) + hi * p.col_waves + cw) * kColumns});
         bad = first = false;
     };
-    for (int f = 0; f < n_tiles; f += kAhead) {
+    if constexpr (!kCodes) {
+        char *const kt = mine, *const vt = mine + S::kOwnBytes / 2;
+        Mover<POOL, D> mover;
+        auto fetch = [&](int f) __attribute__((always_inline)) {  // the tile that is f-th of this range, on its way while the one before it is read
+            mover.load(p, runs, head_of(ahead), lane);
+            ahead.next(p, f + 1 < n_tiles);
+            runs = look();
+        };
+        fetch(0);
+        for (int f = 0; f < n_tiles; ++f) {
+            const SeqPlan sn = now.s;
+            const int tile = now.tile, kv_head = head_of(now), n0 = now.first_key();
+            const bool special = n0 < sn.shared || n0 + 32 > sn.L - sn.R + (p.tree_mask ? 0 : 1);  // some row does not see all of its keys
+            if (fresh) begin();
+            if (special) bad |= mover.template put<true>(kt, vt, lane, n0, sn.shared, sn.L);
+            else mover.template put<false>(kt, vt, lane, 0, 0, 0);
+            if (fresh) st.sign_q(p);
+            if (f + 1 < n_tiles) fetch(f + 1);
+            fresh = now.next(p, f + 1 < n_tiles);
+            wave_sync();
+            if (cols.packed0 < sn.R * p.G)  // (uniform)
+                attend<POOL, D, 1>(p, st, lds, at0, at0 + S::kOwnBytes / 2, half, col, [&](floatx16 &sc, int) __attribute__((always_inline)) {
+                    if (special) cols.mask(p, sn, n0, half, sc);
+                });
+            wave_sync();
+            if (fresh || f + 1 == n_tiles) finish(sn, tile, n0, kv_head);
+        }
+    } else {
+        typedef Codes<D> C;
+        float *const scales = reinterpret_cast<float *>(mine + 4 * S::kCodeBytes);  // of K of the tile's keys, and of V
+        uint32_t sc_byte[2] = {0, 0};
+        auto fetch_k = [&](int f) __attribute__((always_inline)) {
+            C::template load<false>(p, runs, head_of(ahead), lane, mine + f % 2 * S::kCodeBytes);
+        };
+        auto fetch_v = [&](int f, uint32_t &byte) __attribute__((always_inline)) {  // (and the scales, last: a step goes by them)
+            C::template load<true>(p, runs, head_of(ahead), lane, mine + (2 + f % 2) * S::kCodeBytes);
+            asm volatile("" ::: "memory");
+            byte = C::load_scale(p, runs, head_of(ahead), lane);
+            ahead.next(p, f + 1 < n_tiles);
+            runs = look();
+        };
+        fetch_k(0);
+        begin();
+        fetch_v(0, sc_byte[0]);
+        if (1 < n_tiles) {
+            fetch_k(1);
+            fetch_v(1, sc_byte[1]);
+        }
+        auto step = [&](auto place_, int f) __attribute__((always_inline)) {
+            constexpr int kPlace = decltype(place_)::value;
+            const SeqPlan sn = now.s;
+            const int tile = now.tile, kv_head = head_of(now), n0 = now.first_key();
+            const bool special = n0 < sn.shared || n0 + 32 > sn.L - sn.R + (p.tree_mask ? 0 : 1);
+            if (fresh && f > 0) begin();
+            asm volatile("" ::"v"(sc_byte[kPlace]) : "memory");  // (loads come back in order: the tile is there)
+            char *const vt = mine + (2 + kPlace) * S::kCodeBytes;
+            float scale = scale_of((int)sc_byte[kPlace]);
+            if (special) {
+                for (int i = 0; i < S::kOwnLoads; ++i) {
+                    const int n = n0 + i * S::kLoadKeys + lane / S::kPoolPieces;
+                    bad |= sift<true>(vt + i * 1024 + lane * 16, n < sn.shared || n >= sn.L);
+                }
+                if (lane >= 32 && (n0 + lane - 32 < sn.shared || n0 + lane - 32 >= sn.L)) scale = 0.f;
+            }
+            scales[lane] = scale;
+            if (fresh) st.sign_q(p);
+            fresh = now.next(p, f + 1 < n_tiles);
+            wave_sync();
+            const bool active = cols.packed0 < sn.R * p.G;
+            attend_codes<D>(p, st, mine, kPlace * S::kCodeBytes, (2 + kPlace) * S::kCodeBytes, scales, active, half, col,
+                            [&]() __attribute__((always_inline)) {
+                                if (f + 2 < n_tiles) {
+                                    lds_read();  // (K, before its place is written over)
+                                    fetch_k(f + 2);
+                                }
+                            },
+                            [&](floatx16 &sc) __attribute__((always_inline)) {
+                                if (special) cols.mask(p, sn, n0, half, sc);
+                            });
+            if (f + 2 < n_tiles) {
+                lds_read();
+                fetch_v(f + 2, sc_byte[kPlace]);
+            }
+            if (fresh || f + 1 == n_tiles) finish(sn, tile, n0, kv_head);
+        };
+        for (int f = 0; f < n_tiles; f += 2) {
+            step(std::integral_constant<int, 0>{}, f);
+            if (f + 1 < n_tiles) step(std::integral_constant<int, 1>{}, f + 1);
+        }
+    }
+}
+
+// More than 32 columns to a KV head: CW waves with 32 of them each walk one range together and share its tiles, which lie in LDS as they do in the pool (a tile
+// that each loaded for itself would be asked for CW times, and a compute unit can only have so much on its way: 96 sequences of 256 to 8,192 tokens with trees
+// of seven rows at 40/8 heads over 8 bits took 160 us).  All of the work-group's waves, on 4 / CW heads, go from tile to tile at the same time: a step begins
+// with a barrier, then asks for the tile three further on, in the place of the one that was read in the step before.
+template <Pool POOL, int D, int CW>
+__device__ __attribute__((always_inline)) inline void paired_work(const SharedParams &p, char *lds, const Job &job) {
+    using S = Shape<POOL, D>;
+    constexpr bool kCodes = POOL == kE4m3;
+    constexpr int kRing = S::kPairedRing, kHeads = 4 / CW, kLoads = 2 * S::kOwnLoads / CW, kGroup = kLoads + kCodes, kRun = 16 / S::kLoadKeys;  // (of K and V, of a wave)
+    static_assert(kHeads <= S::kPairedHeads && kLoads >= 1, "the tiles fit");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int half = lane >> 5, col = lane & 31, cw = wave % CW, hi = wave / CW, n_tiles = job.tiles, head_groups = p.Hkv / kHeads;
+    char *const ring = lds + hi * kRing * S::kTileBytes;
+    char *const bytes = lds + kHeads * kRing * S::kTileBytes + hi * kRing * 64;                                // scales of K and V of each tile
+    int *const flags = reinterpret_cast<int *>(lds + kHeads * kRing * (S::kTileBytes + 64)) + hi * kRing;       // whether V of a tile held something not finite
+    float *const scales = reinterpret_cast<float *>(lds + kHeads * kRing * (S::kTileBytes + 64 + 16)) + wave * 2 * S::kOwnKeys;
+    OwnPlace now{job.outer, job.item, job.tile, job.s}, ahead = now;
+    State<POOL, D> st;
+    OwnColumns cols{};
+    bool fresh = true, first = true, bad = false;
+    auto head_of = [&](const OwnPlace &x) __attribute__((always_inline)) { return x.outer % head_groups * kHeads + hi; };
+    auto look = [&]() __attribute__((always_inline)) { return Runs(p, ahead.s.e0, ahead.first_key(), ahead.s.L - 1); };
+    Runs r = look();  // of the next tile to fetch
+    auto begin = [&]() __attribute__((always_inline)) {
+        cols.template begin<kCodes>(p, now, (now.outer / head_groups * CW + cw) * kColumns, head_of(now), half, col, st);
+    };
+    // Load i of a tile's is its wave's i / CW-th, for K and then for V; keys run * 16 + j * kLoadKeys on.
+    auto fetch = [&](int f) __attribute__((always_inline)) {
+        const int h = head_of(ahead);
+        char *const to = ring + f % kRing * S::kTileBytes;
+        const uint32_t token = (uint32_t)p.Hkv * D * S::kPoolSize;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-            if (f + i < n_tiles) step(mover[i], f + i);
+        for (int y = 0; y < kLoads; ++y) {
+            const int i = y * CW + cw, at = i % S::kOwnLoads, run = at / kRun, in_run = at % kRun * S::kLoadKeys + lane / S::kPoolPieces, key = run * 16 + in_run;
+            const bool is_v = i >= S::kOwnLoads;
+            const int64_t row = run == 0 ? r[0].row(p, h) : r[1].row(p, h);
+            const char *from = (is_v ? p.v : p.k) + row * (D * S::kPoolSize);
+            const int piece = lane % S::kPoolPieces;
+            int place;
+            if constexpr (kCodes) place = Codes<D>::place(key, piece);
+            else place = is_v ? v_piece<true, D>(key, piece) : k_piece<true, D>(key, piece);
+            const uint32_t off = (uint32_t)min(in_run, run == 0 ? r[0].left : r[1].left) * token + (uint32_t)place * 16;
+            __builtin_amdgcn_global_load_lds((GlobalFrom)(from + off), (LdsTo)(to + i * 1024), 16, 0, 2);
+        }
+        if constexpr (kCodes)  // sixteen lanes with four scales each: K's of both runs, V's of both (those past the last key are not used)
+            if (lane < 16) {
+                const int64_t at = (lane & 4 ? r[1].scale(p, h) - (r[1].slot & 15) : r[0].scale(p, h) - (r[0].slot & 15)) + (lane & 3) * 4;
+                __builtin_amdgcn_global_load_lds((GlobalFrom)((lane & 8 ? p.v_scale : p.k_scale) + at), (LdsTo)(bytes + f % kRing * 64), 4, 0, 0);
+            }
+        ahead.next(p, f + 1 < n_tiles);
+        r = look();
+    };
+    if (lane < kRing && cw == 0) flags[lane] = 0;
+    fetch(0);
+    begin();
+    if (1 < n_tiles) fetch(1);
+    if (2 < n_tiles) fetch(2);
+    meet<63>();
+    for (int f = 0; f < n_tiles; ++f) {
+        const SeqPlan sn = now.s;
+        const int tile = now.tile, kv_head = head_of(now), n0 = now.first_key(), place = f % kRing;
+        const bool special = n0 < sn.shared || n0 + 32 > sn.L - sn.R + (p.tree_mask ? 0 : 1);  // some row does not see all of its keys
+        char *const here = ring + place * S::kTileBytes, *const v_here = here + S::kTileBytes / 2;
+        // This wave's loads of the tile are there, those of the next two may not be.
+        asm volatile("" ::: "memory");
+        if (f + 2 < n_tiles) wait_for<2 * kGroup>();
+        else if (f + 1 < n_tiles) wait_for<kGroup>();
+        else wait_for<0>();
+        asm volatile("" ::: "memory");
+        if (special) {
+            bool mine = false;
+#pragma unroll
+            for (int y = 0; y < kLoads; ++y) {
+                const int i = y * CW + cw, key = (i % S::kOwnLoads) * S::kLoadKeys + lane / S::kPoolPieces;
+                if (i >= S::kOwnLoads) mine |= sift<kCodes>(here + i * 1024 + lane * 16, n0 + key < sn.shared || n0 + key >= sn.L);
+            }
+            if (mine) flags[place] = 1;
+        }
+        meet<63>();  // (the tile is there, and the one before has been read)
+        if (fresh && f > 0) begin();
+        if (f + 3 < n_tiles) fetch(f + 3);
+        if (special) bad |= flags[place] != 0;
+        if (cw == 0 && lane == 0) flags[(f + 2) % kRing] = 0;
+        const bool active = cols.packed0 < sn.R * p.G;  // (uniform)
+        if (fresh) st.sign_q(p);
+        fresh = now.next(p, f + 1 < n_tiles);
+        auto mask = [&](floatx16 &sc) __attribute__((always_inline)) {
+            if (special) cols.mask(p, sn, n0, half, sc);
+        };
+        if constexpr (kCodes) {
+            float scale = scale_of((int)reinterpret_cast<const uint8_t *>(bytes)[place * 64 + lane]);
+            if (special && lane >= 32 && (n0 + lane - 32 < sn.shared || n0 + lane - 32 >= sn.L)) scale = 0.f;
+            scales[lane] = scale;
+            wave_sync();
+            attend_codes<D>(p, st, here, 0, S::kTileBytes / 2, scales, active, half, col, []() {}, mask);
+            wave_sync();
+        } else if (active) {
+            const int at = (int)(here - lds);
+            attend<POOL, D, 1>(p, st, lds, at, at + S::kTileBytes / 2, half, col, [&](floatx16 &sc, int) __attribute__((always_inline)) { mask(sc); });
+        }
+        if (!fresh && f + 1 < n_tiles) continue;
+        const bool whole = cols.begin_tile == 0 && tile + 1 == sn.tiles;
+        if (active)
+            own_finish<POOL, D>(p, st, sn, OwnPart{kv_head, cols.packed0, cols.begin_tile, n0, half, col, whole, whole && sn.shared == 0, __ballot(bad) != 0,
+                                                   (((int64_t)2 * job.range + !first) * 4 + hi * CW + cw) * kColumns});
+        bad = first = false;
     }
 }
 
@@ -1229,7 +1489,13 @@ __global__ __launch_bounds__(kThreads, POOL == kF32 ? 1 : 2) void shared_attenti
     const Job &job = p.jobs[blockIdx.x * 4 + wave / (4 / p.parts_wg)];
     if (job.key != p.key) return;  // (no plan of these sizes)
     if (job.kind == kShared) shared_work<POOL, D>(p, lds, job);
-    else if (job.kind == kOwn) own_work<POOL, D>(p, lds, job);
+    else if (job.kind == kOwn) {
+        if constexpr (POOL == kE4m3) {
+            if (p.col_waves == 4) return paired_work<POOL, D, 4>(p, lds, job);
+            if (p.col_waves == 2) return paired_work<POOL, D, 2>(p, lds, job);
+        }
+        own_work<POOL, D>(p, lds, job);
+    }
 }
 
 // ------------------------------------------------------------------------------------------ joining the parts
@@ -1443,6 +1709,7 @@ respec_status_t run(const char *name, SharedParams &p, int32_t D, int32_t page_s
     if (!sizes_fit(p.B, p.total_q, p.groups, p.max_q, p.max_kv, p.Hq, p.Hkv, D, dt) || p.B > 65535 || (int64_t)p.Hkv * D * (dt == RESPEC_BF16 ? 2 : 4) > (1 << 24))
         return fail(RESPEC_ERR_UNSUPPORTED, "%s: at most 256 rows and heads to a KV head (G * max_q_per_seq), 65,535 sequences, 2^30 rows and heads", name);
     if (p.tree_mask && p.max_q > 64) return fail(RESPEC_ERR_UNSUPPORTED, "%s: a tree has at most 64 rows", name);
+    if (!aligned_to(p.k_scale, 4) || !aligned_to(p.v_scale, 4)) return fail(RESPEC_ERR_INVALID_ARG, "%s: scales must be 4-byte aligned", name);
     if (!aligned_to(p.q, 16) || !aligned_to(p.k, 16) || !aligned_to(p.v, 16) || !aligned_to(p.out, 16))
         return fail(RESPEC_ERR_INVALID_ARG, "%s: data pointers must be 16-byte aligned", name);
     const Layout w = layout(p.B, p.total_q, p.groups, p.Hq, D, dt);
@@ -1463,7 +1730,13 @@ respec_status_t run(const char *name, SharedParams &p, int32_t D, int32_t page_s
     p.shared_whole_ml = reinterpret_cast<float *>(base + w.shared_whole_ml);
     p.page_shift = __builtin_ctz((unsigned)page_size);
     p.G = p.Hq / p.Hkv;
-    for (p.col_waves = 1; p.col_waves < 4 && p.col_waves * kColumns < p.G * p.max_q; p.col_waves *= 2) {}
+    // Columns of a KV head to waves: up to 32 in one, whose neighbours have other heads or keys; more in two (8 bits, as the tiles of two heads fit) or four that
+    // share their tiles.
+    const int columns = p.G * p.max_q;
+    if (pool_dt != RESPEC_E4M3)
+        for (p.col_waves = 1; p.col_waves < 4 && p.col_waves * kColumns < columns; p.col_waves *= 2) {}
+    else
+        p.col_waves = columns <= kColumns ? 1 : columns <= 2 * kColumns && p.Hkv % 2 == 0 ? 2 : 4;
     for (p.heads_wg = 4 / p.col_waves; p.Hkv % p.heads_wg != 0; p.heads_wg /= 2) {}
     p.parts_wg = 4 / (p.col_waves * p.heads_wg);
     p.outer = p.Hkv / p.heads_wg * ((p.G * p.max_q + p.col_waves * kColumns - 1) / (p.col_waves * kColumns));
