@@ -92,7 +92,7 @@ struct SharedParams {
     uint32_t g_mul, g_shift;                // of a division by G
     uint32_t q_and, q_xor;                  // on the bits of q: a negative scale is taken out of it, a zero one makes it zero
     float scale2;                           // |sm_scale| * log2(e)
-    float shared_cost, own_cost;            // of a work-group's tile, in the same unit
+    float own_cost;                         // of a work-group's tile of own keys, against one of shared keys
     int32_t max_ranges, min_tiles;
     uint64_t key;
     SeqPlan *seq;
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
     t.shared_step = shared;
     const int64_t all_own = own * p.outer, all_shared = shared * p.Hkv;
     if (all_shared > 0) {
-        const float cost_s = (float)all_shared * p.shared_cost, cost_o = (float)all_own / p.parts_wg * p.own_cost;
+        const float cost_s = (float)all_shared, cost_o = (float)all_own / p.parts_wg * p.own_cost;
         const int even = (int)(kWorkGroups / 8 * (cost_s / (cost_s + cost_o)) + 0.5f) * 8;
         t.shared_wgs = all_own > 0 ? max(8, min(even, kWorkGroups - 8)) : kWorkGroups;
     }
@@ -1752,9 +1752,13 @@ respec_status_t run(const char *name, SharedParams &p, int32_t D, int32_t page_s
                             (int64_t)page_size, (int64_t)p.Hq, (int64_t)p.Hkv, (int64_t)D, (int64_t)dt, (int64_t)pool_dt})
         p.key = (p.key ^ (uint64_t)x) * 0x100000001b3u;
     const Knobs kn = knobs();
-    p.shared_cost = 1.f;
-    p.own_cost = kn.get(&Knobs::shared_cost, dt == RESPEC_BF16 ? 200 : 100) / 100.f;
-    p.min_tiles = (int)std::max(1L, kn.get(&Knobs::shared_tiles, 2));
+    // What a work-group's tile of own keys takes against one of shared keys.  Over bf16 32 groups of 8 sequences at 28/4 heads (two layers) took 182, 178, 169 and
+    // 175 us with 120, 160, 220 and 250 hundredths, 64 single tokens 62, 58, 51 and 49; over 8 bits 8 groups of 16 at 40/8 took 182, 160, 168 and 177 us
+    // with 120, 160, 200 and 220.
+    p.own_cost = kn.get(&Knobs::shared_cost, pool_dt == RESPEC_E4M3 ? 165 : dt == RESPEC_BF16 ? 230 : 100) / 100.f;
+    // Tiles of own keys that make a range of their own: fp32 takes longer for one than a part more takes to join (8 sequences of up to 40 tokens: 20 us with one,
+    // 26 with two), bf16 products do not (8 sequences of 512 to 8,192 tokens at 16/2 heads over 8 bits: 27 us with one, 24 with two, 26 with three).
+    p.min_tiles = (int)std::max(1L, kn.get(&Knobs::shared_tiles, dt == RESPEC_F32 ? 1 : 2));
     p.max_ranges = (int)std::max(1L, std::min(kn.get(&Knobs::shared_ranges, kJobs), (long)kJobs));
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     hipError_t err;
