@@ -52,23 +52,22 @@ __device__ inline void store8(char *to, const float (&x)[8]) {
 
 // D / 16 lanes hold a head, each two pieces of eight entries: for pairs (i, i + rotary / 2) a piece and the one with its partners, so that no
 // entry leaves its lane but in the sum of squares and the largest magnitude.  A wave goes through the heads of a row, 1024 / D at a time, with the sines
-// and cosines of its position worked out once.  An angle is position * inv_freq, in turns and in 64 bits until its whole turns are taken off (in 32 bits a
+// and cosines of its position worked out once, an angle in each lane (rotary / 2 <= 64
+// of them: 7.6 us for four rows each of 256 sequences at 28/4 heads, 9.2 with eight angles in each of eight lanes' groups).  An angle is position * inv_freq, in turns and in 64 bits until its whole turns are taken off (in 32 bits a
 // position of 100,000 would leave an error of 0.004).
 template <bool BF16, bool E4M3, int D>
 __global__ __launch_bounds__(kThreads) void norm_rope_append_kernel(WriteParams p) {
     constexpr int kLanes = D / 16, kHeads = 64 / kLanes;  // lanes of a head, heads of a wave
     constexpr int kSize = BF16 ? 2 : 4, kRaw = BF16 ? 1 : 2;
-    Tile t;
-    if (!find_tile(p.q_indptr, p.B, p.total_q, p.max_q, 1, p.rows, blockIdx.x, t)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane % kLanes, mine = lane / kLanes;
-    const int row = t.index * p.rows + wave % p.rows, part = wave / p.rows, parts = kWaves / p.rows;
-    if (row >= t.R) return;
+    const int part = wave / p.rows, parts = kWaves / p.rows;
     const int heads = p.Hq + 2 * p.Hkv, units = (heads + kHeads - 1) / kHeads;
-    const int64_t token = t.q0 + row;
+    const int64_t token = (int64_t)blockIdx.x * p.rows + wave % p.rows;
+    if (token >= p.total_q) return;
 
     const int pairs = p.interleaved ? 0 : p.rotary / 16;  // pieces whose partners are other pieces
-    const int a = p.interleaved ? 2 * c : c < pairs ? c : 2 * c, b = p.interleaved || c >= pairs ? a + 1 : c + pairs;
+    const int one = p.interleaved ? 2 * c : c < pairs ? c : 2 * c, two = p.interleaved || c >= pairs ? one + 1 : c + pairs;
     const bool turns = 8 * c < p.rotary / 2;  // (whole lanes: rotary is a multiple of 16)
 
     auto source = [&](int h) __attribute__((always_inline)) {
@@ -80,31 +79,52 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_kernel(WriteParams 
         const char *from = source(min(u * kHeads + mine, heads - 1));
 #pragma unroll
         for (int i = 0; i < kRaw; ++i) {
-            raw[0][i] = *reinterpret_cast<const u32x4 *>(from + a * 8 * kSize + i * 16);
-            raw[1][i] = *reinterpret_cast<const u32x4 *>(from + b * 8 * kSize + i * 16);
+            raw[0][i] = *reinterpret_cast<const u32x4 *>(from + one * 8 * kSize + i * 16);
+            raw[1][i] = *reinterpret_cast<const u32x4 *>(from + two * 8 * kSize + i * 16);
         }
     };
-    if (part < units) load(part);
+    if (part < units) load(part);  // (on its way while the sequence is looked for)
+
+    // The last sequence that begins at or before the token: 64 places are looked at at a time (four rows each of 256 sequences at
+    // 28/4 heads: 9.2 us, and 10.4 with the sequences' rows counted up 64 sequences after the other).
+    int b = 0;
+    for (int end = p.B; end - b > 1;) {
+        const int step = (end - b + 63) / 64, at = b + lane * step;
+        const int found = __popcll(__ballot(at < end && p.q_indptr[min(at, end - 1)] <= token));
+        b += max(0, found - 1) * step;
+        end = min(end, b + step);
+    }
+    const int q0 = max(0, p.q_indptr[b]), R = min(p.q_indptr[b + 1], p.total_q) - q0;
+    const int64_t row = token - q0;
+    if (row < 0 || row >= min(R, p.max_q)) return;
 
     // Where K and V go: -1 if the sequence's pages do not have the place.
-    const int64_t pos = (int64_t)p.kv_len[t.b] - (min(p.q_indptr[t.b + 1], p.total_q) - t.q0) + row;
+    const int64_t pos = (int64_t)p.kv_len[b] - R + row;
     int64_t page = -1;
     {
-        const int e0 = max(0, min(p.page_indptr[t.b], p.table_len)), held = max(0, min(p.page_indptr[t.b + 1], p.table_len) - e0);
+        const int e0 = max(0, min(p.page_indptr[b], p.table_len)), held = max(0, min(p.page_indptr[b + 1], p.table_len) - e0);
         if (pos >= 0 && pos < (int64_t)held << p.page_shift) {
             const int32_t id = p.page_table[e0 + (pos >> p.page_shift)];
             if ((uint32_t)id < (uint32_t)p.num_pages) page = id;
         }
     }
     const int slot = (int)(pos & ((1 << p.page_shift) - 1));
+    // Sines and cosines: each lane works one angle out, and takes its eight through LDS.
+    __shared__ __align__(16) float angles[kWaves][2][64];
     float cs[8], sn[8];
-    if (turns) {
-        const double at = (double)(p.positions ? (int64_t)p.positions[token] : pos) * 0.15915494309189533577;  // 1 / 2 pi
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const double turn = at * (double)p.inv_freq[8 * c + j];
-            sincospif((float)(2.0 * (turn - rint(turn))), &sn[j], &cs[j]);
+    if (p.rotary > 0) {
+        if (2 * lane < p.rotary) {
+            const double turn = (double)(p.positions ? (int64_t)p.positions[token] : pos) * 0.15915494309189533577 * (double)p.inv_freq[lane];  // 1 / 2 pi
+            sincospif((float)(2.0 * (turn - rint(turn))), &angles[wave][0][lane], &angles[wave][1][lane]);
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (turns)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sn[j] = angles[wave][0][8 * c + j];
+                cs[j] = angles[wave][1][8 * c + j];
+            }
     }
 
     for (int u = part; u < units; u += parts) {
@@ -124,7 +144,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_kernel(WriteParams 
             const float r = 1.f / sqrtf(sum * (1.f / D) + p.eps);
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                const floatx4 w = *reinterpret_cast<const floatx4 *>(weight + (i < 8 ? a : b) * 8 + i % 8);
+                const floatx4 w = *reinterpret_cast<const floatx4 *>(weight + (i < 8 ? one : two) * 8 + i % 8);
                 for (int j = 0; j < 4; ++j) x[i / 8][i % 8 + j] *= r * w[j];
             }
         }
@@ -155,8 +175,8 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_kernel(WriteParams 
         if (h >= heads) continue;
         if (is_q) {
             char *to = p.q_out + token * p.ld_out + (int64_t)h * D * kSize;
-            store8<BF16>(to + a * 8 * kSize, x[0]);
-            store8<BF16>(to + b * 8 * kSize, x[1]);
+            store8<BF16>(to + one * 8 * kSize, x[0]);
+            store8<BF16>(to + two * 8 * kSize, x[1]);
         } else if (page >= 0) {
             const int head = is_k ? h - p.Hq : h - p.Hq - p.Hkv;
             char *const pool = is_k ? p.k_pages : p.v_pages;
@@ -168,12 +188,12 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_kernel(WriteParams 
                 for (int i = 0; i < 2; ++i) {
                     const float lo[4] = {x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv};
                     const float hi[4] = {x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv};
-                    *reinterpret_cast<u32x2 *>(pool + at + (i ? b : a) * 8) = u32x2{codes_of(lo), codes_of(hi)};
+                    *reinterpret_cast<u32x2 *>(pool + at + (i ? two : one) * 8) = u32x2{codes_of(lo), codes_of(hi)};
                 }
                 if (c == 0) (is_k ? p.k_scale : p.v_scale)[((page * p.Hkv + head) << p.page_shift) + slot] = (uint8_t)byte;
             } else {
-                store8<BF16>(pool + (at + a * 8) * kSize, x[0]);
-                store8<BF16>(pool + (at + b * 8) * kSize, x[1]);
+                store8<BF16>(pool + (at + one * 8) * kSize, x[0]);
+                store8<BF16>(pool + (at + two * 8) * kSize, x[1]);
             }
         }
     }
@@ -421,8 +441,8 @@ respec_status_t respec_norm_rope_append_paged(const void *q, const void *k, cons
     p.rotary = rotary_dim;
     p.interleaved = interleaved != 0;
     p.eps = eps;
-    p.rows = max_q_per_seq == 1 || total_q <= 2048 ? 1 : 4;
-    const int64_t grid = tiles_bound(B, total_q, max_q_per_seq, 1, p.rows);
+    p.rows = total_q <= 2048 ? 1 : 4;
+    const int64_t grid = ((int64_t)total_q + p.rows - 1) / p.rows;
     if (!grid_fits(grid, kThreads)) return fail(RESPEC_ERR_UNSUPPORTED, "%s: too many rows", name);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (dt == RESPEC_BF16) pool_dt == RESPEC_E4M3 ? launch_write<true, true>(p, D, (unsigned)grid, stream) : launch_write<true, false>(p, D, (unsigned)grid, stream);
