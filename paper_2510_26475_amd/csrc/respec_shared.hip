@@ -1204,7 +1204,7 @@ __device__ inline void lds_read() {  // what the wave has asked LDS for is there
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef i32x2 __attribute__((address_space(3))) *LdsTrBytes;
 
-// A tile of 32 keys as codes (K at `k` of `lds`, V at `v`; `scales` of K's keys, then of V's) into the state; between() once K has been read.
+// A tile of 32 keys as codes (K at `k` of `lds`, V at `v`; `scales` of K's keys, then of V's) into the state; between() once they have been read.
 template <int D, typename Between, typename Mask>
 __device__ __attribute__((always_inline)) inline void attend_codes(const SharedParams &p, State<kE4m3, D> &st, char *lds, int k, int v, const float *scales, bool active,
                                                                    int half, int col, Between &&between, Mask &&mask) {
@@ -1215,41 +1215,49 @@ __device__ __attribute__((always_inline)) inline void attend_codes(const SharedP
     const int v_key = 8 * ((lane & 15) >> 3) + 4 * half + ((lane & 15) >> 1) % 4;
     int k_at = k + col * D + C::place(col, half) * 16, v_at = v + v_key * D + (lane & 1) * 8;
     asm volatile("" : "+v"(k_at), "+v"(v_at));
-    floatx16 s[1];
+    // All of the tile's codes into registers, so that its place is free for the tile that between() asks for.
+    u32x4 kc[D / 32];
+    i32x2 vc[2][S::kDTiles];
+    floatx4 v_scale[4];
+    float k_scale;
     if (active) {
-        const float k_scale = scales[col];
-        floatx16 other;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) s[0][x] = other[x] = 0.f;
+        for (int y = 0; y < D / 32; ++y) kc[y] = *reinterpret_cast<const u32x4 *>(lds + (k_at ^ (32 * y)));
+        k_scale = scales[col];
 #pragma unroll
-        for (int y = 0; y < D / 32; ++y) {
-            const u32x4 a = *reinterpret_cast<const u32x4 *>(lds + (k_at ^ (32 * y)));
-            s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_of(a[0], a[1], k_scale), __builtin_bit_cast(bf16x8, st.qf[2 * y]), s[0], 0, 0, 0);
-            other = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_of(a[2], a[3], k_scale), __builtin_bit_cast(bf16x8, st.qf[2 * y + 1]), other, 0, 0, 0);
-        }
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int x = 0; x < 16; ++x) s[0][x] += other[x];
+            for (int d = 0; d < S::kDTiles; ++d)
+                vc[i][d] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LdsTrBytes)(lds + v_at + i * 16 * D + C::place(i * 16 + v_key, 2 * d + ((lane >> 4) & 1)) * 16));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v_scale[i] = *reinterpret_cast<const floatx4 *>(scales + 32 + 8 * i + 4 * half);
     }
     between();
     if (!active) return;
+    floatx16 s[1], other;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) s[0][x] = other[x] = 0.f;
+#pragma unroll
+    for (int y = 0; y < D / 32; ++y) {
+        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_of(kc[y][0], kc[y][1], k_scale), __builtin_bit_cast(bf16x8, st.qf[2 * y]), s[0], 0, 0, 0);
+        other = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_of(kc[y][2], kc[y][3], k_scale), __builtin_bit_cast(bf16x8, st.qf[2 * y + 1]), other, 0, 0, 0);
+    }
+#pragma unroll
+    for (int x = 0; x < 16; ++x) s[0][x] += other[x];
     mask(s[0]);
     st.exponentials(p, s);
     u32x4 pf[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {  // (a power of two: nothing but the exponent moves)
-        const floatx4 vs = *reinterpret_cast<const floatx4 *>(scales + 32 + 8 * i + 4 * half);
+    for (int i = 0; i < 4; ++i)  // (a power of two: nothing but the exponent moves)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-            pf[i / 2][i % 2 * 2 + j] =
-                __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{s[0][4 * i + 2 * j] * vs[2 * j], s[0][4 * i + 2 * j + 1] * vs[2 * j + 1]}, bf16x2));
-    }
+            pf[i / 2][i % 2 * 2 + j] = __builtin_bit_cast(
+                uint32_t, __builtin_convertvector(floatx2{s[0][4 * i + 2 * j] * v_scale[i][2 * j], s[0][4 * i + 2 * j + 1] * v_scale[i][2 * j + 1]}, bf16x2));
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int d = 0; d < S::kDTiles; ++d) {
-            const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LdsTrBytes)(lds + v_at + i * 16 * D + C::place(i * 16 + v_key, 2 * d + ((lane >> 4) & 1)) * 16));
-            st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_of((uint32_t)c[0], (uint32_t)c[1], 1.f), __builtin_bit_cast(bf16x8, pf[i]), st.o[d], 0, 0, 0);
-        }
+        for (int d = 0; d < S::kDTiles; ++d)
+            st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_of((uint32_t)vc[i][d][0], (uint32_t)vc[i][d][1], 1.f), __builtin_bit_cast(bf16x8, pf[i]), st.o[d], 0, 0, 0);
 }
 
 // Every wave walks a range of its own, without barriers, in tiles of 32 keys.  Neighbouring waves have neighbouring KV heads of the same keys.
@@ -1312,23 +1320,17 @@ __device__ __attribute__((always_inline)) inline void own_work(const SharedParam
         typedef Codes<D> C;
         float *const scales = reinterpret_cast<float *>(mine + 4 * S::kCodeBytes);  // of K of the tile's keys, and of V
         uint32_t sc_byte[2] = {0, 0};
-        auto fetch_k = [&](int f) __attribute__((always_inline)) {
+        auto fetch = [&](int f, uint32_t &byte) __attribute__((always_inline)) {  // (the scales last: a step goes by them)
             C::template load<false>(p, runs, head_of(ahead), lane, mine + f % 2 * S::kCodeBytes);
-        };
-        auto fetch_v = [&](int f, uint32_t &byte) __attribute__((always_inline)) {  // (and the scales, last: a step goes by them)
             C::template load<true>(p, runs, head_of(ahead), lane, mine + (2 + f % 2) * S::kCodeBytes);
             asm volatile("" ::: "memory");
             byte = C::load_scale(p, runs, head_of(ahead), lane);
             ahead.next(p, f + 1 < n_tiles);
             runs = look();
         };
-        fetch_k(0);
         begin();
-        fetch_v(0, sc_byte[0]);
-        if (1 < n_tiles) {
-            fetch_k(1);
-            fetch_v(1, sc_byte[1]);
-        }
+        fetch(0, sc_byte[0]);
+        if (1 < n_tiles) fetch(1, sc_byte[1]);
         auto step = [&](auto place_, int f) __attribute__((always_inline)) {
             constexpr int kPlace = decltype(place_)::value;
             const SeqPlan sn = now.s;
@@ -1353,17 +1355,13 @@ __device__ __attribute__((always_inline)) inline void own_work(const SharedParam
             attend_codes<D>(p, st, mine, kPlace * S::kCodeBytes, (2 + kPlace) * S::kCodeBytes, scales, active, half, col,
                             [&]() __attribute__((always_inline)) {
                                 if (f + 2 < n_tiles) {
-                                    lds_read();  // (K, before its place is written over)
-                                    fetch_k(f + 2);
+                                    lds_read();  // (before its place is written over)
+                                    fetch(f + 2, sc_byte[kPlace]);
                                 }
                             },
                             [&](floatx16 &sc) __attribute__((always_inline)) {
                                 if (special) cols.mask(p, sn, n0, half, sc);
                             });
-            if (f + 2 < n_tiles) {
-                lds_read();
-                fetch_v(f + 2, sc_byte[kPlace]);
-            }
             if (fresh || f + 1 == n_tiles) finish(sn, tile, n0, kv_head);
         };
         for (int f = 0; f < n_tiles; f += 2) {
