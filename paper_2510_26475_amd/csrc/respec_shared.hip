@@ -52,6 +52,10 @@ struct SeqPlan {
     int32_t shared, group;     // tokens that its group reads for it; -1: none
     int32_t tiles, pad;
 };
+struct SeqGroup {              // of a sequence's group, for the join
+    int64_t base;
+    int32_t q0, rows, key_tiles, pad;
+};
 struct GroupPlan {
     int64_t base;              // tiles of shared keys before this group's
     int32_t q0, rows, shared, e0;
@@ -96,6 +100,7 @@ struct SharedParams {
     int32_t max_ranges, min_tiles;
     uint64_t key;
     SeqPlan *seq;
+    SeqGroup *seq_grp;
     GroupPlan *grp;
     Job *jobs;
     Totals *totals;
@@ -128,8 +133,8 @@ struct Shape {
     static constexpr int kSharedLoads = kWaveKeys / kLoadKeys, kSharedBytes = 2 * kSharedKeys * kRowBytes;
     static constexpr int kPlaces = kHalf ? 5 : 4;                 // for K or V of a tile of shared keys in LDS: three (two) of K, two of V
     static constexpr int kTileBytes = 2 * kOwnKeys * D * kPoolSize;  // of K and V as they are in the pool
-    static constexpr int kPairedRing = 4, kPairedHeads = POOL == kE4m3 ? 2 : 1;  // tiles in LDS where waves share them; KV heads at most
-    static constexpr int kPairedBytes = kHalf ? kPairedHeads * kPairedRing * (kTileBytes + 64 + 16) + 4 * 2 * kOwnKeys * 4 : 0;
+    static constexpr int kPairedRing = 4, kPairedHeads = 2;       // 8 bits: tiles in LDS where waves share them; KV heads at most
+    static constexpr int kPairedBytes = POOL == kE4m3 ? kPairedHeads * kPairedRing * (kTileBytes + 64 + 16) + 4 * 2 * kOwnKeys * 4 : 0;
     static constexpr int most(int a, int b) { return a > b ? a : b; }
     static constexpr int kLdsBytes = most(most(4 * kOwnBytes, kPlaces * kSharedBytes / 2), kPairedBytes);
     static_assert(kSharedLoads >= 1 && 16 % kLoadKeys == 0, "a wave's load lies in one page");
@@ -238,6 +243,17 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
     __shared__ GroupPlan lds_grp[FEW ? kFewGroups : 1];
     SeqPlan *const seq = FEW ? lds_seq : p.seq;
     GroupPlan *const grp = FEW ? lds_grp : p.grp;
+    // A group shares what all its members hold before their new tokens.
+    auto group = [&](int g) __attribute__((always_inline)) {
+        const int first = max(0, min(p.group_indptr[g], p.B)), end = max(first, min(p.group_indptr[g + 1], p.B));
+        GroupPlan t{};
+        t.first = first;
+        t.end = end;
+        t.shared = end - first < 2 ? 0 : max(0, p.shared_len[g]);
+        return t;
+    };
+    GroupPlan mine{};  // (on its way while the sequences are)
+    if ((int)threadIdx.x < p.groups) mine = group(threadIdx.x);
     for (int b = threadIdx.x; b < p.B; b += kPrepThreads) {
         SeqPlan s{};
         const int q0 = p.q_indptr[b], q1 = p.q_indptr[b + 1], e0 = p.page_indptr[b], e1 = p.page_indptr[b + 1], length = p.kv_len[b];
@@ -249,16 +265,8 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
         s.group = -1;
         seq[b] = s;
     }
-    __syncthreads();
-    // A group shares what all its members hold before their new tokens.
-    for (int g = threadIdx.x; g < p.groups; g += kPrepThreads) {
-        const int first = max(0, min(p.group_indptr[g], p.B)), end = max(first, min(p.group_indptr[g + 1], p.B));
-        GroupPlan t{};
-        t.first = first;
-        t.end = end;
-        t.shared = end - first < 2 ? 0 : max(0, p.shared_len[g]);
-        grp[g] = t;
-    }
+    if ((int)threadIdx.x < p.groups) grp[threadIdx.x] = mine;
+    for (int g = threadIdx.x + kPrepThreads; g < p.groups; g += kPrepThreads) grp[g] = group(g);
     __syncthreads();
     auto group_of = [&](int b) __attribute__((always_inline)) {  // the last one that begins at or before b, if b is in it
         int at = 0;
@@ -371,6 +379,11 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
         job.kind = kind;
         job.key = p.key;
     }
+    if (blockIdx.x == 0 && p.groups > 0)
+        for (int b = threadIdx.x; b < p.B; b += kPrepThreads) {
+            const int g = seq[b].group;
+            if (g >= 0) copy_plan(p.seq_grp[b], SeqGroup{grp[g].base, grp[g].q0, grp[g].rows, grp[g].key_tiles, 0});
+        }
     if (FEW && blockIdx.x == 0) {
         for (int b = threadIdx.x; b < p.B; b += kPrepThreads) copy_plan(p.seq[b], seq[b]);
         for (int g = threadIdx.x; g < p.groups; g += kPrepThreads) copy_plan(p.grp[g], grp[g]);
@@ -728,11 +741,14 @@ __device__ __attribute__((always_inline)) inline void mask_past(floatx16 (&s)[NB
             if (n0 + b * 32 + 8 * (x / 4) + 4 * half + x % 4 >= end) s[b][x] = -INFINITY;
 }
 
-// The waves of the work-group meet: what they have written to LDS is there, and all but the `kLeft` loads that each has asked for last.
+// All but the `kLeft` loads that the wave has asked for last are there.
 template <int kLeft>
 __device__ __attribute__((always_inline)) inline void wait_for() {
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x0f70 | (kLeft & 15) | (kLeft >> 4) << 14);  // vmcnt(kLeft)
+    asm volatile("" ::: "memory");
 }
+// The waves of the work-group meet: what they have written to LDS is there, and all but those loads.
 template <int kLeft>
 __device__ __attribute__((always_inline)) inline void meet() {
     asm volatile("" ::: "memory");
@@ -1375,11 +1391,10 @@ __device__ __attribute__((always_inline)) inline void own_work(const SharedParam
 // that each loaded for itself would be asked for CW times, and a compute unit can only have so much on its way: 96 sequences of 256 to 8,192 tokens with trees
 // of seven rows at 40/8 heads over 8 bits took 160 us).  All of the work-group's waves, on 4 / CW heads, go from tile to tile at the same time: a step begins
 // with a barrier, then asks for the tile three further on, in the place of the one that was read in the step before.
-template <Pool POOL, int D, int CW>
+template <int D, int CW>
 __device__ __attribute__((always_inline)) inline void paired_work(const SharedParams &p, char *lds, const Job &job) {
-    using S = Shape<POOL, D>;
-    constexpr bool kCodes = POOL == kE4m3;
-    constexpr int kRing = S::kPairedRing, kHeads = 4 / CW, kLoads = 2 * S::kOwnLoads / CW, kGroup = kLoads + kCodes, kRun = 16 / S::kLoadKeys;  // (of K and V, of a wave)
+    using S = Shape<kE4m3, D>;
+    constexpr int kRing = S::kPairedRing, kHeads = 4 / CW, kLoads = 2 * S::kOwnLoads / CW, kGroup = kLoads + 1, kRun = 16 / S::kLoadKeys;  // (of K and V, of a wave)
     static_assert(kHeads <= S::kPairedHeads && kLoads >= 1, "the tiles fit");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int half = lane >> 5, col = lane & 31, cw = wave % CW, hi = wave / CW, n_tiles = job.tiles, head_groups = p.Hkv / kHeads;
@@ -1388,38 +1403,32 @@ __device__ __attribute__((always_inline)) inline void paired_work(const SharedPa
     int *const flags = reinterpret_cast<int *>(lds + kHeads * kRing * (S::kTileBytes + 64)) + hi * kRing;       // whether V of a tile held something not finite
     float *const scales = reinterpret_cast<float *>(lds + kHeads * kRing * (S::kTileBytes + 64 + 16)) + wave * 2 * S::kOwnKeys;
     OwnPlace now{job.outer, job.item, job.tile, job.s}, ahead = now;
-    State<POOL, D> st;
+    State<kE4m3, D> st;
     OwnColumns cols{};
     bool fresh = true, first = true, bad = false;
     auto head_of = [&](const OwnPlace &x) __attribute__((always_inline)) { return x.outer % head_groups * kHeads + hi; };
     auto look = [&]() __attribute__((always_inline)) { return Runs(p, ahead.s.e0, ahead.first_key(), ahead.s.L - 1); };
     Runs r = look();  // of the next tile to fetch
     auto begin = [&]() __attribute__((always_inline)) {
-        cols.template begin<kCodes>(p, now, (now.outer / head_groups * CW + cw) * kColumns, head_of(now), half, col, st);
+        cols.template begin<true>(p, now, (now.outer / head_groups * CW + cw) * kColumns, head_of(now), half, col, st);
     };
     // Load i of a tile's is its wave's i / CW-th, for K and then for V; keys run * 16 + j * kLoadKeys on.
     auto fetch = [&](int f) __attribute__((always_inline)) {
         const int h = head_of(ahead);
         char *const to = ring + f % kRing * S::kTileBytes;
-        const uint32_t token = (uint32_t)p.Hkv * D * S::kPoolSize;
+        const uint32_t token = (uint32_t)p.Hkv * D;
 #pragma unroll
         for (int y = 0; y < kLoads; ++y) {
             const int i = y * CW + cw, at = i % S::kOwnLoads, run = at / kRun, in_run = at % kRun * S::kLoadKeys + lane / S::kPoolPieces, key = run * 16 + in_run;
-            const bool is_v = i >= S::kOwnLoads;
-            const int64_t row = run == 0 ? r[0].row(p, h) : r[1].row(p, h);
-            const char *from = (is_v ? p.v : p.k) + row * (D * S::kPoolSize);
-            const int piece = lane % S::kPoolPieces;
-            int place;
-            if constexpr (kCodes) place = Codes<D>::place(key, piece);
-            else place = is_v ? v_piece<true, D>(key, piece) : k_piece<true, D>(key, piece);
-            const uint32_t off = (uint32_t)min(in_run, run == 0 ? r[0].left : r[1].left) * token + (uint32_t)place * 16;
+            const char *from = (i >= S::kOwnLoads ? p.v : p.k) + (run == 0 ? r[0].row(p, h) : r[1].row(p, h)) * D;
+            const uint32_t off = (uint32_t)min(in_run, run == 0 ? r[0].left : r[1].left) * token + (uint32_t)Codes<D>::place(key, lane % S::kPoolPieces) * 16;
             __builtin_amdgcn_global_load_lds((GlobalFrom)(from + off), (LdsTo)(to + i * 1024), 16, 0, 2);
         }
-        if constexpr (kCodes)  // sixteen lanes with four scales each: K's of both runs, V's of both (those past the last key are not used)
-            if (lane < 16) {
-                const int64_t at = (lane & 4 ? r[1].scale(p, h) - (r[1].slot & 15) : r[0].scale(p, h) - (r[0].slot & 15)) + (lane & 3) * 4;
-                __builtin_amdgcn_global_load_lds((GlobalFrom)((lane & 8 ? p.v_scale : p.k_scale) + at), (LdsTo)(bytes + f % kRing * 64), 4, 0, 0);
-            }
+        // sixteen lanes with four scales each: K's of both runs, V's of both (those past the last key are not used)
+        if (lane < 16) {
+            const int64_t at = (lane & 4 ? r[1].scale(p, h) - (r[1].slot & 15) : r[0].scale(p, h) - (r[0].slot & 15)) + (lane & 3) * 4;
+            __builtin_amdgcn_global_load_lds((GlobalFrom)((lane & 8 ? p.v_scale : p.k_scale) + at), (LdsTo)(bytes + f % kRing * 64), 4, 0, 0);
+        }
         ahead.next(p, f + 1 < n_tiles);
         r = look();
     };
@@ -1433,19 +1442,17 @@ __device__ __attribute__((always_inline)) inline void paired_work(const SharedPa
         const SeqPlan sn = now.s;
         const int tile = now.tile, kv_head = head_of(now), n0 = now.first_key(), place = f % kRing;
         const bool special = n0 < sn.shared || n0 + 32 > sn.L - sn.R + (p.tree_mask ? 0 : 1);  // some row does not see all of its keys
-        char *const here = ring + place * S::kTileBytes, *const v_here = here + S::kTileBytes / 2;
+        char *const here = ring + place * S::kTileBytes;
         // This wave's loads of the tile are there, those of the next two may not be.
-        asm volatile("" ::: "memory");
         if (f + 2 < n_tiles) wait_for<2 * kGroup>();
         else if (f + 1 < n_tiles) wait_for<kGroup>();
         else wait_for<0>();
-        asm volatile("" ::: "memory");
         if (special) {
             bool mine = false;
 #pragma unroll
             for (int y = 0; y < kLoads; ++y) {
                 const int i = y * CW + cw, key = (i % S::kOwnLoads) * S::kLoadKeys + lane / S::kPoolPieces;
-                if (i >= S::kOwnLoads) mine |= sift<kCodes>(here + i * 1024 + lane * 16, n0 + key < sn.shared || n0 + key >= sn.L);
+                if (i >= S::kOwnLoads) mine |= sift<true>(here + i * 1024 + lane * 16, n0 + key < sn.shared || n0 + key >= sn.L);
             }
             if (mine) flags[place] = 1;
         }
@@ -1457,24 +1464,18 @@ __device__ __attribute__((always_inline)) inline void paired_work(const SharedPa
         const bool active = cols.packed0 < sn.R * p.G;  // (uniform)
         if (fresh) st.sign_q(p);
         fresh = now.next(p, f + 1 < n_tiles);
-        auto mask = [&](floatx16 &sc) __attribute__((always_inline)) {
+        float scale = scale_of((int)reinterpret_cast<const uint8_t *>(bytes)[place * 64 + lane]);
+        if (special && lane >= 32 && (n0 + lane - 32 < sn.shared || n0 + lane - 32 >= sn.L)) scale = 0.f;
+        scales[lane] = scale;
+        wave_sync();
+        attend_codes<D>(p, st, here, 0, S::kTileBytes / 2, scales, active, half, col, []() {}, [&](floatx16 &sc) __attribute__((always_inline)) {
             if (special) cols.mask(p, sn, n0, half, sc);
-        };
-        if constexpr (kCodes) {
-            float scale = scale_of((int)reinterpret_cast<const uint8_t *>(bytes)[place * 64 + lane]);
-            if (special && lane >= 32 && (n0 + lane - 32 < sn.shared || n0 + lane - 32 >= sn.L)) scale = 0.f;
-            scales[lane] = scale;
-            wave_sync();
-            attend_codes<D>(p, st, here, 0, S::kTileBytes / 2, scales, active, half, col, []() {}, mask);
-            wave_sync();
-        } else if (active) {
-            const int at = (int)(here - lds);
-            attend<POOL, D, 1>(p, st, lds, at, at + S::kTileBytes / 2, half, col, [&](floatx16 &sc, int) __attribute__((always_inline)) { mask(sc); });
-        }
+        });
+        wave_sync();
         if (!fresh && f + 1 < n_tiles) continue;
         const bool whole = cols.begin_tile == 0 && tile + 1 == sn.tiles;
         if (active)
-            own_finish<POOL, D>(p, st, sn, OwnPart{kv_head, cols.packed0, cols.begin_tile, n0, half, col, whole, whole && sn.shared == 0, __ballot(bad) != 0,
+            own_finish<kE4m3, D>(p, st, sn, OwnPart{kv_head, cols.packed0, cols.begin_tile, n0, half, col, whole, whole && sn.shared == 0, __ballot(bad) != 0,
                                                    (((int64_t)2 * job.range + !first) * 4 + hi * CW + cw) * kColumns});
         bad = first = false;
     }
@@ -1489,8 +1490,8 @@ __global__ __launch_bounds__(kThreads, POOL == kF32 ? 1 : 2) void shared_attenti
     if (job.kind == kShared) shared_work<POOL, D>(p, lds, job);
     else if (job.kind == kOwn) {
         if constexpr (POOL == kE4m3) {
-            if (p.col_waves == 4) return paired_work<POOL, D, 4>(p, lds, job);
-            if (p.col_waves == 2) return paired_work<POOL, D, 2>(p, lds, job);
+            if (p.col_waves == 4) return paired_work<D, 4>(p, lds, job);
+            if (p.col_waves == 2) return paired_work<D, 2>(p, lds, job);
         }
         own_work<POOL, D>(p, lds, job);
     }
@@ -1506,6 +1507,8 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
     __shared__ float lds[SPLIT ? kWaves * kPer * (D + 4) : 1];
     const Totals t = *p.totals;
     const SeqPlan s = p.seq[blockIdx.y];
+    SeqGroup g{};
+    if (p.groups > 0) g = p.seq_grp[blockIdx.y];  // (of no meaning where the sequence shares nothing)
     const int wave = threadIdx.x >> 6, part = threadIdx.x % kLanes, sub = (SPLIT ? threadIdx.x & 63 : threadIdx.x) / kLanes;
     const int last = s.R * p.Hq - 1, item = min((int)blockIdx.x * kPer + sub, last);
     if (t.key != p.key || (int)blockIdx.x * kPer > last) return;
@@ -1521,7 +1524,6 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
     constexpr int kSharedStep = 2 * kBlock;
     const int own_step = 2 * p.heads_wg * p.col_waves * kColumns;
     if (s.shared > 0) {
-        const GroupPlan g = p.grp[s.group];
         const int packed = max(0, min((int)(row - g.q0) * p.G + g_head, g.rows * p.G - 1));
         const int64_t b = t.shared_step * kv_head + g.base + (int64_t)(packed / kBlock) * g.key_tiles;
         const int r = range_of(t.shared, b);
@@ -1551,50 +1553,68 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
     constexpr int kRowBytes = D * (HALF ? 2 : 4);
     const int n = written ? 0 : n_shared + n_own, share = SPLIT ? (n + kWaves - 1) / kWaves : n;
     const int begin = SPLIT ? min(n, wave * share) : 0, end = SPLIT ? min(n, begin + share) : n;
+    constexpr int kWords = HALF ? 1 : 2;
+    // N parts at a time, all asked for before the first is waited for (one behind the other they take 0.8 us each).
+    auto ask = [&](int j, int to, auto &x) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(x) / sizeof(x[0])); ++i) {
+            const int at_part = min(j + i, to - 1), in_own = at_part - n_shared;
+            const char *from = in_own < 0 ? shared_o + (shared_at + (int64_t)at_part * kSharedStep + (at_part == 0 ? shared_late : 0)) * kRowBytes
+                                          : own_o + (own_at + (int64_t)in_own * own_step + (in_own == 0 ? own_late : 0)) * kRowBytes;
+#pragma unroll
+            for (int y = 0; y < kWords; ++y) x[i][y] = *reinterpret_cast<const u32x4 *>(from + part * (HALF ? 16 : 32) + 16 * y);
+        }
+    };
     for (int j0 = begin; j0 < end; j0 += kLanes) {
-        const int mine = j0 + part, in_own = mine - n_shared;
+        const int mine = j0 + part, in_own = mine - n_shared, to = min(end, j0 + kLanes), lane0 = (int)(threadIdx.x & 63) / kLanes * kLanes;
         floatx2 ml = {-INFINITY, 0.f};
         if (mine < end)
             ml = in_own < 0 ? reinterpret_cast<const floatx2 *>(shared_ml)[shared_at + (int64_t)mine * kSharedStep + (mine == 0 ? shared_late : 0)]
                             : reinterpret_cast<const floatx2 *>(own_ml)[own_at + (int64_t)in_own * own_step + (in_own == 0 ? own_late : 0)];
-        if (ml[1] == 0.f) ml[0] = -INFINITY;  // (no key of this part is seen)
-        float top = ml[0];
+        float e = 0.f;
+        auto weigh = [&]() __attribute__((always_inline)) {
+            if (ml[1] == 0.f) ml[0] = -INFINITY;  // (no key of this part is seen)
+            float top = ml[0];
 #pragma unroll
-        for (int step = 1; step < kLanes; step *= 2) top = fmaxf(top, __shfl_xor(top, step));
-        const float m_new = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
-        const float e = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m_new);
-        float sum = ml[1] * e;
+            for (int step = 1; step < kLanes; step *= 2) top = fmaxf(top, __shfl_xor(top, step));
+            const float m_new = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+            e = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m_new);
+            float sum = ml[1] * e;
 #pragma unroll
-        for (int step = 1; step < kLanes; step *= 2) sum += __shfl_xor(sum, step);
-        l = l * f + sum;
-        for (int x = 0; x < 8; ++x) o[x] *= f;
-        m = m_new;
-        const int to = min(end, j0 + kLanes), lane0 = (int)(threadIdx.x & 63) / kLanes * kLanes;
-        // kBatch parts at a time, all asked for before the first is waited for (one behind the other they take 0.8 us each).
-        constexpr int kBatch = HALF ? 8 : 4;
-        for (int j = j0; j < to; j += kBatch) {
-            u32x4 x[kBatch][HALF ? 1 : 2];
+            for (int step = 1; step < kLanes; step *= 2) sum += __shfl_xor(sum, step);
+            l = l * f + sum;
+            for (int x = 0; x < 8; ++x) o[x] *= f;
+            m = m_new;
+        };
+        auto add = [&](int j, auto &x) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                const int at_part = min(j + i, to - 1), in_own = at_part - n_shared;
-                const char *from = in_own < 0 ? shared_o + (shared_at + (int64_t)at_part * kSharedStep + (at_part == 0 ? shared_late : 0)) * kRowBytes
-                                              : own_o + (own_at + (int64_t)in_own * own_step + (in_own == 0 ? own_late : 0)) * kRowBytes;
-#pragma unroll
-                for (int y = 0; y < (HALF ? 1 : 2); ++y) x[i][y] = *reinterpret_cast<const u32x4 *>(from + part * (HALF ? 16 : 32) + 16 * y);
-            }
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
+            for (int i = 0; i < (int)(sizeof(x) / sizeof(x[0])); ++i) {
                 const float w = __shfl(e, lane0 + min(j + i, to - 1) - j0);
                 if (j + i >= to)
 #pragma unroll
-                    for (int y = 0; y < (HALF ? 1 : 2); ++y) x[i][y] = u32x4{0, 0, 0, 0};
+                    for (int y = 0; y < kWords; ++y) x[i][y] = u32x4{0, 0, 0, 0};
                 if constexpr (HALF) {
                     const halfx8 h = __builtin_bit_cast(halfx8, x[i][0]);
                     for (int y = 0; y < 8; ++y) o[y] = fmaf((float)h[y], w, o[y]);
                 } else {
-                    const floatx4 a = __builtin_bit_cast(floatx4, x[i][0]), b = __builtin_bit_cast(floatx4, x[i][HALF ? 0 : 1]);
+                    const floatx4 a = __builtin_bit_cast(floatx4, x[i][0]), b = __builtin_bit_cast(floatx4, x[i][kWords - 1]);
                     for (int y = 0; y < 8; ++y) o[y] = fmaf(y < 4 ? a[y % 4] : b[y % 4], w, o[y]);
                 }
+            }
+        };
+        if (__ballot(to - j0 > 2) == 0) {  // (most sequences of a large batch)
+            u32x4 x[2][kWords];
+            ask(j0, to, x);
+            weigh();
+            add(j0, x);
+        } else {
+            u32x4 x[HALF ? 8 : 4][kWords];
+            ask(j0, to, x);
+            weigh();
+            add(j0, x);
+            for (int j = j0 + (HALF ? 8 : 4); j < to; j += HALF ? 8 : 4) {
+                ask(j, to, x);
+                add(j, x);
             }
         }
     }
@@ -1631,7 +1651,7 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
 // ------------------------------------------------------------------------------------------ host side
 // The workspace, piece by piece, each at a multiple of 256 bytes.
 struct Layout {
-    size_t seq, grp, jobs, totals, own_o, own_ml, shared_o, shared_ml, own_whole_o, own_whole_ml, shared_whole_o, shared_whole_ml, bytes;
+    size_t seq, seq_grp, grp, jobs, totals, own_o, own_ml, shared_o, shared_ml, own_whole_o, own_whole_ml, shared_whole_o, shared_whole_ml, bytes;
 };
 Layout layout(int32_t B, int32_t total_q, int32_t groups, int32_t Hq, int32_t D, respec_dtype_t dt) {
     Layout w{};
@@ -1644,6 +1664,7 @@ Layout layout(int32_t B, int32_t total_q, int32_t groups, int32_t Hq, int32_t D,
     const size_t ml = 2 * sizeof(float), o = (size_t)D * (dt == RESPEC_BF16 ? 2 : 4);
     const size_t rows = groups > 0 ? (size_t)total_q * Hq : 0, own = (size_t)kWorkGroups * 8 * kColumns, shared = groups > 0 ? (size_t)kWorkGroups * 2 * kBlock : 0;
     w.seq = take((size_t)B * sizeof(SeqPlan));
+    w.seq_grp = take(groups > 0 ? (size_t)B * sizeof(SeqGroup) : 0);
     w.grp = take((size_t)groups * sizeof(GroupPlan));
     w.jobs = take(kJobs * sizeof(Job));
     w.totals = take(sizeof(Totals));
@@ -1715,6 +1736,7 @@ respec_status_t run(const char *name, SharedParams &p, int32_t D, int32_t page_s
         return fail(RESPEC_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) needed, got %zu", name, w.bytes, workspace ? workspace_bytes : (size_t)0);
     char *const base = static_cast<char *>(workspace);
     p.seq = reinterpret_cast<SeqPlan *>(base + w.seq);
+    p.seq_grp = reinterpret_cast<SeqGroup *>(base + w.seq_grp);
     p.grp = reinterpret_cast<GroupPlan *>(base + w.grp);
     p.jobs = reinterpret_cast<Job *>(base + w.jobs);
     p.totals = reinterpret_cast<Totals *>(base + w.totals);
