@@ -429,8 +429,8 @@ respec_status_t respec_pages_copy(void *k_pages, void *v_pages, const int32_t *c
  *           byte for each token and head; code c under byte e stands for c 2^(e-127), which is a bf16 number exactly.  With top = the largest finite
  *           |x| of the token's head (of what the formulas give, before any rounding) e is the least byte >= 1 with top <= 448 2^(e-127) and c is x / 2^(e-127)
  *           rounded to nearest even; what is not finite becomes NaN.
- *   D in {64, 128}; rotary_dim a multiple of 16 up to D; strides multiples of 16 bytes; q, k, v, q_out, pools and weights
- *   16-byte aligned; a token's heads at most 2^24 bytes (RESPEC_ERR_UNSUPPORTED otherwise).
+ *   D in {64, 128}; rotary_dim a multiple of 16 up to D; strides multiples of 16 bytes; q, k, v, q_out, pools, scales and
+ *   weights 16-byte aligned; a token's heads at most 2^24 bytes (RESPEC_ERR_UNSUPPORTED otherwise).
  */
 respec_status_t respec_norm_rope_append_paged(const void *q, const void *k, const void *v, const float *q_weight, const float *k_weight,
                                               const float *inv_freq, const int32_t *positions, void *q_out, void *k_pages, void *v_pages,
@@ -446,7 +446,7 @@ respec_status_t respec_norm_rope_append_paged(const void *q, const void *k, cons
  *   k_out, v_out [total_kv, Hkv, D] dt, contiguous, 16-byte aligned (written; bf16 and fp32 are both exact)
  *   kv_indptr    [B+1] int64, not decreasing: as many tokens as fit between two entries are written; rows of no sequence, those of tokens past
  *                max_kv_len and those of page ids outside [0, num_pages) are left as they were
- * Pools, scales, tables and page_size as in respec_norm_rope_append_paged; scales 16-byte aligned.
+ * Pools, scales, tables and page_size as in respec_norm_rope_append_paged.
  */
 respec_status_t respec_read_paged_quantised(const void *k_pages, const void *v_pages, const uint8_t *k_scale, const uint8_t *v_scale,
                                             const int32_t *page_indptr, const int32_t *page_table, const int32_t *kv_len, const int64_t *kv_indptr,

@@ -407,8 +407,8 @@ respec_status_t respec_norm_rope_append_paged(const void *q, const void *k, cons
     if (ld_k * esz % 16 != 0 || ld_v * esz % 16 != 0 || (q && (ld_q * esz % 16 != 0 || ld_q_out * esz % 16 != 0)))
         return fail(RESPEC_ERR_UNSUPPORTED, "%s: token strides must be multiples of 16 bytes", name);
     for (const void *x : {q, k, v, static_cast<const void *>(q_out), static_cast<const void *>(k_pages), static_cast<const void *>(v_pages),
-                          static_cast<const void *>(q_weight), static_cast<const void *>(k_weight)})
-        if (!aligned_to(x, 16)) return fail(RESPEC_ERR_INVALID_ARG, "%s: data pointers must be 16-byte aligned", name);
+                          static_cast<const void *>(q_weight), static_cast<const void *>(k_weight), static_cast<const void *>(k_scale), static_cast<const void *>(v_scale)})
+        if (!aligned_to(x, 16)) return fail(RESPEC_ERR_INVALID_ARG, "%s: data pointers and scales must be 16-byte aligned", name);
     WriteParams p{};
     p.q = static_cast<const char *>(q);
     p.k = static_cast<const char *>(k);

@@ -645,6 +645,10 @@ __device__ __attribute__((always_inline)) inline void write_part(const State<POO
     }
 }
 
+// One of two buffers of a workspace.  (Chosen by the pointers themselves, the compiler keeps both in scratch and reads the one that is meant.)
+template <typename T>
+__device__ inline T *either(bool first, T *a, T *b) { return b + (first ? a - b : 0); }
+
 // ------------------------------------------------------------------------------------------ keys that a group shares
 // f(0), f(1) ... f(N-1), each with its number as a type.
 template <int N, typename F, int... I>
@@ -985,6 +989,9 @@ __device__ __attribute__((always_inline)) inline void shared_tiles(const SharedP
     meet<0>();  // (LDS is free)
 }
 
+__device__ __attribute__((always_inline)) inline void settle(GroupPlan &g) {  // (every lane has the same: kept in scalar registers)
+    for (int32_t *x : {&g.q0, &g.rows, &g.shared, &g.e0, &g.key_tiles, &g.blocks}) *x = __builtin_amdgcn_readfirstlane(*x);
+}
 // A range of the tiles over shared keys, group after group and block of columns after block: every wave has 32 of the work-group's 128 columns, and the four
 // stage the tiles together.
 template <Pool POOL, int D>
@@ -993,6 +1000,7 @@ __device__ __attribute__((always_inline)) inline void shared_work(const SharedPa
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     int left = job.tiles, tile = job.tile, block = job.block, item = job.item, h = job.outer;
     GroupPlan g = job.g;
+    settle(g);
     bool first = true;
     for (;;) {
         const int t1 = min(g.key_tiles, tile + left), last = g.rows * p.G - 1, column0 = block * kBlock + wave * kColumns;
@@ -1009,7 +1017,7 @@ __device__ __attribute__((always_inline)) inline void shared_work(const SharedPa
             asm volatile("" : "+v"(half), "+v"(col));  // (as in attend)
             const int packed = column0 + col, i = by_g(p, packed);
             const int64_t to = whole ? ((int64_t)g.q0 + i) * p.Hq + h * p.G + packed - i * p.G : ((int64_t)2 * job.range + !first) * kBlock + wave * kColumns + col;
-            write_part(st, sum_of_halves(st.l), whole ? p.shared_whole_o : p.shared_o, whole ? p.shared_whole_ml : p.shared_ml, half, packed > last ? -1 : to);
+            write_part(st, sum_of_halves(st.l), either(whole, p.shared_whole_o, p.shared_o), either(whole, p.shared_whole_ml, p.shared_ml), half, packed > last ? -1 : to);
         }
         first = false;
         left -= t1 - tile;
@@ -1024,6 +1032,7 @@ __device__ __attribute__((always_inline)) inline void shared_work(const SharedPa
                 }
             } while (p.grp[item].key_tiles == 0);
             g = p.grp[item];
+            settle(g);
         }
     }
 }
@@ -1047,7 +1056,7 @@ __device__ __attribute__((always_inline)) inline void own_finish(const SharedPar
         const int packed = w.packed0 + c, i = by_g(p, packed);
         return packed >= sn.R * p.G ? (int64_t)-1 : ((int64_t)sn.q0 + i) * p.Hq + w.kv_head * p.G + packed - i * p.G;
     };
-    char *const part_o = w.whole ? p.own_whole_o : p.own_o;
+    char *const part_o = either(w.whole, p.own_whole_o, p.own_o);
     if (w.final) {
         const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // (no visible key: zero; NaN stays)
         const int64_t mine = row_of(col);
@@ -1064,7 +1073,7 @@ __device__ __attribute__((always_inline)) inline void own_finish(const SharedPar
         }
     } else {
         const int64_t at = row_of(col);
-        write_part(st, l, part_o, w.whole ? p.own_whole_ml : p.own_ml, half, at < 0 || w.whole ? at : w.slot + col);
+        write_part(st, l, part_o, either(w.whole, p.own_whole_ml, p.own_ml), half, at < 0 || w.whole ? at : w.slot + col);
     }
     if (!w.bad) return;
     // The values that put() left out, added to what this wave has written: a column and a d of it per lane.
@@ -1728,9 +1737,8 @@ respec_status_t run(const char *name, SharedParams &p, int32_t D, int32_t page_s
     if (!sizes_fit(p.B, p.total_q, p.groups, p.max_q, p.max_kv, p.Hq, p.Hkv, D, dt) || p.B > 65535 || (int64_t)p.Hkv * D * (dt == RESPEC_BF16 ? 2 : 4) > (1 << 24))
         return fail(RESPEC_ERR_UNSUPPORTED, "%s: at most 256 rows and heads to a KV head (G * max_q_per_seq), 65,535 sequences, 2^30 rows and heads", name);
     if (p.tree_mask && p.max_q > 64) return fail(RESPEC_ERR_UNSUPPORTED, "%s: a tree has at most 64 rows", name);
-    if (!aligned_to(p.k_scale, 4) || !aligned_to(p.v_scale, 4)) return fail(RESPEC_ERR_INVALID_ARG, "%s: scales must be 4-byte aligned", name);
-    if (!aligned_to(p.q, 16) || !aligned_to(p.k, 16) || !aligned_to(p.v, 16) || !aligned_to(p.out, 16))
-        return fail(RESPEC_ERR_INVALID_ARG, "%s: data pointers must be 16-byte aligned", name);
+    if (!aligned_to(p.q, 16) || !aligned_to(p.k, 16) || !aligned_to(p.v, 16) || !aligned_to(p.out, 16) || !aligned_to(p.k_scale, 16) || !aligned_to(p.v_scale, 16))
+        return fail(RESPEC_ERR_INVALID_ARG, "%s: data pointers and scales must be 16-byte aligned", name);
     const Layout w = layout(p.B, p.total_q, p.groups, p.Hq, D, dt);
     if (!workspace || workspace_bytes < w.bytes || !aligned_to(workspace, 256))
         return fail(RESPEC_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) needed, got %zu", name, w.bytes, workspace ? workspace_bytes : (size_t)0);

@@ -42,7 +42,7 @@ BAD = [
     (W, dict(D=96), UNSUPPORTED), (W, dict(rotary=130), INVALID), (W, dict(rotary=-16), INVALID), (W, dict(rotary=0), INVALID), (W, dict(rotary=24), UNSUPPORTED),
     (W, dict(inv_freq=None), INVALID), (W, dict(eps=-1.0), INVALID), (W, dict(eps=float("nan")), INVALID), (W, dict(page_size=24), UNSUPPORTED),
     (W, dict(ld_q=1023), INVALID), (W, dict(ld_k=255), INVALID), (W, dict(ld_v=257), UNSUPPORTED), (W, dict(ld_out=1025), UNSUPPORTED), (W, dict(k=ODD), INVALID),
-    (W, dict(q_out=ODD), INVALID), (W, dict(k_weight=ODD), INVALID), (W, dict(v_pages=ODD), INVALID), (W, dict(B=1 << 25, total_q=1 << 25, max_q=1), UNSUPPORTED),
+    (W, dict(q_out=ODD), INVALID), (W, dict(k_weight=ODD), INVALID), (W, dict(v_pages=ODD), INVALID), (W, dict(k_scale=ODD), INVALID), (W, dict(total_q=2 ** 31 - 1), UNSUPPORTED),
     (W, dict(Hq=1 << 17, ld_q=1 << 24, ld_out=1 << 24), UNSUPPORTED),
     (R, dict(B=0), INVALID), (R, dict(total_kv=0), INVALID), (R, dict(max_kv=0), INVALID), (R, dict(dt=E4M3), INVALID), (R, dict(D=32), UNSUPPORTED),
     (R, dict(page_size=8), UNSUPPORTED), (R, dict(k_out=ODD), INVALID), (R, dict(v_scale=ODD), INVALID), (R, dict(total_kv=1 << 40), UNSUPPORTED),
@@ -55,7 +55,7 @@ for name in (S, "respec_verify_attention_shared_next_layer", "respec_verify_atte
         (dict(dt=E4M3), INVALID), (dict(k_scale=None), INVALID), (dict(sm_scale=float("inf")), INVALID), (dict(page_size=40), UNSUPPORTED),
         (dict(total_q=400, max_q=65), UNSUPPORTED), (dict(total_q=70, max_q=65, Hkv=8, tree_mask=PTR), UNSUPPORTED), (dict(B=65536, total_q=65536), UNSUPPORTED),
         (dict(total_q=1 << 28), UNSUPPORTED), (dict(max_kv=2 ** 31 - 200), UNSUPPORTED), (dict(q=ODD), INVALID), (dict(out=ODD), INVALID),
-        (dict(workspace=ctypes.c_void_p(0x100010)), WORKSPACE), (dict(workspace_bytes=1000), WORKSPACE))]
+        (dict(k_scale=ODD), INVALID), (dict(v_scale=ODD), INVALID), (dict(workspace=ctypes.c_void_p(0x100010)), WORKSPACE), (dict(workspace_bytes=1000), WORKSPACE))]
 BAD += [(S, dict(groups=-1), INVALID), (S, dict(pool_dt=BF16), INVALID), (S, dict(pool_dt=F32, k_scale=None, v_scale=None), INVALID)]
 
 
