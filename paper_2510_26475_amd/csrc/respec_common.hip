@@ -59,6 +59,8 @@ void read_knobs_locked() {
     g_knobs.shared_ranges = env_long("RESPEC_SHARED_RANGES");
     g_knobs.shared_tiles = env_long("RESPEC_SHARED_TILES");
     g_knobs.shared_cost = env_long("RESPEC_SHARED_COST");
+    g_knobs.shared_own_head = env_long("RESPEC_SHARED_OWN_HEAD");
+    g_knobs.shared_head = env_long("RESPEC_SHARED_HEAD");
     g_knobs_read = true;
 }
 

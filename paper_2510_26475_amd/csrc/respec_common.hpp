@@ -51,6 +51,8 @@ struct Knobs {
     long shared_ranges;     // RESPEC_SHARED_RANGES: most ranges that either kind of work of the attention over shared pages is cut into
     long shared_tiles;      // RESPEC_SHARED_TILES: fewest tiles of a sequence's own keys in a range of that attention
     long shared_cost;       // RESPEC_SHARED_COST: what a work-group's step over a sequence's own keys costs, in percent of one over shared keys
+    long shared_own_head;   // RESPEC_SHARED_OWN_HEAD: what beginning and ending with a sequence's own keys takes there, in tiles
+    long shared_head;       // RESPEC_SHARED_HEAD: what beginning and ending with a block of columns over shared keys takes there, in tiles
     long get(long Knobs::*field, long fallback) const { return this->*field == kUnset ? fallback : this->*field; }
 };
 Knobs knobs();

@@ -47,20 +47,21 @@ constexpr int kJobs = 4 * kWorkGroups;  // one for each wave, or for the waves t
 constexpr int kFewSeqs = 1024, kFewGroups = 256;  // whose plan is made in LDS
 
 struct SeqPlan {
-    int64_t base;              // tiles of its own before this sequence's
+    int64_t base;              // its place in the list of own work
     int32_t q0, R, L, e0;      // first row, rows, tokens, first entry of page_table
     int32_t shared, group;     // tokens that its group reads for it; -1: none
-    int32_t tiles, pad;
+    int32_t tiles, before;     // tiles of its own; sequences before it that have some
 };
 struct SeqGroup {              // of a sequence's group, for the join
     int64_t base;
     int32_t q0, rows, key_tiles, pad;
 };
 struct GroupPlan {
-    int64_t base;              // tiles of shared keys before this group's
+    int64_t base;              // its place in the list of shared work
     int32_t q0, rows, shared, e0;
     int32_t key_tiles, blocks; // tiles of keys, blocks of columns
     int32_t first, end;        // its sequences
+    int32_t before, pad;       // blocks before its
 };
 enum Kind { kNone = 0, kShared = 1, kOwn = 2 };
 struct Job {                   // a range: where it begins and all that its work-group (own work: its wave) needs for that
@@ -70,14 +71,15 @@ struct Job {                   // a range: where it begins and all that its work
     SeqPlan s;
     GroupPlan g;
 };
-// A flat list of `total` tiles cut into n even ranges: the first `more` of them have a tile more than the others.
+// A flat list of `total` places cut into n even ranges: the first `more` of them have one more than the others.  Every sequence with keys of its own and every
+// block of columns has a place for each of its tiles, and `head` before them for what it takes to begin and to end with it.
 struct Cut {
     int64_t total, each;
     int32_t n, more;
 };
 struct Totals {
     Cut own, shared;
-    int64_t own_step, shared_step;  // tiles of an outer step of own work; of a head of shared work
+    int64_t own_step, shared_step;  // places of an outer step of own work; of a head of shared work
     int32_t shared_wgs, pad;
     uint64_t key;                   // of the sizes that the plan was made for
 };
@@ -96,6 +98,7 @@ struct SharedParams {
     uint32_t g_mul, g_shift;                // of a division by G
     uint32_t q_and, q_xor;                  // on the bits of q: a negative scale is taken out of it, a zero one makes it zero
     float scale2;                           // |sm_scale| * log2(e)
+    int32_t own_head, shared_head;          // places before the tiles of a sequence and of a block
     float own_cost;                         // of a work-group's tile of own keys, against one of shared keys
     int32_t max_ranges, min_tiles;
     uint64_t key;
@@ -189,31 +192,33 @@ __device__ inline int range_of(const Cut &c, int64_t f) {  // the range that til
     return (int)(f < longer ? quotient(f, c.each + 1) : c.more + quotient(f - longer, c.each));
 }
 
-// Exclusive sums over the threads of two numbers below 2^31, in one go: each as 13 low bits and the rest, whose sums over the threads fit 32 bits.
-__device__ inline void block_scan(int x, int y, int64_t &x_before, int64_t &y_before, int64_t &x_all, int64_t &y_all, int (*lds)[4]) {
+// Exclusive sums over the threads: of two numbers below 2^31, each as 13 low bits and the rest, whose sums over the threads fit 32 bits, and of two whose sums do.
+struct Sums {
+    int64_t x, y;
+    int32_t u, w;
+};
+__device__ inline void block_scan(int x, int y, int u, int w, Sums &before, Sums &all, int (*lds)[6]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int v[4] = {x & 8191, x >> 13, y & 8191, y >> 13};
-    int sum[4], all[4] = {0, 0, 0, 0};
+    const int v[6] = {x & 8191, x >> 13, y & 8191, y >> 13, u, w};
+    int sum[6], total[6] = {};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] = wave_scan_add(v[i]);
+    for (int i = 0; i < 6; ++i) sum[i] = wave_scan_add(v[i]);
     if (lane == 63)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lds[wave][i] = sum[i];
+        for (int i = 0; i < 6; ++i) lds[wave][i] = sum[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] -= v[i];
+    for (int i = 0; i < 6; ++i) sum[i] -= v[i];
 #pragma unroll
-    for (int w = 0; w < kPrepThreads / 64; ++w)
+    for (int k = 0; k < kPrepThreads / 64; ++k)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            sum[i] += w < wave ? lds[w][i] : 0;
-            all[i] += lds[w][i];
+        for (int i = 0; i < 6; ++i) {
+            sum[i] += k < wave ? lds[k][i] : 0;
+            total[i] += lds[k][i];
         }
     __syncthreads();
-    x_before = sum[0] + ((int64_t)sum[1] << 13);
-    y_before = sum[2] + ((int64_t)sum[3] << 13);
-    x_all = all[0] + ((int64_t)all[1] << 13);
-    y_all = all[2] + ((int64_t)all[3] << 13);
+    before = Sums{sum[0] + ((int64_t)sum[1] << 13), sum[2] + ((int64_t)sum[3] << 13), sum[4], sum[5]};
+    all = Sums{total[0] + ((int64_t)total[1] << 13), total[2] + ((int64_t)total[3] << 13), total[4], total[5]};
 }
 
 // The place of `f` in the flat list: the last item whose base is not past it.
@@ -238,7 +243,7 @@ __device__ inline void copy_plan(T &to, const T &from) {
 // one writes it down and all share the jobs out; for more there is one work-group.
 template <int SHARED_KEYS, bool FEW>
 __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams p) {
-    __shared__ int lds[kPrepThreads / 64][4];
+    __shared__ int lds[kPrepThreads / 64][6];
     __shared__ SeqPlan lds_seq[FEW ? kFewSeqs : 1];
     __shared__ GroupPlan lds_grp[FEW ? kFewGroups : 1];
     SeqPlan *const seq = FEW ? lds_seq : p.seq;
@@ -299,27 +304,34 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
         grp[g] = t;
     }
     __syncthreads();
-    int64_t own = 0, shared = 0;
+    Sums done{};  // tiles of own and of shared keys, sequences with own ones, blocks
     for (int i0 = 0; i0 < max(p.B, p.groups); i0 += kPrepThreads) {
         const int i = i0 + threadIdx.x;
-        int tiles = 0, blocks = 0;
+        int tiles = 0, blocks = 0, shared_tiles = 0;
         if (i < p.B) {
             SeqPlan s = seq[i];
             s.shared = s.group < 0 ? 0 : grp[s.group].shared;
             seq[i].shared = s.shared;
             if (s.R > 0 && s.L > s.shared) tiles = (int)(((int64_t)s.L + 31) / 32) - s.shared / 32;
         }
-        if (i < p.groups) blocks = grp[i].key_tiles * grp[i].blocks;
-        int64_t own_before, shared_before, own_more, shared_more;
-        block_scan(tiles, blocks, own_before, shared_before, own_more, shared_more, lds);
+        if (i < p.groups) {
+            blocks = grp[i].blocks;
+            shared_tiles = grp[i].key_tiles * blocks;
+        }
+        Sums before, all;
+        block_scan(tiles, shared_tiles, tiles > 0, blocks, before, all, lds);
         if (i < p.B) {
-            seq[i].base = own + own_before;
+            seq[i].before = done.u + before.u;
+            seq[i].base = done.x + before.x + (int64_t)p.own_head * seq[i].before;
             seq[i].tiles = tiles;
         }
-        if (i < p.groups) grp[i].base = shared + shared_before;
-        own += own_more;
-        shared += shared_more;
+        if (i < p.groups) {
+            grp[i].before = done.w + before.w;
+            grp[i].base = done.y + before.y + (int64_t)p.shared_head * grp[i].before;
+        }
+        done = Sums{done.x + all.x, done.y + all.y, done.u + all.u, done.w + all.w};
     }
+    const int64_t own = done.x + (int64_t)p.own_head * done.u, shared = done.y + (int64_t)p.shared_head * done.w;
     // Work-groups for each kind by what its tiles cost, whole eights of them (the XCDs take turns).
     Totals t{};
     t.own_step = own;
@@ -343,36 +355,45 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
         if (wg < t.shared_wgs) {
             // consecutive ranges, which read the same keys for other columns, on one XCD (work-groups go to the XCDs in turn)
             const int r = wg % 8 * (t.shared_wgs / 8) + wg / 8;
+            // Tiles before place f, and where it is.
+            auto at = [&](int64_t f, int &outer, int &item, int &block, int &tile) __attribute__((always_inline)) {
+                outer = (int)quotient(f, shared);
+                item = find_item(grp, p.groups, f - outer * shared);
+                const int64_t in = f - outer * shared - grp[item].base;
+                const int places = grp[item].key_tiles + p.shared_head;
+                block = (int)quotient(in, places);
+                tile = max(0, (int)(in - (int64_t)block * places) - p.shared_head);
+                return outer * done.y + grp[item].base - (int64_t)p.shared_head * grp[item].before + (int64_t)block * grp[item].key_tiles + tile;
+            };
             if (r < t.shared.n) {
-                const int64_t f = begin_of(t.shared, r);
-                kind = kShared;
+                int outer, item, block, tile;
+                const int64_t end = at(begin_of(t.shared, r + 1), outer, item, block, tile), begin = at(begin_of(t.shared, r), outer, item, block, tile);
+                if (end > begin) kind = kShared;
                 job.range = r;
-                job.tiles = (int)(begin_of(t.shared, r + 1) - f);
-                const int outer = (int)quotient(f, shared);
-                const int64_t rest = f - outer * shared;
-                const int item = find_item(grp, p.groups, rest);
+                job.tiles = (int)(end - begin);
                 job.outer = outer;
-                const int key_tiles = grp[item].key_tiles;
-                const int64_t in = rest - grp[item].base;
-                const int block = (int)quotient(in, key_tiles);
                 job.item = item;
                 job.block = block;
-                job.tile = (int)(in - (int64_t)block * key_tiles);
+                job.tile = tile;
                 copy_plan(job.g, grp[item]);
             }
         } else {
             const int r = j - t.shared_wgs * p.parts_wg;
+            auto at = [&](int64_t f, int &outer, int &item, int &tile) __attribute__((always_inline)) {
+                outer = (int)quotient(f, own);
+                item = find_item(seq, p.B, f - outer * own);
+                tile = max(0, (int)(f - outer * own - seq[item].base) - p.own_head);
+                return outer * done.x + seq[item].base - (int64_t)p.own_head * seq[item].before + tile;
+            };
             if (r < t.own.n) {
-                const int64_t f = begin_of(t.own, r);
-                kind = kOwn;
+                int outer, item, tile;
+                const int64_t end = at(begin_of(t.own, r + 1), outer, item, tile), begin = at(begin_of(t.own, r), outer, item, tile);
+                if (end > begin) kind = kOwn;
                 job.range = r;
-                job.tiles = (int)(begin_of(t.own, r + 1) - f);
-                const int outer = (int)quotient(f, own);
-                const int64_t rest = f - outer * own;
-                const int item = find_item(seq, p.B, rest);
+                job.tiles = (int)(end - begin);
                 job.outer = outer;
                 job.item = item;
-                job.tile = (int)(rest - seq[item].base);
+                job.tile = tile;
                 copy_plan(job.s, seq[item]);
             }
         }
@@ -1534,9 +1555,9 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
     const int own_step = 2 * p.heads_wg * p.col_waves * kColumns;
     if (s.shared > 0) {
         const int packed = max(0, min((int)(row - g.q0) * p.G + g_head, g.rows * p.G - 1));
-        const int64_t b = t.shared_step * kv_head + g.base + (int64_t)(packed / kBlock) * g.key_tiles;
-        const int r = range_of(t.shared, b);
-        n_shared = range_of(t.shared, b + g.key_tiles - 1) - r + 1;
+        const int64_t b = t.shared_step * kv_head + g.base + (int64_t)(packed / kBlock) * (g.key_tiles + p.shared_head);
+        const int r = range_of(t.shared, b + p.shared_head);
+        n_shared = range_of(t.shared, b + p.shared_head + g.key_tiles - 1) - r + 1;
         if (n_shared > 1) {
             shared_o = p.shared_o;
             shared_ml = p.shared_ml;
@@ -1547,8 +1568,8 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
     if (s.tiles > 0) {
         const int cols = p.col_waves * kColumns, c_block = c / cols, c_in = c - c_block * cols, head_block = kv_head / p.heads_wg;
         const int64_t b = t.own_step * (c_block * (p.Hkv / p.heads_wg) + head_block) + s.base;
-        const int r = range_of(t.own, b);
-        n_own = range_of(t.own, b + s.tiles - 1) - r + 1;
+        const int r = range_of(t.own, b + p.own_head);
+        n_own = range_of(t.own, b + p.own_head + s.tiles - 1) - r + 1;
         if (n_own > 1) {
             own_o = p.own_o;
             own_ml = p.own_ml;
@@ -1780,13 +1801,18 @@ respec_status_t run(const char *name, SharedParams &p, int32_t D, int32_t page_s
                             (int64_t)page_size, (int64_t)p.Hq, (int64_t)p.Hkv, (int64_t)D, (int64_t)dt, (int64_t)pool_dt})
         p.key = (p.key ^ (uint64_t)x) * 0x100000001b3u;
     const Knobs kn = knobs();
-    // What a work-group's tile of own keys takes against one of shared keys.  Over bf16 32 groups of 8 sequences at 28/4 heads (two layers) took 182, 178, 169 and
-    // 175 us with 120, 160, 220 and 250 hundredths, 64 single tokens 62, 58, 51 and 49; over 8 bits 8 groups of 16 at 40/8 took 182, 160, 168 and 177 us
-    // with 120, 160, 200 and 220.
-    p.own_cost = kn.get(&Knobs::shared_cost, pool_dt == RESPEC_E4M3 ? 165 : dt == RESPEC_BF16 ? 230 : 100) / 100.f;
+    // What a work-group's tile of own keys takes against one of shared keys.  Over bf16 32 groups of 8 sequences at 28/4 heads (two layers) took 178, 163, 162 and
+    // 167 us with 130, 165, 220 and 250 hundredths, 64 single tokens 52, 48, 44 and 43; over 8 bits 8 groups of 16 at 40/8 took 165, 157, 166 and 175 us
+    // with 130, 160, 200 and 250.
+    p.own_cost = kn.get(&Knobs::shared_cost, pool_dt == RESPEC_E4M3 ? 160 : dt == RESPEC_BF16 ? 220 : 100) / 100.f;
     // Tiles of own keys that make a range of their own: fp32 takes longer for one than a part more takes to join (8 sequences of up to 40 tokens: 20 us with one,
-    // 26 with two), bf16 products do not (8 sequences of 512 to 8,192 tokens at 16/2 heads over 8 bits: 27 us with one, 24 with two, 26 with three).
+    // 26 with two), bf16 products do not (8 sequences of 512 to 8,192 tokens at 16/2 heads over 8 bits: 27 us with one, 22 with two, 23 with three).
     p.min_tiles = (int)std::max(1L, kn.get(&Knobs::shared_tiles, dt == RESPEC_F32 ? 1 : 2));
+    // What beginning and ending with a sequence's own keys and with a block of columns takes, in tiles.  With none counted the ranges that hold many of them end
+    // last: 32 groups of 8 (as above) 177 us, 162 with 1 and 3; 64 single tokens 52 and 44; over 8 bits 8 groups of 16 168 and, with 2 and 3, 157, 256
+    // sequences of 512 to 4,096 tokens at 28/4 heads 117 and 109, 96 with trees of seven rows 142 and 130.
+    p.own_head = (int)std::max(0L, std::min(kn.get(&Knobs::shared_own_head, pool_dt == RESPEC_BF16 ? 1 : 2), 1000L));
+    p.shared_head = (int)std::max(0L, std::min(kn.get(&Knobs::shared_head, 3), 1000L));
     p.max_ranges = (int)std::max(1L, std::min(kn.get(&Knobs::shared_ranges, kJobs), (long)kJobs));
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     hipError_t err;
