@@ -221,16 +221,18 @@ __device__ inline void block_scan(int x, int y, int u, int w, Sums &before, Sums
     all = Sums{total[0] + ((int64_t)total[1] << 13), total[2] + ((int64_t)total[3] << 13), total[4], total[5]};
 }
 
-// The place of `f` in the flat list: the last item whose base is not past it.
+// Where places f[0] and f[1] of the flat list are: the last items whose bases are not past them.  (Both at once: each step of one waits for LDS.)
 template <typename Item>
-__device__ inline int find_item(const Item *items, int n, int64_t f) {
-    int at = 0;
-    for (int end = n; end - at > 1;) {
-        const int mid = (at + end) / 2;
-        if (items[mid].base <= f) at = mid;
-        else end = mid;
-    }
-    return at;
+__device__ inline void find_items(const Item *items, int n, const int64_t (&f)[2], int (&at)[2]) {
+    int end[2] = {n, n};
+    at[0] = at[1] = 0;
+    for (int span = n; span > 1; span = (span + 1) / 2)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int mid = (at[i] + end[i]) / 2;
+            if (items[mid].base <= f[i]) at[i] = mid;
+            else end[i] = mid;
+        }
 }
 
 template <typename T>
@@ -355,46 +357,52 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
         if (wg < t.shared_wgs) {
             // consecutive ranges, which read the same keys for other columns, on one XCD (work-groups go to the XCDs in turn)
             const int r = wg % 8 * (t.shared_wgs / 8) + wg / 8;
-            // Tiles before place f, and where it is.
-            auto at = [&](int64_t f, int &outer, int &item, int &block, int &tile) __attribute__((always_inline)) {
-                outer = (int)quotient(f, shared);
-                item = find_item(grp, p.groups, f - outer * shared);
-                const int64_t in = f - outer * shared - grp[item].base;
-                const int places = grp[item].key_tiles + p.shared_head;
-                block = (int)quotient(in, places);
-                tile = max(0, (int)(in - (int64_t)block * places) - p.shared_head);
-                return outer * done.y + grp[item].base - (int64_t)p.shared_head * grp[item].before + (int64_t)block * grp[item].key_tiles + tile;
-            };
             if (r < t.shared.n) {
-                int outer, item, block, tile;
-                const int64_t end = at(begin_of(t.shared, r + 1), outer, item, block, tile), begin = at(begin_of(t.shared, r), outer, item, block, tile);
-                if (end > begin) kind = kShared;
+                // The range's first place and the one behind its last: where they are, and how many tiles come before them.
+                int64_t f[2] = {begin_of(t.shared, r), begin_of(t.shared, r + 1)}, before[2];
+                int outer[2], item[2], block[2], tile[2];
+                for (int i = 0; i < 2; ++i) {
+                    outer[i] = (int)quotient(f[i], shared);
+                    f[i] -= outer[i] * shared;
+                }
+                find_items(grp, p.groups, f, item);
+                for (int i = 0; i < 2; ++i) {
+                    const int64_t in = f[i] - grp[item[i]].base;
+                    const int key_tiles = grp[item[i]].key_tiles, places = key_tiles + p.shared_head;
+                    block[i] = (int)quotient(in, places);
+                    tile[i] = max(0, (int)(in - (int64_t)block[i] * places) - p.shared_head);
+                    before[i] = outer[i] * done.y + grp[item[i]].base - (int64_t)p.shared_head * grp[item[i]].before + (int64_t)block[i] * key_tiles + tile[i];
+                }
+                if (before[1] > before[0]) kind = kShared;
                 job.range = r;
-                job.tiles = (int)(end - begin);
-                job.outer = outer;
-                job.item = item;
-                job.block = block;
-                job.tile = tile;
-                copy_plan(job.g, grp[item]);
+                job.tiles = (int)(before[1] - before[0]);
+                job.outer = outer[0];
+                job.item = item[0];
+                job.block = block[0];
+                job.tile = tile[0];
+                copy_plan(job.g, grp[item[0]]);
             }
         } else {
             const int r = j - t.shared_wgs * p.parts_wg;
-            auto at = [&](int64_t f, int &outer, int &item, int &tile) __attribute__((always_inline)) {
-                outer = (int)quotient(f, own);
-                item = find_item(seq, p.B, f - outer * own);
-                tile = max(0, (int)(f - outer * own - seq[item].base) - p.own_head);
-                return outer * done.x + seq[item].base - (int64_t)p.own_head * seq[item].before + tile;
-            };
             if (r < t.own.n) {
-                int outer, item, tile;
-                const int64_t end = at(begin_of(t.own, r + 1), outer, item, tile), begin = at(begin_of(t.own, r), outer, item, tile);
-                if (end > begin) kind = kOwn;
+                int64_t f[2] = {begin_of(t.own, r), begin_of(t.own, r + 1)}, before[2];
+                int outer[2], item[2], tile[2];
+                for (int i = 0; i < 2; ++i) {
+                    outer[i] = (int)quotient(f[i], own);
+                    f[i] -= outer[i] * own;
+                }
+                find_items(seq, p.B, f, item);
+                for (int i = 0; i < 2; ++i) {
+                    tile[i] = max(0, (int)(f[i] - seq[item[i]].base) - p.own_head);
+                    before[i] = outer[i] * done.x + seq[item[i]].base - (int64_t)p.own_head * seq[item[i]].before + tile[i];
+                }
+                if (before[1] > before[0]) kind = kOwn;
                 job.range = r;
-                job.tiles = (int)(end - begin);
-                job.outer = outer;
-                job.item = item;
-                job.tile = tile;
-                copy_plan(job.s, seq[item]);
+                job.tiles = (int)(before[1] - before[0]);
+                job.outer = outer[0];
+                job.item = item[0];
+                job.tile = tile[0];
+                copy_plan(job.s, seq[item[0]]);
             }
         }
         job.kind = kind;
@@ -1804,7 +1812,7 @@ respec_status_t run(const char *name, SharedParams &p, int32_t D, int32_t page_s
     // What a work-group's tile of own keys takes against one of shared keys.  Over bf16 32 groups of 8 sequences at 28/4 heads (two layers) took 178, 163, 162 and
     // 167 us with 130, 165, 220 and 250 hundredths, 64 single tokens 52, 48, 44 and 43; over 8 bits 8 groups of 16 at 40/8 took 165, 157, 166 and 175 us
     // with 130, 160, 200 and 250.
-    p.own_cost = kn.get(&Knobs::shared_cost, pool_dt == RESPEC_E4M3 ? 160 : dt == RESPEC_BF16 ? 220 : 100) / 100.f;
+    p.own_cost = kn.get(&Knobs::shared_cost, pool_dt == RESPEC_E4M3 ? 155 : dt == RESPEC_BF16 ? 220 : 100) / 100.f;
     // Tiles of own keys that make a range of their own: fp32 takes longer for one than a part more takes to join (8 sequences of up to 40 tokens: 20 us with one,
     // 26 with two), bf16 products do not (8 sequences of 512 to 8,192 tokens at 16/2 heads over 8 bits: 27 us with one, 22 with two, 23 with three).
     p.min_tiles = (int)std::max(1L, kn.get(&Knobs::shared_tiles, dt == RESPEC_F32 ? 1 : 2));
