@@ -6,7 +6,7 @@
 //     m = max m_i,   l = sum_i l_i 2^(m_i - m),   o = sum_i o_i 2^(m_i - m) / l.
 // A work-group does one of the two kinds of work, in one launch: the shared part keeps the matrix cores busy, the other one the memory, and a compute unit
 // holds two work-groups.  Both kinds form a flat list of tiles that is cut into even ranges, so every work-group has as much to do whatever the lengths
-// are; a range that ends inside a sequence leaves a part, and a second kernel joins the parts in a fixed order.
+// are (what beginning and ending with a sequence takes is counted); a range that ends inside a sequence leaves a part, and a second kernel joins the parts in a fixed order.
 //
 // Products as in the prompt attention: S^T = K Q^T with 32 packed rows (G heads of a KV head to a row) as a wave's columns, the probabilities of a lane's column
 // the B operand of O^T = V^T P^T, exponents against a running maximum that moves only where it grows by more than 2^8.
@@ -241,8 +241,9 @@ __device__ inline void copy_plan(T &to, const T &from) {
     for (int i = 0; i < (int)(sizeof(T) / 8); ++i) reinterpret_cast<uint64_t *>(&to)[i] = reinterpret_cast<const uint64_t *>(&from)[i];
 }
 
-// What each sequence and group has to do, and where the ranges begin.  Up to kFewSeqs sequences every work-group makes the plan for itself, in LDS, the first
-// one writes it down and all share the jobs out; for more there is one work-group.
+// What each sequence and group has to do, and where the ranges begin.  Up to kFewSeqs sequences every work-group makes the plan for itself, in LDS, and all
+// share the jobs out and write the plan down; for more there is one work-group.  Latency: with 256 sequences in 32 groups the index arrays take 1.3 us, the groups 1.1,
+// the sums 1.3, the cut 0.7 and the jobs 1.
 template <int SHARED_KEYS, bool FEW>
 __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams p) {
     __shared__ int lds[kPrepThreads / 64][6];
@@ -350,7 +351,9 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
     t.key = p.key;
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.totals = t;
     __syncthreads();
-    for (int j = blockIdx.x * kPrepThreads + threadIdx.x; j < kWorkGroups * p.parts_wg; j += gridDim.x * kPrepThreads) {
+    // (wave after wave of all work-groups: the first one by itself needs 2 us for 512 jobs)
+    const int turn = (threadIdx.x / 64 * gridDim.x + blockIdx.x) * 64 + threadIdx.x % 64;
+    for (int j = turn; j < kWorkGroups * p.parts_wg; j += gridDim.x * kPrepThreads) {
         const int wg = j / p.parts_wg;
         Job &job = p.jobs[wg * 4 + j - wg * p.parts_wg];
         int kind = kNone;
@@ -408,15 +411,14 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
         job.kind = kind;
         job.key = p.key;
     }
-    if (blockIdx.x == 0 && p.groups > 0)
-        for (int b = threadIdx.x; b < p.B; b += kPrepThreads) {
-            const int g = seq[b].group;
-            if (g >= 0) copy_plan(p.seq_grp[b], SeqGroup{grp[g].base, grp[g].q0, grp[g].rows, grp[g].key_tiles, 0});
-        }
-    if (FEW && blockIdx.x == 0) {
-        for (int b = threadIdx.x; b < p.B; b += kPrepThreads) copy_plan(p.seq[b], seq[b]);
-        for (int g = threadIdx.x; g < p.groups; g += kPrepThreads) copy_plan(p.grp[g], grp[g]);
+    const int last = gridDim.x * kPrepThreads - 1 - turn;  // (from the other end: waves without jobs)
+    for (int b = last; b < p.B; b += gridDim.x * kPrepThreads) {
+        if (FEW) copy_plan(p.seq[b], seq[b]);
+        const int g = seq[b].group;
+        if (g >= 0) copy_plan(p.seq_grp[b], SeqGroup{grp[g].base, grp[g].q0, grp[g].rows, grp[g].key_tiles, 0});
     }
+    if (FEW)
+        for (int g = last; g < p.groups; g += gridDim.x * kPrepThreads) copy_plan(p.grp[g], grp[g]);
 }
 
 // ------------------------------------------------------------------------------------------ what both kinds of work do
@@ -543,7 +545,8 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams 
 }
 
 // Where sixteen keys of a sequence lie that begin at key n (a multiple of eight), all in one page: keys past the last one are the last one's, as they are
-// never seen.  The entry of the page table is asked for a step before it is needed: waited for at once it takes a sixth of a step.
+// never seen.  The entry of the page table is asked for a step before it is needed (waited for at once: 96 sequences of 256 to 8,192 tokens with trees of seven rows at
+// 40/8 heads over 8 bits 181 us, 162 so).
 struct Run {
     int32_t entry, slot, left;  // slot: of the first; left: keys behind it
     __device__ __attribute__((always_inline)) inline Run(const SharedParams &p, int e0, int n, int last) {
@@ -614,7 +617,7 @@ struct Mover {
 };
 
 // A wave's column times `factor` to `to`, a row of D in bf16 (OUT) or in fp16 (parts); nullptr: there is no such column.  The halves of the wave trade four of
-// eight d each, so that a lane writes sixteen bytes.
+// eight d each, so that a lane writes sixteen bytes (through LDS, eight columns at a time: 96 sequences with trees of seven rows 163 us, 152 so).
 template <Pool POOL, int D, bool OUT>
 __device__ __attribute__((always_inline)) inline void write_row(const State<POOL, D> &st, float factor, char *to, int half) {
     using S = Shape<POOL, D>;
@@ -1192,7 +1195,8 @@ struct OwnColumns {
 // 8 bits: K and V of two tiles at a time are on their way into a wave's part of LDS as they are, each lane asking for the piece that belongs where its sixteen
 // bytes land.  They are turned into bf16 behind the reads that the products take them by: sixteen codes of a key's K, and by the transposing read of bytes
 // (sixteen lanes address eight keys by sixteen d and receive one d of the eight keys each) eight of V, whose scales go to the probabilities.  So neither
-// the registers nor LDS hold a tile twice: 96 sequences of 256 to 8,192 tokens with trees of seven rows at 40/8 heads take 178 us by registers and bf16 in LDS.
+// the registers nor LDS hold a tile twice (those trees: 178 us by registers and bf16 in LDS, 173 so).  bf16 goes through registers: straight into LDS there is
+// room for one tile to a wave only, which is asked for after the one before it has been read (32 groups of 8, 28/4 heads: 191 us, 184 by registers).
 template <int D>
 struct Codes {
     using S = Shape<kE4m3, D>;
@@ -1269,7 +1273,8 @@ __device__ __attribute__((always_inline)) inline void attend_codes(const SharedP
     const int v_key = 8 * ((lane & 15) >> 3) + 4 * half + ((lane & 15) >> 1) % 4;
     int k_at = k + col * D + C::place(col, half) * 16, v_at = v + v_key * D + (lane & 1) * 8;
     asm volatile("" : "+v"(k_at), "+v"(v_at));
-    // All of the tile's codes into registers, so that its place is free for the tile that between() asks for.
+    // All of the tile's codes into registers, so that its place is free for the tile that between() asks for (256 sequences of 512 to 4,096 tokens at 28/4 heads: 128 us
+    // with V read and asked for after the scores, 116 so).
     u32x4 kc[D / 32];
     i32x2 vc[2][S::kDTiles];
     floatx4 v_scale[4];
@@ -1425,10 +1430,10 @@ __device__ __attribute__((always_inline)) inline void own_work(const SharedParam
     }
 }
 
-// More than 32 columns to a KV head: CW waves with 32 of them each walk one range together and share its tiles, which lie in LDS as they do in the pool (a tile
-// that each loaded for itself would be asked for CW times, and a compute unit can only have so much on its way: 96 sequences of 256 to 8,192 tokens with trees
-// of seven rows at 40/8 heads over 8 bits took 160 us).  All of the work-group's waves, on 4 / CW heads, go from tile to tile at the same time: a step begins
-// with a barrier, then asks for the tile three further on, in the place of the one that was read in the step before.
+// 8 bits, more than 32 columns to a KV head: CW waves with 32 of them each walk one range together and share its tiles, which lie in LDS as they do in the pool.
+// All of the work-group's waves, on 4 / CW heads, go from tile to tile at the same time: a step begins with a barrier, then asks for the tile three further on,
+// in the place of the one that was read in the step before.  (A tile that each wave loads for itself is asked for CW times, and a compute unit can only
+// have so much on its way: those trees 158 us, 142 so.  bf16 tiles are twice as large, the code for them beside this cost the shared keys 5 %.)
 template <int D, int CW>
 __device__ __attribute__((always_inline)) inline void paired_work(const SharedParams &p, char *lds, const Job &job) {
     using S = Shape<kE4m3, D>;
