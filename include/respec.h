@@ -473,7 +473,8 @@ respec_status_t respec_pages_copy_quantised(void *k_pages, void *v_pages, uint8_
  *   shared_len   [num_groups] int32: so many tokens at the beginning are the same for all members of the group; they are read from the
  *                pages of its first one.  Any number: what some member does not hold before its new tokens (kv_len[b]-R_b) counts as its own
  *   k_pages, v_pages  of pool_dt, which is dt, with k_scale and v_scale NULL, or RESPEC_E4M3 (dt then RESPEC_BF16; as in
- *                respec_norm_rope_append_paged, bytes 1 to 247): the attention over the bf16 numbers that the codes stand for
+ *                respec_norm_rope_append_paged, bytes 1 to 247): the attention over the bf16 numbers that the codes stand for (values of
+ *                V below 2^-90 may count as zero)
  *   Everything else as in respec_verify_attention_paged; rows of no sequence are left as they were; B <= 65,535,
  *   max_q_per_seq * Hq / Hkv <= 256 (trees: max_q_per_seq <= 64), total_q * Hq < 2^30 (RESPEC_ERR_UNSUPPORTED otherwise).
  *   workspace    respec_verify_attention_shared_workspace_bytes(...) bytes, 256-byte aligned, scratch (nothing to prepare): calls that

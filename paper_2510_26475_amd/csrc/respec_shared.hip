@@ -107,7 +107,7 @@ struct SharedParams {
     GroupPlan *grp;
     Job *jobs;
     Totals *totals;
-    // Parts of ranges' ends, and those that are a row's only one of their kind ([total_q * Hq]): outputs, and pairs of maximum and sum.
+    // Parts of ranges' ends, and those that are a row's only one of their kind ([total_q * Hq]): outputs, and four words with maximum, sum and the outputs' unit.
     char *own_o, *shared_o, *own_whole_o, *shared_whole_o;
     float *own_ml, *shared_ml, *own_whole_ml, *shared_whole_ml;
 };
@@ -192,33 +192,36 @@ __device__ inline int range_of(const Cut &c, int64_t f) {  // the range that til
     return (int)(f < longer ? quotient(f, c.each + 1) : c.more + quotient(f - longer, c.each));
 }
 
-// Exclusive sums over the threads: of two numbers below 2^31, each as 13 low bits and the rest, whose sums over the threads fit 32 bits, and of two whose sums do.
+// Exclusive sums over the threads: of x below 2^31 and y below 2^58, as parts whose sums over the threads fit 32 bits, and of two whose sums do.
 struct Sums {
     int64_t x, y;
     int32_t u, w;
 };
-__device__ inline void block_scan(int x, int y, int u, int w, Sums &before, Sums &all, int (*lds)[6]) {
+__device__ inline void block_scan(int x, int64_t y, int u, int w, Sums &before, Sums &all, int (*lds)[8]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int v[6] = {x & 8191, x >> 13, y & 8191, y >> 13, u, w};
-    int sum[6], total[6] = {};
+    const int v[7] = {x & 8191, x >> 13, (int)(y & 0xfffff), (int)(y >> 20 & 0xfffff), (int)(y >> 40), u, w};
+    int sum[7], total[7] = {};
 #pragma unroll
-    for (int i = 0; i < 6; ++i) sum[i] = wave_scan_add(v[i]);
+    for (int i = 0; i < 7; ++i) sum[i] = wave_scan_add(v[i]);
     if (lane == 63)
 #pragma unroll
-        for (int i = 0; i < 6; ++i) lds[wave][i] = sum[i];
+        for (int i = 0; i < 7; ++i) lds[wave][i] = sum[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 6; ++i) sum[i] -= v[i];
+    for (int i = 0; i < 7; ++i) sum[i] -= v[i];
 #pragma unroll
     for (int k = 0; k < kPrepThreads / 64; ++k)
 #pragma unroll
-        for (int i = 0; i < 6; ++i) {
+        for (int i = 0; i < 7; ++i) {
             sum[i] += k < wave ? lds[k][i] : 0;
             total[i] += lds[k][i];
         }
     __syncthreads();
-    before = Sums{sum[0] + ((int64_t)sum[1] << 13), sum[2] + ((int64_t)sum[3] << 13), sum[4], sum[5]};
-    all = Sums{total[0] + ((int64_t)total[1] << 13), total[2] + ((int64_t)total[3] << 13), total[4], total[5]};
+    auto joined = [](const int (&t)[7]) __attribute__((always_inline)) {
+        return Sums{t[0] + ((int64_t)t[1] << 13), t[2] + ((int64_t)t[3] << 20) + ((int64_t)t[4] << 40), t[5], t[6]};
+    };
+    before = joined(sum);
+    all = joined(total);
 }
 
 // Where places f[0] and f[1] of the flat list are: the last items whose bases are not past them.  (Both at once: each step of one waits for LDS.)
@@ -246,7 +249,7 @@ __device__ inline void copy_plan(T &to, const T &from) {
 // the sums 1.3, the cut 0.7 and the jobs 1.
 template <int SHARED_KEYS, bool FEW>
 __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams p) {
-    __shared__ int lds[kPrepThreads / 64][6];
+    __shared__ int lds[kPrepThreads / 64][8];
     __shared__ SeqPlan lds_seq[FEW ? kFewSeqs : 1];
     __shared__ GroupPlan lds_grp[FEW ? kFewGroups : 1];
     SeqPlan *const seq = FEW ? lds_seq : p.seq;
@@ -310,7 +313,8 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
     Sums done{};  // tiles of own and of shared keys, sequences with own ones, blocks
     for (int i0 = 0; i0 < max(p.B, p.groups); i0 += kPrepThreads) {
         const int i = i0 + threadIdx.x;
-        int tiles = 0, blocks = 0, shared_tiles = 0;
+        int tiles = 0, blocks = 0;
+        int64_t shared_tiles = 0;
         if (i < p.B) {
             SeqPlan s = seq[i];
             s.shared = s.group < 0 ? 0 : grp[s.group].shared;
@@ -319,7 +323,7 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
         }
         if (i < p.groups) {
             blocks = grp[i].blocks;
-            shared_tiles = grp[i].key_tiles * blocks;
+            shared_tiles = (int64_t)grp[i].key_tiles * blocks;
         }
         Sums before, all;
         block_scan(tiles, shared_tiles, tiles > 0, blocks, before, all, lds);
@@ -639,14 +643,14 @@ __device__ __attribute__((always_inline)) inline void write_row(const State<POOL
         }
 }
 
-// A wave's column as a part: unnormalised output, maximum and sum, to row `to` of `o` and `ml` (negative: there is no such column).  Outputs of bf16
-// products are written in fp16, relative to their largest: (m, l, o) and (m + e, l 2^-e, o 2^-e) are the same part, and with all o 2^-e below 1 the rounding is
-// 2^-12 of each and 2^-25 of the largest, against 2^-9 of the probabilities before and of the result after (half the bytes: 256 sequences of 512 to 4,096
-// tokens at 28/4 heads over 8 bits leave 20 MB).  What is not finite stays so.
+// A wave's column as a part: to row `to` of `ml` its maximum, its sum and the unit of its output, to row `to` of `o` the unnormalised output (negative: there
+// is no such column).  Outputs of bf16 products are written in fp16 in a unit 2^e that all of them lie below: the rounding is 2^-12 of each and 2^-25 of the
+// largest, against 2^-9 of the probabilities before and of the result after (half the bytes: 256 sequences of 512 to 4,096 tokens at 28/4 heads over 8 bits
+// leave 20 MB).  What is not finite stays so.
 template <Pool POOL, int D>
 __device__ __attribute__((always_inline)) inline void write_part(const State<POOL, D> &st, float l, char *o, float *ml, int half, int64_t to) {
     using S = Shape<POOL, D>;
-    float m = st.m, factor = 1.f;
+    float factor = 1.f, unit = 1.f;
     if constexpr (S::kHalf) {
         float top = 0.f;
 #pragma unroll
@@ -662,10 +666,9 @@ __device__ __attribute__((always_inline)) inline void write_part(const State<POO
         }
         const int e = max(-100, min((int)(__float_as_uint(max_of_halves(top)) >> 23) - 126, 126));  // top < 2^e
         factor = __uint_as_float((uint32_t)(127 - e) << 23);
-        m += (float)e;
-        l *= factor;
+        unit = __uint_as_float((uint32_t)(127 + e) << 23);
     }
-    if (half == 0 && to >= 0) *reinterpret_cast<floatx2 *>(ml + to * 2) = floatx2{m, l};
+    if (half == 0 && to >= 0) *reinterpret_cast<floatx4 *>(ml + to * 4) = floatx4{st.m, l, unit, 0.f};
     if constexpr (S::kHalf) {
         write_row<POOL, D, false>(st, factor, to < 0 ? nullptr : o + to * (D * 2), half);
     } else if (to >= 0) {
@@ -1559,7 +1562,7 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
     const int i = item / p.Hq, head = item - i * p.Hq, kv_head = head / p.G, g_head = head - kv_head * p.G, c = i * p.G + g_head;
     const int64_t row = s.q0 + i, at = row * p.Hq + head;
     int n_shared = 0, n_own = 0;
-    // Where the parts of each kind lie, in rows of D (and pairs of maximum and sum): the first one, and how far apart they are.
+    // Where the parts of each kind lie, in rows of D (and of their four words): the first one, and how far apart they are.
     const char *shared_o = p.shared_whole_o, *own_o = p.own_whole_o;
     const float *shared_ml = p.shared_whole_ml, *own_ml = p.own_whole_ml;
     int64_t shared_at = at, own_at = at;
@@ -1610,10 +1613,10 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
     };
     for (int j0 = begin; j0 < end; j0 += kLanes) {
         const int mine = j0 + part, in_own = mine - n_shared, to = min(end, j0 + kLanes), lane0 = (int)(threadIdx.x & 63) / kLanes * kLanes;
-        floatx2 ml = {-INFINITY, 0.f};
+        floatx4 ml = {-INFINITY, 0.f, 0.f, 0.f};
         if (mine < end)
-            ml = in_own < 0 ? reinterpret_cast<const floatx2 *>(shared_ml)[shared_at + (int64_t)mine * kSharedStep + (mine == 0 ? shared_late : 0)]
-                            : reinterpret_cast<const floatx2 *>(own_ml)[own_at + (int64_t)in_own * own_step + (in_own == 0 ? own_late : 0)];
+            ml = in_own < 0 ? reinterpret_cast<const floatx4 *>(shared_ml)[shared_at + (int64_t)mine * kSharedStep + (mine == 0 ? shared_late : 0)]
+                            : reinterpret_cast<const floatx4 *>(own_ml)[own_at + (int64_t)in_own * own_step + (in_own == 0 ? own_late : 0)];
         float e = 0.f;
         auto weigh = [&]() __attribute__((always_inline)) {
             if (ml[1] == 0.f) ml[0] = -INFINITY;  // (no key of this part is seen)
@@ -1623,6 +1626,7 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
             const float m_new = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
             e = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m_new);
             float sum = ml[1] * e;
+            e *= ml[2];  // (of the output, in its unit)
 #pragma unroll
             for (int step = 1; step < kLanes; step *= 2) sum += __shfl_xor(sum, step);
             l = l * f + sum;
@@ -1704,7 +1708,7 @@ Layout layout(int32_t B, int32_t total_q, int32_t groups, int32_t Hq, int32_t D,
         at += round_up(n, 256);
         return here;
     };
-    const size_t ml = 2 * sizeof(float), o = (size_t)D * (dt == RESPEC_BF16 ? 2 : 4);
+    const size_t ml = 4 * sizeof(float), o = (size_t)D * (dt == RESPEC_BF16 ? 2 : 4);
     const size_t rows = groups > 0 ? (size_t)total_q * Hq : 0, own = (size_t)kWorkGroups * 8 * kColumns, shared = groups > 0 ? (size_t)kWorkGroups * 2 * kBlock : 0;
     w.seq = take((size_t)B * sizeof(SeqPlan));
     w.seq_grp = take(groups > 0 ? (size_t)B * sizeof(SeqGroup) : 0);
@@ -1817,7 +1821,7 @@ respec_status_t run(const char *name, SharedParams &p, int32_t D, int32_t page_s
     // What a work-group's tile of own keys takes against one of shared keys.  Over bf16 32 groups of 8 sequences at 28/4 heads (two layers) took 178, 163, 162 and
     // 167 us with 130, 165, 220 and 250 hundredths, 64 single tokens 52, 48, 44 and 43; over 8 bits 8 groups of 16 at 40/8 took 165, 157, 166 and 175 us
     // with 130, 160, 200 and 250.
-    p.own_cost = kn.get(&Knobs::shared_cost, pool_dt == RESPEC_E4M3 ? 155 : dt == RESPEC_BF16 ? 220 : 100) / 100.f;
+    p.own_cost = (float)std::max(1L, kn.get(&Knobs::shared_cost, pool_dt == RESPEC_E4M3 ? 155 : dt == RESPEC_BF16 ? 220 : 100)) / 100.f;
     // Tiles of own keys that make a range of their own: fp32 takes longer for one than a part more takes to join (8 sequences of up to 40 tokens: 20 us with one,
     // 26 with two), bf16 products do not (8 sequences of 512 to 8,192 tokens at 16/2 heads over 8 bits: 27 us with one, 22 with two, 23 with three).
     p.min_tiles = (int)std::max(1L, kn.get(&Knobs::shared_tiles, dt == RESPEC_F32 ? 1 : 2));

@@ -87,3 +87,19 @@ def test_groups_of_many_and_many_groups():
     for groups, shared in (([list(range(300))], [64]), ([[2 * i, 2 * i + 1] for i in range(300)], [48] * 150 + [16] * 150)):
         c = Cache(lens, 1, 64, 16, BF16, groups, shared, seed=35)
         check(c, [1 + i % 4 for i in range(1000)], 4, BF16, groups, shared)
+
+
+@pytest.mark.parametrize("dtype,pool", POOLS)
+@pytest.mark.parametrize("power", [110, 60, -60])
+@pytest.mark.parametrize("grouped", [False, True])
+def test_parts_of_very_different_sizes(dtype, pool, power, grouped):
+    """Values of V of 2^110 (2^60, 2^-60) in one half of the keys and of 1 in the other: each part's sum counts for all."""
+    groups, shared = ([[0, 1]], [1024]) if grouped else ((), ())
+    c = Cache([2100, 1500, 700], 2, 64, 16, dtype, groups, shared, pool, seed=36)
+    for b, first, end in ((0, 0, 64), (1, 0, 64), (2, 20, 40)):
+        for page in set(c.pages[b][first:end]) - (set(c.pages[0][:64]) if grouped and b == 1 else set()):
+            if pool == "e4m3":
+                c.v_scale[page] = (c.v_scale[page].int() + power).clamp(1, 247).to(torch.uint8)
+            else:
+                c.v[page] = torch.where(torch.isnan(c.v[page]), c.v[page], c.v[page] * 2.0 ** power)
+    check(c, [4, 3, 4], 8, dtype, groups, shared)
