@@ -440,21 +440,16 @@ struct State {  // of a wave's 32 columns
         ref = l = 0.f;
     }
     // The scores of a tile to probabilities: the maximum moves where it grows by more than 2^8, the sum is theirs before any rounding.
-    template <int NB>
-    __device__ __attribute__((always_inline)) inline void exponentials(const SharedParams &p, floatx16 (&s)[NB]) {
-        float top = s[0][0];
+    __device__ __attribute__((always_inline)) inline void exponentials(const SharedParams &p, floatx16 &s) {
+        float top = s[0];
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int x = b == 0; x < 16; ++x) top = fmaxf(top, s[b][x]);
+        for (int x = 1; x < 16; ++x) top = fmaxf(top, s[x]);
         rescale(p, top);
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                s[b][x] = __builtin_amdgcn_exp2f(fmaf(s[b][x], p.scale2, -ref));
-                l += s[b][x];
-            }
+        for (int x = 0; x < 16; ++x) {
+            s[x] = __builtin_amdgcn_exp2f(fmaf(s[x], p.scale2, -ref));
+            l += s[x];
+        }
     }
     __device__ __attribute__((always_inline)) inline void rescale(const SharedParams &p, float top) {  // with the largest score that this lane has
         top = max_of_halves(top) * p.scale2;
@@ -483,37 +478,33 @@ struct State {  // of a wave's 32 columns
     }
 };
 
-// A tile of NB blocks of 32 keys in LDS (K at `k`, V at `v`): the scores, masked by `mask` (scores of a block, its number), into the state.
-template <Pool POOL, int D, int NB, typename Mask>
+// A tile of 32 keys in LDS (K at `k`, V at `v`): the scores, masked by mask(), into the state.
+template <Pool POOL, int D, typename Mask>
 __device__ __attribute__((always_inline)) inline void attend(const SharedParams &p, State<POOL, D> &st, const char *lds, int k, int v, int half, int col, Mask &&mask) {
     using S = Shape<POOL, D>;
-    floatx16 s[NB];
     // The place of a piece within its row is an exclusive or, so the x-th pair of pieces of K lies at k_at ^ 32 x and the d-th tile of V at v_at ^ 64 d.
     int k_at = k + col * S::kRowBytes + k_piece<S::kHalf, D>(col, half) * 16;
     asm volatile("" : "+v"(k_at));  // (the addresses that follow from it would not fit beside the tiles in flight)
+    floatx16 s, other;  // (a second chain of products: a wave by itself waits for each)
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        for (int x = 0; x < 16; ++x) s[b][x] = 0.f;
-        floatx16 other = s[b];  // (a second chain of products: a wave by itself waits for each)
+    for (int x = 0; x < 16; ++x) s[x] = other[x] = 0.f;
 #pragma unroll
-        for (int x = 0; x < S::kPieces / 2; ++x) {
-            const u32x4 a = *reinterpret_cast<const u32x4 *>(lds + (k_at ^ (32 * x)) + b * 32 * S::kRowBytes);
-            if constexpr (S::kHalf) {
-                floatx16 &to = x % 2 == 0 ? s[b] : other;
-                to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, st.qf[x]), to, 0, 0, 0);
-            } else {
+    for (int x = 0; x < S::kPieces / 2; ++x) {
+        const u32x4 a = *reinterpret_cast<const u32x4 *>(lds + (k_at ^ (32 * x)));
+        if constexpr (S::kHalf) {
+            floatx16 &to = x % 2 == 0 ? s : other;
+            to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, st.qf[x]), to, 0, 0, 0);
+        } else {
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    floatx16 &to = y % 2 == 0 ? s[b] : other;
-                    to = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[y]), __uint_as_float(st.qf[x][y]), to, 0, 0, 0);
-                }
+            for (int y = 0; y < 4; ++y) {
+                floatx16 &to = y % 2 == 0 ? s : other;
+                to = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[y]), __uint_as_float(st.qf[x][y]), to, 0, 0, 0);
             }
         }
-#pragma unroll
-        for (int x = 0; x < 16; ++x) s[b][x] += other[x];
     }
 #pragma unroll
-    for (int b = 0; b < NB; ++b) mask(s[b], b);
+    for (int x = 0; x < 16; ++x) s[x] += other[x];
+    mask(s);
     st.exponentials(p, s);
     if constexpr (S::kHalf) {
         // V by transposing reads: sixteen lanes address four keys by sixteen d and receive one d of the four keys each.
@@ -521,11 +512,10 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams 
         int v_at = v + v_key * S::kRowBytes + v_piece<true, D>(v_key, d0 >> 4) * 16 + (d0 & 15);
         asm volatile("" : "+v"(v_at));
 #pragma unroll
-        for (int g = 0; g < 2 * NB; ++g) {  // sixteen keys at a time: slot j is key 8 (j / 4) + 4 half + j % 4 of them; their probabilities rounded to bf16
+        for (int g = 0; g < 2; ++g) {  // sixteen keys at a time: slot j is key 8 (j / 4) + 4 half + j % 4 of them; their probabilities rounded to bf16
             u32x4 pf;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                pf[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{s[g / 2][g % 2 * 8 + 2 * j], s[g / 2][g % 2 * 8 + 2 * j + 1]}, bf16x2));
+            for (int j = 0; j < 4; ++j) pf[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{s[g * 8 + 2 * j], s[g * 8 + 2 * j + 1]}, bf16x2));
 #pragma unroll
             for (int d = 0; d < S::kDTiles; ++d) {
                 s16x4 vt[2];
@@ -537,14 +527,12 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams 
         }
     } else {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int x = 0; x < 16; ++x) {
+            const int key = 8 * (x / 4) + 4 * half + x % 4;
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                const int key = b * 32 + 8 * (x / 4) + 4 * half + x % 4;
-#pragma unroll
-                for (int d = 0; d < S::kDTiles; ++d)
-                    st.o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float *>(lds + v + key * S::kRowBytes + (d * 32 + col) * 4), s[b][x], st.o[d], 0, 0, 0);
-            }
+            for (int d = 0; d < S::kDTiles; ++d)
+                st.o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float *>(lds + v + key * S::kRowBytes + (d * 32 + col) * 4), s[x], st.o[d], 0, 0, 0);
+        }
     }
 }
 
@@ -816,7 +804,7 @@ __device__ __attribute__((always_inline)) inline void shared_tiles(const SharedP
         }
         __syncthreads();  // (this tile is there, and the one before the last has been read)
         if (active)
-            attend<kF32, D, 1>(p, st, lds, at, at + S::kSharedBytes / 2, half, col, [&](floatx16 &s, int) __attribute__((always_inline)) {
+            attend(p, st, lds, at, at + S::kSharedBytes / 2, half, col, [&](floatx16 &s) __attribute__((always_inline)) {
                 if (n0 + S::kSharedKeys <= g.shared) return;
                 floatx16 x[1] = {s};
                 mask_past(x, n0, half, g.shared);
@@ -1296,17 +1284,17 @@ __device__ __attribute__((always_inline)) inline void attend_codes(const SharedP
     }
     between();
     if (!active) return;
-    floatx16 s[1], other;
+    floatx16 s, other;
 #pragma unroll
-    for (int x = 0; x < 16; ++x) s[0][x] = other[x] = 0.f;
+    for (int x = 0; x < 16; ++x) s[x] = other[x] = 0.f;
 #pragma unroll
     for (int y = 0; y < D / 32; ++y) {
-        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_of(kc[y][0], kc[y][1], k_scale), __builtin_bit_cast(bf16x8, st.qf[2 * y]), s[0], 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_of(kc[y][0], kc[y][1], k_scale), __builtin_bit_cast(bf16x8, st.qf[2 * y]), s, 0, 0, 0);
         other = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_of(kc[y][2], kc[y][3], k_scale), __builtin_bit_cast(bf16x8, st.qf[2 * y + 1]), other, 0, 0, 0);
     }
 #pragma unroll
-    for (int x = 0; x < 16; ++x) s[0][x] += other[x];
-    mask(s[0]);
+    for (int x = 0; x < 16; ++x) s[x] += other[x];
+    mask(s);
     st.exponentials(p, s);
     u32x4 pf[2];
 #pragma unroll
@@ -1314,7 +1302,7 @@ __device__ __attribute__((always_inline)) inline void attend_codes(const SharedP
 #pragma unroll
         for (int j = 0; j < 2; ++j)
             pf[i / 2][i % 2 * 2 + j] = __builtin_bit_cast(
-                uint32_t, __builtin_convertvector(floatx2{s[0][4 * i + 2 * j] * v_scale[i][2 * j], s[0][4 * i + 2 * j + 1] * v_scale[i][2 * j + 1]}, bf16x2));
+                uint32_t, __builtin_convertvector(floatx2{s[4 * i + 2 * j] * v_scale[i][2 * j], s[4 * i + 2 * j + 1] * v_scale[i][2 * j + 1]}, bf16x2));
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -1372,7 +1360,7 @@ __device__ __attribute__((always_inline)) inline void own_work(const SharedParam
             fresh = now.next(p, f + 1 < n_tiles);
             wave_sync();
             if (cols.packed0 < sn.R * p.G)  // (uniform)
-                attend<POOL, D, 1>(p, st, lds, at0, at0 + S::kOwnBytes / 2, half, col, [&](floatx16 &sc, int) __attribute__((always_inline)) {
+                attend(p, st, lds, at0, at0 + S::kOwnBytes / 2, half, col, [&](floatx16 &sc) __attribute__((always_inline)) {
                     if (special) cols.mask(p, sn, n0, half, sc);
                 });
             wave_sync();
