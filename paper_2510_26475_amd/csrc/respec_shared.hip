@@ -632,8 +632,8 @@ __device__ __attribute__((always_inline)) inline void write_row(const State<POOL
 }
 
 // A wave's column as a part: to row `to` of `ml` its maximum, its sum and the unit of its output, to row `to` of `o` the unnormalised output (negative: there
-// is no such column).  Outputs of bf16 products are written in fp16 in a unit 2^e that all of them lie below: the rounding is 2^-12 of each and 2^-25 of the
-// largest, against 2^-9 of the probabilities before and of the result after (half the bytes: 256 sequences of 512 to 4,096 tokens at 28/4 heads over 8 bits
+// is no such column).  Outputs of bf16 products are written in fp16 in a unit 2^e that all of them lie below: the rounding is at most 2^-11 of each and 2^-25 of
+// the unit, against 2^-8 of the probabilities before and of the result after (half the bytes: 256 sequences of 512 to 4,096 tokens at 28/4 heads over 8 bits
 // leave 20 MB).  What is not finite stays so.
 template <Pool POOL, int D>
 __device__ __attribute__((always_inline)) inline void write_part(const State<POOL, D> &st, float l, char *o, float *ml, int half, int64_t to) {
@@ -868,7 +868,7 @@ __device__ __attribute__((always_inline)) inline void shared_tiles(const SharedP
         return top;
     };
     // Two probabilities of sixteen keys' B operand, the n-th pair of all: slot j is key 8 (j / 4) + 4 half + j % 4 of them.  Rounded to bf16 for the
-    // second product (2^-9 each, averaging over the keys); the sum is that of the unrounded ones.
+    // second product (2^-8 each at most, averaging over the keys); the sum is that of the unrounded ones.
     auto pair = [&](auto n_, const floatx16(&s)[kBlocks], u32x4(&pf)[2 * kBlocks]) __attribute__((always_inline)) {
         constexpr int n = decltype(n_)::value, i = n / 4, j = n % 4 * 2;
         const float a = __builtin_amdgcn_exp2f(fmaf(s[i / 2][i % 2 * 8 + j], p.scale2, -st.ref));
