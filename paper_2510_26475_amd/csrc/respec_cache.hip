@@ -52,9 +52,9 @@ __device__ inline void store8(char *to, const float (&x)[8]) {
 
 // D / 16 lanes hold a head, each two pieces of eight entries: for pairs (i, i + rotary / 2) a piece and the one with its partners, so that no
 // entry leaves its lane but in the sum of squares and the largest magnitude.  A wave goes through the heads of a row, 1024 / D at a time, with the sines
-// and cosines of its position worked out once, an angle in each lane (rotary / 2 <= 64
-// of them: 7.6 us for four rows each of 256 sequences at 28/4 heads, 9.2 with eight angles in each of eight lanes' groups).  An angle is position * inv_freq, in turns and in 64 bits until its whole turns are taken off (in 32 bits a
-// position of 100,000 would leave an error of 0.004).
+// and cosines of its position worked out once, an angle in each lane (rotary / 2 <= 64 of them: 7.6 us for four rows each of 256 sequences at 28/4 heads,
+// 9.2 with eight angles in each of eight lanes' groups).  An angle is position * inv_freq, in turns and in 64 bits until its whole turns are taken off (in
+// 32 bits a position of 100,000 would leave an error of 0.004).
 template <bool BF16, bool E4M3, int D>
 __global__ __launch_bounds__(kThreads) void norm_rope_append_kernel(WriteParams p) {
     constexpr int kLanes = D / 16, kHeads = 64 / kLanes;  // lanes of a head, heads of a wave
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_kernel(WriteParams 
         b += max(0, found - 1) * step;
         end = min(end, b + step);
     }
-    const int q0 = max(0, p.q_indptr[b]), R = min(p.q_indptr[b + 1], p.total_q) - q0;
+    const int q0 = max(0, p.q_indptr[b]), R = max(0, min(p.q_indptr[b + 1], p.total_q)) - q0;
     const int64_t row = token - q0;
     if (row < 0 || row >= min(R, p.max_q)) return;
 
