@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_kernel(WriteParams 
     const int64_t pos = (int64_t)p.kv_len[b] - R + row;
     int64_t page = -1;
     {
-        const int e0 = max(0, min(p.page_indptr[b], p.table_len)), held = max(0, min(p.page_indptr[b + 1], p.table_len) - e0);
+        const int e0 = max(0, min(p.page_indptr[b], p.table_len)), held = max(0, max(0, min(p.page_indptr[b + 1], p.table_len)) - e0);
         if (pos >= 0 && pos < (int64_t)held << p.page_shift) {
             const int32_t id = p.page_table[e0 + (pos >> p.page_shift)];
             if ((uint32_t)id < (uint32_t)p.num_pages) page = id;
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(kThreads) void read_quantised_kernel(ReadParams p) 
         while (b + 1 < p.B && p.kv_indptr[b + 1] <= row) ++b;
         const int64_t j = row - p.kv_indptr[b];
         if (j < 0 || row >= p.kv_indptr[b + 1]) continue;
-        const int e0 = max(0, min(p.page_indptr[b], p.table_len)), held = max(0, min(p.page_indptr[b + 1], p.table_len) - e0);
+        const int e0 = max(0, min(p.page_indptr[b], p.table_len)), held = max(0, max(0, min(p.page_indptr[b + 1], p.table_len)) - e0);
         if (j >= min(p.kv_len[b], p.max_kv) || j >= (int64_t)held << p.page_shift) continue;
         const int32_t id = p.page_table[e0 + (j >> p.page_shift)];
         if ((uint32_t)id >= (uint32_t)p.num_pages) continue;
@@ -271,8 +271,8 @@ struct CommitQParams {
 __global__ __launch_bounds__(kThreads) void commit_quantised_kernel(CommitQParams p) {
     const int b = blockIdx.x;
     const int q0 = max(0, min(p.q_indptr[b], p.total_q));
-    const int R = max(0, min(p.q_indptr[b + 1] - q0, min(p.max_q, p.total_q - q0)));
-    const int e0 = max(0, min(p.page_indptr[b], p.table_len)), held = max(0, min(p.page_indptr[b + 1], p.table_len) - e0);
+    const int R = max(0, min(max(0, min(p.q_indptr[b + 1], p.total_q)) - q0, p.max_q));
+    const int e0 = max(0, min(p.page_indptr[b], p.table_len)), held = max(0, max(0, min(p.page_indptr[b + 1], p.table_len)) - e0);
     __shared__ int sh_len;  // (read by the thread that overwrites it: a wave that starts late must not see the new length)
     if (threadIdx.x == 0) sh_len = p.kv_len[b];
     __syncthreads();

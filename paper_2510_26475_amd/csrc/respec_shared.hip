@@ -269,9 +269,9 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
         SeqPlan s{};
         const int q0 = p.q_indptr[b], q1 = p.q_indptr[b + 1], e0 = p.page_indptr[b], e1 = p.page_indptr[b + 1], length = p.kv_len[b];
         s.q0 = max(0, min(q0, p.total_q));
-        s.R = max(0, min(min(q1, p.total_q) - s.q0, p.max_q));
+        s.R = max(0, min(max(0, min(q1, p.total_q)) - s.q0, p.max_q));
         s.e0 = max(0, min(e0, p.table_len));
-        const int64_t held = max(0, min(e1, p.table_len) - s.e0);
+        const int64_t held = max(0, max(0, min(e1, p.table_len)) - s.e0);
         s.L = (int)max((int64_t)0, min(min((int64_t)length, held << p.page_shift), (int64_t)p.max_kv));
         s.group = -1;
         seq[b] = s;

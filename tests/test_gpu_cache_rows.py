@@ -43,14 +43,23 @@ def test_rows_of_no_sequence_and_past_the_bound(q_indptr, total_q, max_q):
         assert torch.equal(pool, expected)
 
 
-@pytest.mark.parametrize("q_indptr", [[5, 3, 1], [-4, 2, 30], [0, 2 ** 31 - 1, 4], [-2 ** 31, -1, 6], [7, 0, 7]])
-def test_offsets_that_mean_nothing(q_indptr):
+@pytest.mark.parametrize("page_indptr", [[0, 2, 4], [0, 3, -2 ** 31], [3, -2 ** 31, 2 ** 31 - 1], [-2 ** 31, 4, 1]])
+@pytest.mark.parametrize("q_indptr", [[5, 3, 1], [-4, 2, 30], [0, 2 ** 31 - 1, 4], [-2 ** 31, -1, 6], [7, 0, 7], [0, 8, -2 ** 31], [0, 5, 8]])
+def test_offsets_that_mean_nothing(q_indptr, page_indptr):
     total_q, D, page = 8, 64, 16
     k, v = (torch.randn((total_q, 1, D), device="cuda") for _ in range(2))
     guard = [torch.full((6, page, 1, D), 7.0, device="cuda") for _ in range(2)]
     pools = [g[1:5] for g in guard]
-    binding.respec_norm_rope_append_paged(None, k, v, None, None, None, None, None, *pools, None, None, ints(q_indptr), ints([0, 2, 4]), ints([0, 1, 2, 3]), ints([20, 9]),
+    binding.respec_norm_rope_append_paged(None, k, v, None, None, None, None, None, *pools, None, None, ints(q_indptr), ints(page_indptr), ints([0, 1, 2, 3]), ints([20, 9]),
                                           8, 0.0)
     torch.cuda.synchronize()
     for g in guard:
         assert (g[0] == 7.0).all() and (g[5] == 7.0).all() and torch.isfinite(g).all()
+    # and the attention over them
+    q, out = torch.randn((total_q, 2, D), device="cuda"), torch.full((total_q + 8, 2, D), 5.0, device="cuda")
+    for groups in ((None, None), (ints([0, 2]), ints([16]))):
+        ws = torch.empty(binding.respec_verify_attention_shared_workspace_bytes(2, total_q, 1, 8, 64, 2, 1, D, 0), dtype=torch.uint8, device="cuda")
+        binding.respec_verify_attention_shared(q, *pools, None, None, ints(q_indptr), ints(page_indptr), ints([0, 1, 2, 3]), ints([20, 9]), *groups, None, out[:total_q], None,
+                                               8, 64, 0.1, ws)
+        torch.cuda.synchronize()
+        assert (out[total_q:] == 5.0).all() and torch.isfinite(out).all()
