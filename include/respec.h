@@ -426,9 +426,10 @@ respec_status_t respec_pages_copy(void *k_pages, void *v_pages, const int32_t *c
  *   q_weight, k_weight [D] f32 or NULL;  inv_freq [rotary_dim/2] f32 or NULL with rotary_dim = 0
  *   pool_dt dt, with k_scale and v_scale NULL, or RESPEC_E4M3, a cache of 8 bits: k_pages, v_pages [num_pages, page_size, Hkv, D] hold
  *           e4m3 codes (4 exponent and 3 mantissa bits, no infinities) and k_scale, v_scale [num_pages, Hkv, page_size] uint8 an exponent
- *           byte for each token and head; code c under byte e stands for c 2^(e-127), which is a bf16 number exactly.  With top = the largest finite
- *           |x| of the token's head (of what the formulas give, before any rounding) e is the least byte >= 1 with top <= 448 2^(e-127) and c is x / 2^(e-127)
- *           rounded to nearest even; what is not finite becomes NaN.
+ *           byte for each token and head; code c under byte e stands for c 2^(e-127).  With top = the largest finite |x| of the token's head (of what
+ *           the formulas give, before any rounding) e is the least byte >= 1 with top <= 448 2^(e-127) and c is x / 2^(e-127) rounded to nearest even;
+ *           what is not finite becomes NaN.  c 2^(e-127) is a bf16 number exactly for bytes from 3 on (under 1 and 2, heads below 2^-116, it may lie between two),
+ *           and a float for all, but for numbers from 31/32 of 2^128 on: they round to 2^128, which is infinite when it is read.
  *   D in {64, 128}; rotary_dim a multiple of 16 up to D; strides multiples of 16 bytes; q, k, v, q_out, pools, scales and
  *   weights 16-byte aligned; a token's heads at most 2^24 bytes (RESPEC_ERR_UNSUPPORTED otherwise).
  */
@@ -443,7 +444,7 @@ respec_status_t respec_norm_rope_append_paged(const void *q, const void *k, cons
 /*
  * Whole sequences out of a cache of 8 bits: what tokens 0 .. kv_len[b]-1 of sequence b stand for to rows kv_indptr[b] on of k_out and
  * v_out, the layout that respec_prompt_attention reads (a prompt's next chunk is appended, read back with its earlier tokens and attended).
- *   k_out, v_out [total_kv, Hkv, D] dt, contiguous, 16-byte aligned (written; bf16 and fp32 are both exact)
+ *   k_out, v_out [total_kv, Hkv, D] dt, contiguous, 16-byte aligned (written; fp32 is exact, bf16 too from byte 3 on, and rounded to nearest even under 1 and 2)
  *   kv_indptr    [B+1] int64, not decreasing: as many tokens as fit between two entries are written; rows of no sequence, those of tokens past
  *                max_kv_len and those of page ids outside [0, num_pages) are left as they were
  * Pools, scales, tables and page_size as in respec_norm_rope_append_paged.
@@ -473,7 +474,7 @@ respec_status_t respec_pages_copy_quantised(void *k_pages, void *v_pages, uint8_
  *   shared_len   [num_groups] int32: so many tokens at the beginning are the same for all members of the group; they are read from the
  *                pages of its first one.  Any number: what some member does not hold before its new tokens (kv_len[b]-R_b) counts as its own
  *   k_pages, v_pages  of pool_dt, which is dt, with k_scale and v_scale NULL, or RESPEC_E4M3 (dt then RESPEC_BF16; as in
- *                respec_norm_rope_append_paged, bytes 1 to 247): the attention over the bf16 numbers that the codes stand for (values of
+ *                respec_norm_rope_append_paged, bytes 1 to 247): the attention over what respec_read_paged_quantised reads in bf16 (values of
  *                V below 2^-90 may count as zero)
  *   Everything else as in respec_verify_attention_paged; rows of no sequence are left as they were; B <= 65,535,
  *   max_q_per_seq * Hq / Hkv <= 256 (trees: max_q_per_seq <= 64), total_q * Hq < 2^30 (RESPEC_ERR_UNSUPPORTED otherwise).

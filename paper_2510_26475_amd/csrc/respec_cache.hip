@@ -242,17 +242,17 @@ __global__ __launch_bounds__(kThreads) void read_quantised_kernel(ReadParams p) 
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
             const u32x4 codes = w ? vc : kc;
-            uint32_t x[8];
-#pragma unroll
-            for (int y = 0; y < 4; ++y) values_of(codes[y], w ? vs : ks, x[2 * y], x[2 * y + 1]);
+            const float step = w ? vs : ks;
             char *out = (w ? p.v_out : p.k_out) + to * (BF16 ? 32 : 64);
             if constexpr (BF16) {
+                uint32_t x[8];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) values_of(codes[y], step, x[2 * y], x[2 * y + 1]);
                 *reinterpret_cast<u32x4 *>(out) = u32x4{x[0], x[1], x[2], x[3]};
                 *reinterpret_cast<u32x4 *>(out + 16) = u32x4{x[4], x[5], x[6], x[7]};
             } else {
 #pragma unroll
-                for (int y = 0; y < 4; ++y)
-                    *reinterpret_cast<u32x4 *>(out + 16 * y) = u32x4{x[2 * y] << 16, x[2 * y] & 0xffff0000u, x[2 * y + 1] << 16, x[2 * y + 1] & 0xffff0000u};
+                for (int y = 0; y < 4; ++y) *reinterpret_cast<floatx4 *>(out + 16 * y) = floats_of(codes[y], step);
             }
         }
     }

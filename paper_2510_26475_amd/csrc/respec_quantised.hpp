@@ -2,8 +2,10 @@
 //
 // With top = max |x| of a token's head the scale is the least power of two s = 2^e with top <= 448 s (448 is the largest e4m3 number), kept
 // as the byte e + 127, and the codes are x / s rounded to nearest even.  A division by a power of two is exact, so the codes depend on
-// the bits of x alone; and as e4m3 has four significant bits, what a code stands for is a bf16 number exactly.  Against top / 448 itself
-// the power of two costs nothing but range at the low end: e4m3 is a floating-point format, its relative step is the same everywhere above 2^-6.
+// the bits of x alone.  What a code stands for has four significant bits and is a multiple of 2^(byte - 136): a bf16 number exactly under bytes from 3
+// on (the least bf16 number is 2^-133), a float under all of them; but codes past 240 under byte 247 (numbers from 31/32 of 2^128 on) are read as infinite.
+// Against top / 448 itself the power of two costs nothing but range at the low end: e4m3 is a floating-point format, its relative step is the same
+// everywhere above 2^-6.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -13,6 +15,8 @@
 namespace respec {
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float floatx2_t __attribute__((ext_vector_type(2)));
+typedef float floatx4_t __attribute__((ext_vector_type(4)));
 
 // The byte of the scale of a head whose largest finite magnitude is `top`: the exponent of top less 8, one more where top's significand
 // is past 1.75 = 448 / 256.
@@ -31,10 +35,15 @@ __device__ inline uint32_t codes_of(const float (&x)[4]) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
 }
 
-// What four codes stand for, as four bf16 numbers (exact).
+// What four codes stand for, as four bf16 numbers: exact for bytes from 3 on, rounded to nearest even under 1 and 2.
 __device__ inline void values_of(uint32_t codes, float scale, uint32_t &lo, uint32_t &hi) {
     lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false));
     hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true));
+}
+// The same as four floats: exact under every byte.
+__device__ inline floatx4_t floats_of(uint32_t codes, float scale) {
+    const floatx2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, true);
+    return floatx4_t{lo[0], lo[1], hi[0], hi[1]};
 }
 
 }  // namespace respec
