@@ -608,9 +608,10 @@ struct Mover {
     }
 };
 
-// A wave's column times `factor` to `to`, a row of D in bf16 (OUT) or in fp16 (parts); nullptr: there is no such column.  The halves of the wave trade four of
+enum RowType { kOutRow, kPartRow, kWideRow };  // the output (bf16), a part (fp16), a part whose numbers lie too far apart for fp16 (bf16)
+// A wave's column times `factor` to `to`, a row of D; nullptr: there is no such column.  The halves of the wave trade four of
 // eight d each, so that a lane writes sixteen bytes (through LDS, eight columns at a time: 96 sequences with trees of seven rows 163 us, 152 so).
-template <Pool POOL, int D, bool OUT>
+template <Pool POOL, int D, RowType ROW>
 __device__ __attribute__((always_inline)) inline void write_row(const State<POOL, D> &st, float factor, char *to, int half) {
     using S = Shape<POOL, D>;
 #pragma unroll
@@ -621,24 +622,27 @@ __device__ __attribute__((always_inline)) inline void write_row(const State<POOL
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const floatx2 a = {st.o[d][x + 2 * j] * factor, st.o[d][x + 2 * j + 1] * factor};
-                y[j] = OUT ? __builtin_bit_cast(uint32_t, __builtin_convertvector(a, bf16x2)) : __builtin_bit_cast(uint32_t, __builtin_convertvector(a, halfx2));
+                y[j] = ROW != kPartRow ? __builtin_bit_cast(uint32_t, __builtin_convertvector(a, bf16x2)) : __builtin_bit_cast(uint32_t, __builtin_convertvector(a, halfx2));
             }
             const auto lo = __builtin_amdgcn_permlane32_swap(y[0], y[2], false, false), hi = __builtin_amdgcn_permlane32_swap(y[1], y[3], false, false);
             const u32x4 z = {lo[0], hi[0], lo[1], hi[1]};
             u32x4 *const at = reinterpret_cast<u32x4 *>(to + (32 * d + 2 * x + 8 * half) * 2);
-            if (to && OUT) __builtin_nontemporal_store(z, at);
+            if (to && ROW == kOutRow) __builtin_nontemporal_store(z, at);
             else if (to) *at = z;  // (read soon)
         }
 }
 
-// A wave's column as a part: to row `to` of `ml` its maximum, its sum and the unit of its output, to row `to` of `o` the unnormalised output (negative: there
-// is no such column).  Outputs of bf16 products are written in fp16 in a unit 2^e that all of them lie below: the rounding is at most 2^-11 of each and 2^-25 of
-// the unit, against 2^-8 of the probabilities before and of the result after (half the bytes: 256 sequences of 512 to 4,096 tokens at 28/4 heads over 8 bits
-// leave 20 MB).  What is not finite stays so.
+// A wave's column as a part: to row `to` of `ml` its maximum, its sum, the unit of its output and whether that is a wide row, to row `to` of `o` the unnormalised
+// output (negative: there is no such column).  Outputs of bf16 products are written in fp16, in a unit that puts the largest of a row between 2^14 and 2^15:
+// the rounding is at most 2^-11 of each number down to 2^-29 of the largest, against 2^-8 of the probabilities before and of the result after (half
+// the bytes: 256 sequences of 512 to 4,096 tokens at 28/4 heads over 8 bits leave 20 MB).  A row with a smaller number that is not zero (channels of V
+// that far apart; by cancellation one row in a million) is written in bf16, as it is: 2^-8 of each number.  What is not finite stays so.  Returns the wide
+// rows, a bit for each column.
 template <Pool POOL, int D>
-__device__ __attribute__((always_inline)) inline void write_part(const State<POOL, D> &st, float l, char *o, float *ml, int half, int64_t to) {
+__device__ __attribute__((always_inline)) inline uint32_t write_part(const State<POOL, D> &st, float l, char *o, float *ml, int half, int64_t to) {
     using S = Shape<POOL, D>;
     float factor = 1.f, unit = 1.f;
+    uint32_t wide = 0;
     if constexpr (S::kHalf) {
         float top = 0.f;
 #pragma unroll
@@ -652,13 +656,24 @@ __device__ __attribute__((always_inline)) inline void write_part(const State<POO
 #pragma unroll
                 for (int x = 0; x < 16; ++x) top = fmaxf(top, fabsf(st.o[d][x]) < INFINITY ? fabsf(st.o[d][x]) : 0.f);
         }
-        const int e = max(-100, min((int)(__float_as_uint(max_of_halves(top)) >> 23) - 126, 126));  // top < 2^e
-        factor = __uint_as_float((uint32_t)(127 - e) << 23);
-        unit = __uint_as_float((uint32_t)(127 + e) << 23);
+        const int e = max(-97, (int)(__float_as_uint(max_of_halves(top)) >> 23) - 126);  // top < 2^e, 128 at most
+        factor = __uint_as_float((uint32_t)(142 - e) << 23);
+        unit = __uint_as_float((uint32_t)(112 + e) << 23);
+        // The smallest magnitude that is not zero, by its bits (twice them less one: zero is the largest), against 2^-14 units, where fp16 begins to lose bits.
+        uint32_t least = ~0u;
+#pragma unroll
+        for (int d = 0; d < S::kDTiles; ++d)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) least = min(least, (__float_as_uint(st.o[d][x]) << 1) - 1);
+        const uint64_t lanes = __ballot(least < ((uint32_t)(98 + e) << 24) - 1);
+        wide = (uint32_t)lanes | (uint32_t)(lanes >> 32);
     }
-    if (half == 0 && to >= 0) *reinterpret_cast<floatx4 *>(ml + to * 4) = floatx4{st.m, l, unit, 0.f};
+    const bool mine = wide >> (threadIdx.x & 31) & 1;
+    if (half == 0 && to >= 0) *reinterpret_cast<floatx4 *>(ml + to * 4) = floatx4{st.m, l, mine ? 1.f : unit, mine ? 1.f : 0.f};
     if constexpr (S::kHalf) {
-        write_row<POOL, D, false>(st, factor, to < 0 ? nullptr : o + to * (D * 2), half);
+        char *const row = to < 0 ? nullptr : o + to * (D * 2);
+        write_row<POOL, D, kPartRow>(st, factor, mine ? nullptr : row, half);
+        if (wide != 0) write_row<POOL, D, kWideRow>(st, 1.f, mine ? row : nullptr, half);
     } else if (to >= 0) {
 #pragma unroll
         for (int d = 0; d < S::kDTiles; ++d)
@@ -666,6 +681,7 @@ __device__ __attribute__((always_inline)) inline void write_part(const State<POO
             for (int x = 0; x < 16; x += 4)
                 *reinterpret_cast<floatx4 *>(o + (to * D + d * 32 + 2 * x + 4 * half) * 4) = floatx4{st.o[d][x], st.o[d][x + 1], st.o[d][x + 2], st.o[d][x + 3]};
     }
+    return wide;
 }
 
 // One of two buffers of a workspace.  (Chosen by the pointers themselves, the compiler keeps both in scratch and reads the one that is meant.)
@@ -1080,12 +1096,13 @@ __device__ __attribute__((always_inline)) inline void own_finish(const SharedPar
         return packed >= sn.R * p.G ? (int64_t)-1 : ((int64_t)sn.q0 + i) * p.Hq + w.kv_head * p.G + packed - i * p.G;
     };
     char *const part_o = either(w.whole, p.own_whole_o, p.own_o);
+    uint32_t wide = 0;
     if (w.final) {
         const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // (no visible key: zero; NaN stays)
         const int64_t mine = row_of(col);
         if (p.lse && half == 0 && mine >= 0) p.lse[mine] = l == 0.f ? -INFINITY : st.m * 0.693147180559945309f + logf(l);
         if constexpr (S::kHalf) {
-            write_row<POOL, D, true>(st, inv, mine < 0 ? nullptr : p.out + mine * S::kRowBytes, half);
+            write_row<POOL, D, kOutRow>(st, inv, mine < 0 ? nullptr : p.out + mine * S::kRowBytes, half);
         } else if (mine >= 0) {
 #pragma unroll
             for (int d = 0; d < S::kDTiles; ++d)
@@ -1096,7 +1113,7 @@ __device__ __attribute__((always_inline)) inline void own_finish(const SharedPar
         }
     } else {
         const int64_t at = row_of(col);
-        write_part(st, l, part_o, either(w.whole, p.own_whole_ml, p.own_ml), half, at < 0 || w.whole ? at : w.slot + col);
+        wide = write_part(st, l, part_o, either(w.whole, p.own_whole_ml, p.own_ml), half, at < 0 || w.whole ? at : w.slot + col);
     }
     if (!w.bad) return;
     // The values that put() left out, added to what this wave has written: a column and a d of it per lane.
@@ -1131,7 +1148,7 @@ __device__ __attribute__((always_inline)) inline void own_finish(const SharedPar
         const int64_t row = row_of(e / D);
         char *const to = w.final ? p.out + (row * D + d) * S::kSize : part_o + ((w.whole ? row : w.slot + e / D) * D + d) * S::kSize;
         if constexpr (!S::kHalf) *reinterpret_cast<float *>(to) += sum;
-        else if (w.final) *reinterpret_cast<__bf16 *>(to) = (__bf16)((float)*reinterpret_cast<__bf16 *>(to) + sum);
+        else if (w.final || (wide >> (e / D) & 1)) *reinterpret_cast<__bf16 *>(to) = (__bf16)((float)*reinterpret_cast<__bf16 *>(to) + sum);
         else *reinterpret_cast<_Float16 *>(to) = (_Float16)((float)*reinterpret_cast<_Float16 *>(to) + sum);
     }
 }
@@ -1606,6 +1623,7 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
             ml = in_own < 0 ? reinterpret_cast<const floatx4 *>(shared_ml)[shared_at + (int64_t)mine * kSharedStep + (mine == 0 ? shared_late : 0)]
                             : reinterpret_cast<const floatx4 *>(own_ml)[own_at + (int64_t)in_own * own_step + (in_own == 0 ? own_late : 0)];
         float e = 0.f;
+        bool any_wide = false;  // of these parts
         auto weigh = [&]() __attribute__((always_inline)) {
             if (ml[1] == 0.f) ml[0] = -INFINITY;  // (no key of this part is seen)
             float top = ml[0];
@@ -1614,14 +1632,18 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
             const float m_new = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
             e = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m_new);
             float sum = ml[1] * e;
-            e *= ml[2];  // (of the output, in its unit)
+            e *= ml[2];  // (of the output, in its unit; negative for a wide row)
+            if constexpr (HALF) {
+                any_wide = __ballot(ml[3] != 0.f) != 0;
+                if (ml[3] != 0.f) e = -e;
+            }
 #pragma unroll
             for (int step = 1; step < kLanes; step *= 2) sum += __shfl_xor(sum, step);
             l = l * f + sum;
             for (int x = 0; x < 8; ++x) o[x] *= f;
             m = m_new;
         };
-        auto add = [&](int j, auto &x) __attribute__((always_inline)) {
+        auto sum_up = [&](int j, auto &x, auto wide_) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < (int)(sizeof(x) / sizeof(x[0])); ++i) {
                 const float w = __shfl(e, lane0 + min(j + i, to - 1) - j0);
@@ -1630,12 +1652,23 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
                     for (int y = 0; y < kWords; ++y) x[i][y] = u32x4{0, 0, 0, 0};
                 if constexpr (HALF) {
                     const halfx8 h = __builtin_bit_cast(halfx8, x[i][0]);
-                    for (int y = 0; y < 8; ++y) o[y] = fmaf((float)h[y], w, o[y]);
+                    if constexpr (!decltype(wide_)::value) {
+                        for (int y = 0; y < 8; ++y) o[y] = fmaf((float)h[y], w, o[y]);
+                    } else {
+                        for (int y = 0; y < 8; ++y) {
+                            const uint32_t word = x[i][0][y / 2];
+                            o[y] = fmaf(__float_as_int(w) < 0 ? __uint_as_float(y % 2 ? word & 0xffff0000u : word << 16) : (float)h[y], fabsf(w), o[y]);
+                        }
+                    }
                 } else {
                     const floatx4 a = __builtin_bit_cast(floatx4, x[i][0]), b = __builtin_bit_cast(floatx4, x[i][kWords - 1]);
                     for (int y = 0; y < 8; ++y) o[y] = fmaf(y < 4 ? a[y % 4] : b[y % 4], w, o[y]);
                 }
             }
+        };
+        auto add = [&](int j, auto &x) __attribute__((always_inline)) {
+            if (any_wide) sum_up(j, x, std::true_type{});
+            else sum_up(j, x, std::false_type{});
         };
         if (__ballot(to - j0 > 2) == 0) {  // (most sequences of a large batch)
             u32x4 x[2][kWords];
