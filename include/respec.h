@@ -416,7 +416,8 @@ respec_status_t respec_pages_copy(void *k_pages, void *v_pages, const int32_t *c
  *     x' = x / sqrt(mean_d x[d]^2 + eps) * weight[d]                                       (weight NULL: x' = x)
  *     (x'[a], x'[b]) -> (x'[a] cos t - x'[b] sin t, x'[b] cos t + x'[a] sin t),  t = position * inv_freq[i]
  * for the pairs i in [0, rotary_dim/2) of its first rotary_dim entries: a = i, b = i + rotary_dim/2, or, interleaved, a = 2i, b = 2i + 1
- * (inv_freq NULL: no rotation).  V is written as it is.  Everything is computed in fp32, angles in 64 bits, and rounded once.
+ * (inv_freq NULL: no rotation).  V is written as it is.  Everything is computed in fp32, angles in 64 bits up to their sines and cosines, which are within two units of
+ * fp32, and rounded once.
  * Row i of sequence b belongs to position kv_len[b]-R_b+i, where K and V go as in respec_append_paged: rows i >= max_q_per_seq are not
  * processed; rows whose place the sequence's pages do not have write no K and V.  positions [total_q] int32, where not NULL, takes the place
  * of that number in the rotation (a tree's rows lie at the depths of their nodes), not in where they go.
