@@ -80,7 +80,7 @@ struct Cut {
 struct Totals {
     Cut own, shared;
     int64_t own_step, shared_step;  // places of an outer step of own work; of a head of shared work
-    int32_t shared_wgs, pad;
+    int32_t shared_wgs, own_head, shared_head, pad;  // heads: as the cuts were made with them
     uint64_t key;                   // of the sizes that the plan was made for
 };
 
@@ -98,7 +98,7 @@ struct SharedParams {
     uint32_t g_mul, g_shift;                // of a division by G
     uint32_t q_and, q_xor;                  // on the bits of q: a negative scale is taken out of it, a zero one makes it zero
     float scale2;                           // |sm_scale| * log2(e)
-    int32_t own_head, shared_head;          // places before the tiles of a sequence and of a block
+    int32_t own_head, shared_head;          // places before the tiles of a sequence and of a block (the plan's; the join goes by what the plan holds)
     float own_cost;                         // of a work-group's tile of own keys, against one of shared keys
     int32_t max_ranges, min_tiles;
     uint64_t key;
@@ -352,6 +352,8 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
     t.shared = make_cut(all_shared, min(t.shared_wgs, p.max_ranges));
     // (at least a few tiles to a range: parts have to be joined)
     t.own = make_cut(all_own, (int)min((int64_t)min((kWorkGroups - t.shared_wgs) * p.parts_wg, p.max_ranges), (all_own + p.min_tiles - 1) / p.min_tiles));
+    t.own_head = p.own_head;
+    t.shared_head = p.shared_head;
     t.key = p.key;
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.totals = t;
     __syncthreads();
@@ -1576,9 +1578,9 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
     const int own_step = 2 * p.heads_wg * p.col_waves * kColumns;
     if (s.shared > 0) {
         const int packed = max(0, min((int)(row - g.q0) * p.G + g_head, g.rows * p.G - 1));
-        const int64_t b = t.shared_step * kv_head + g.base + (int64_t)(packed / kBlock) * (g.key_tiles + p.shared_head);
-        const int r = range_of(t.shared, b + p.shared_head);
-        n_shared = range_of(t.shared, b + p.shared_head + g.key_tiles - 1) - r + 1;
+        const int64_t b = t.shared_step * kv_head + g.base + (int64_t)(packed / kBlock) * (g.key_tiles + t.shared_head);
+        const int r = range_of(t.shared, b + t.shared_head);
+        n_shared = range_of(t.shared, b + t.shared_head + g.key_tiles - 1) - r + 1;
         if (n_shared > 1) {
             shared_o = p.shared_o;
             shared_ml = p.shared_ml;
@@ -1589,8 +1591,8 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedParams p) {
     if (s.tiles > 0) {
         const int cols = p.col_waves * kColumns, c_block = c / cols, c_in = c - c_block * cols, head_block = kv_head / p.heads_wg;
         const int64_t b = t.own_step * (c_block * (p.Hkv / p.heads_wg) + head_block) + s.base;
-        const int r = range_of(t.own, b + p.own_head);
-        n_own = range_of(t.own, b + p.own_head + s.tiles - 1) - r + 1;
+        const int r = range_of(t.own, b + t.own_head);
+        n_own = range_of(t.own, b + t.own_head + s.tiles - 1) - r + 1;
         if (n_own > 1) {
             own_o = p.own_o;
             own_ml = p.own_ml;
