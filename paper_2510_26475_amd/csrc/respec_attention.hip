@@ -1954,9 +1954,6 @@ __global__ __launch_bounds__(256) void commit_accepted_kernel(CommitParams p) {
 // ------------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------------
-thread_local hipEvent_t g_mark_before_main = nullptr;
-thread_local hipEvent_t g_mark_after_main = nullptr;
-
 struct Plan {
     int32_t Mpad;
     size_t ws_o_bytes, ws_ml_bytes, prefix_bytes, start_bytes, flag_bytes, cut_bytes, ws_bytes;
@@ -2091,11 +2088,6 @@ int few_tiles_groups(int D, int nt, int32_t B, int32_t Hkv, int64_t kv_tokens, i
 
 extern "C" {
 
-void respec_profile_mark_main(void *before_main, void *after_main) {
-    respec::g_mark_before_main = static_cast<hipEvent_t>(before_main);
-    respec::g_mark_after_main = static_cast<hipEvent_t>(after_main);
-}
-
 size_t respec_verify_attention_workspace_bytes(int32_t B, int32_t total_q, int64_t total_kv,
                                                int32_t max_q_per_seq, int32_t max_kv_len,
                                                int32_t Hq, int32_t Hkv, int32_t D,
@@ -2225,10 +2217,7 @@ respec_status_t verify_attention_any(const void *q, const void *k_cache, const v
     hipError_t err;
     const int M = p.G * max_q_per_seq;
     if (dt == RESPEC_F32) {
-        if (g_mark_before_main) {
-            (void)hipEventRecord(g_mark_before_main, stream);
-            g_mark_before_main = nullptr;
-        }
+        mark_before_main(stream);
         const dim3 grid((unsigned)(B * Hq), (unsigned)max_q_per_seq);
         if (D == 128)
             hipLaunchKernelGGL(attn_f32_kernel<128>, grid, dim3(kF32Threads), 0, stream, p);
@@ -2237,10 +2226,7 @@ respec_status_t verify_attention_any(const void *q, const void *k_cache, const v
         err = hipGetLastError();
         if (err != hipSuccess)
             return fail(RESPEC_ERR_HIP, "verify_attention: launch failed: %s", hipGetErrorString(err));
-        if (g_mark_after_main) {
-            (void)hipEventRecord(g_mark_after_main, stream);
-            g_mark_after_main = nullptr;
-        }
+        mark_after_main(stream);
         clear_error();
         return RESPEC_OK;
     }
@@ -2350,10 +2336,7 @@ respec_status_t verify_attention_any(const void *q, const void *k_cache, const v
         if (err != hipSuccess)
             return fail(RESPEC_ERR_HIP, "verify_attention: prep launch failed: %s", hipGetErrorString(err));
     }
-    if (g_mark_before_main) {
-        (void)hipEventRecord(g_mark_before_main, stream);
-        g_mark_before_main = nullptr;
-    }
+    mark_before_main(stream);
     const dim3 grid((unsigned)((W + streams - 1) / streams), (unsigned)col_blocks);
     if (few)
         err = D == 128 ? launch_few<128>(nt, p, stream) : launch_few<64>(nt, p, stream);
@@ -2361,10 +2344,7 @@ respec_status_t verify_attention_any(const void *q, const void *k_cache, const v
         err = D == 128 ? launch_bf16_nt<128>(nt, cw, nc, p, grid, stream) : launch_bf16_nt<64>(nt, cw, nc, p, grid, stream);
     if (err != hipSuccess)
         return fail(RESPEC_ERR_HIP, "verify_attention: main launch failed: %s", hipGetErrorString(err));
-    if (g_mark_after_main) {
-        (void)hipEventRecord(g_mark_after_main, stream);
-        g_mark_after_main = nullptr;
-    }
+    mark_after_main(stream);
     {
         const double most = few ? (double)max_kv_len / (4 * kTileKeys) + 1 : (double)kMaxWaves;
         err = D == 128 ? launch_combine<128>(p, M, kv_tokens, most, kn.get(&Knobs::attn_combine, 0), stream)

@@ -9,7 +9,14 @@ namespace respec {
 
 namespace {
 thread_local char g_last_error[512] = "";
+thread_local hipEvent_t g_mark_before_main = nullptr;
+thread_local hipEvent_t g_mark_after_main = nullptr;
+
+void record_once(hipEvent_t &event, hipStream_t stream) {
+    if (event) (void)hipEventRecord(event, stream);
+    event = nullptr;
 }
+}  // namespace
 
 respec_status_t fail(respec_status_t status, const char *fmt, ...) {
     va_list ap;
@@ -20,6 +27,9 @@ respec_status_t fail(respec_status_t status, const char *fmt, ...) {
 }
 
 void clear_error() { g_last_error[0] = '\0'; }
+
+void mark_before_main(hipStream_t stream) { record_once(g_mark_before_main, stream); }
+void mark_after_main(hipStream_t stream) { record_once(g_mark_after_main, stream); }
 
 namespace {
 
@@ -97,5 +107,10 @@ const char *respec_last_error(void) { return respec::g_last_error; }
 int respec_version(void) { return 200; /* 0.2.0 */ }
 
 void respec_reload_knobs(void) { respec::reload_knobs(); }
+
+void respec_profile_mark_main(void *before_main, void *after_main) {
+    respec::g_mark_before_main = static_cast<hipEvent_t>(before_main);
+    respec::g_mark_after_main = static_cast<hipEvent_t>(after_main);
+}
 
 }  // extern "C"

@@ -58,4 +58,8 @@ struct Knobs {
 Knobs knobs();
 void reload_knobs();
 
+// The profiling hook's events (respec_profile_mark_main), the calling thread's: each is recorded by the next attention call around its main kernel, and forgotten.
+void mark_before_main(hipStream_t stream);
+void mark_after_main(hipStream_t stream);
+
 }  // namespace respec

@@ -1768,7 +1768,9 @@ hipError_t launch(const SharedParams &p, bool prepared, hipStream_t stream) {
         const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLdsBytes);
         if (err != hipSuccess) return err;
     }
+    mark_before_main(stream);
     hipLaunchKernelGGL(kernel, dim3(kWorkGroups), dim3(kThreads), S::kLdsBytes, stream, p);
+    mark_after_main(stream);
     // Few rows have many parts each, which four waves share out.
     const bool split = (int64_t)p.total_q * p.Hq <= 4096;
     const int per = (split ? 64 : kThreads) / (D / 8);
