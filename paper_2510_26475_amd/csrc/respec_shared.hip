@@ -745,13 +745,21 @@ struct Stage {
             constexpr int kOut = POOL == kE4m3 ? 2 : 1;
             const int my_key = wave * S::kWaveKeys + lane / S::kPoolPieces, piece = lane % S::kPoolPieces * kOut;
             const int at = my_key * S::kRowBytes + (V ? v_piece<S::kHalf, D>(my_key, piece) : k_piece<S::kHalf, D>(my_key, piece)) * 16;
+            u32x4 mine[kLoads];
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                if constexpr (kRaw) mine[i] = *reinterpret_cast<const u32x4 *>(raw + (wave * kLoads + i) * 1024 + lane * 16);
+                else mine[i] = x[i];
+            }
+            // (read, before the next straight load into `raw` is asked for: nothing else holds that back)
+            if constexpr (kRaw)
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) asm volatile("" : "+v"(mine[i]) : : "memory");
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 u32x4 a[kOut];
                 if constexpr (POOL == kE4m3) {
-                    u32x4 codes;
-                    if constexpr (kRaw) codes = *reinterpret_cast<const u32x4 *>(raw + (wave * kLoads + i) * 1024 + lane * 16);
-                    else codes = x[i];
+                    const u32x4 codes = mine[i];
                     const float step = scale_of(__shfl((int)scale, i * S::kLoadKeys + lane / S::kPoolPieces));
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
@@ -761,7 +769,7 @@ struct Stage {
                         a[w / 2][w % 2 * 2 + 1] = hi;
                     }
                 } else {
-                    a[0] = x[i];
+                    a[0] = mine[i];
                 }
                 if (V && end < S::kSharedKeys) {
 #pragma unroll
@@ -1334,7 +1342,6 @@ template <Pool POOL, int D>
 __device__ __attribute__((always_inline)) inline void own_work(const SharedParams &p, char *lds, const Job &job) {
     using S = Shape<POOL, D>;
     constexpr bool kCodes = POOL == kE4m3;
-    constexpr int kAhead = kCodes ? 2 : 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int half = lane >> 5, col = lane & 31;
     const int cw = wave % p.col_waves, hi = wave / p.col_waves % p.heads_wg, n_tiles = job.tiles;
