@@ -471,7 +471,7 @@ respec_status_t respec_pages_copy_quantised(void *k_pages, void *v_pages, uint8_
  * every sequence's own tokens (with a tree_mask: on trees) up to rounding, also where sequences have no rows or no tokens: a row that sees no key
  * gets zeros and lse = -inf.
  *   group_indptr [num_groups+1] int32: group g is the sequences group_indptr[g] .. group_indptr[g+1]-1, no sequence in two groups.  Sequences of
- *                no group are read alone.  NULL with num_groups = 0: no groups
+ *                no group are read alone (all of them if the offsets decrease anywhere).  NULL with num_groups = 0: no groups
  *   shared_len   [num_groups] int32: so many tokens at the beginning are the same for all members of the group; they are read from the
  *                pages of its first one.  Any number: what some member does not hold before its new tokens (kv_len[b]-R_b) counts as its own
  *   k_pages, v_pages  of pool_dt, which is dt, with k_scale and v_scale NULL, or RESPEC_E4M3 (dt then RESPEC_BF16; as in

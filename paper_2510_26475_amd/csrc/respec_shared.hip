@@ -255,8 +255,10 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
     SeqPlan *const seq = FEW ? lds_seq : p.seq;
     GroupPlan *const grp = FEW ? lds_grp : p.grp;
     // A group shares what all its members hold before their new tokens.
+    bool mixed = false;  // offsets that decrease: sequences could be in two groups, so nothing is shared
     auto group = [&](int g) __attribute__((always_inline)) {
-        const int first = max(0, min(p.group_indptr[g], p.B)), end = max(first, min(p.group_indptr[g + 1], p.B));
+        const int from = p.group_indptr[g], to = p.group_indptr[g + 1], first = max(0, min(from, p.B)), end = max(first, min(to, p.B));
+        mixed |= to < from;
         GroupPlan t{};
         t.first = first;
         t.end = end;
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
     }
     if ((int)threadIdx.x < p.groups) grp[threadIdx.x] = mine;
     for (int g = threadIdx.x + kPrepThreads; g < p.groups; g += kPrepThreads) grp[g] = group(g);
-    __syncthreads();
+    const bool none = __syncthreads_or(mixed);
     auto group_of = [&](int b) __attribute__((always_inline)) {  // the last one that begins at or before b, if b is in it
         int at = 0;
         for (int end = p.groups; end - at > 1;) {
@@ -299,7 +301,7 @@ __global__ __launch_bounds__(kPrepThreads) void shared_prep_kernel(SharedParams 
         GroupPlan t{};
         t.first = first;
         t.end = end;
-        if (shared > 0) {
+        if (shared > 0 && !none) {
             t.q0 = seq[first].q0;
             t.rows = max(0, seq[end - 1].q0 + seq[end - 1].R - t.q0);
             t.e0 = seq[first].e0;
