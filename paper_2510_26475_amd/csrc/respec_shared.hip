@@ -1047,7 +1047,6 @@ __device__ __attribute__((always_inline)) inline void settle(GroupPlan &g) {  //
 // stage the tiles together.
 template <Pool POOL, int D>
 __device__ __attribute__((always_inline)) inline void shared_work(const SharedParams &p, char *lds, const Job &job) {
-    using S = Shape<POOL, D>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     int left = job.tiles, tile = job.tile, block = job.block, item = job.item, h = job.outer;
     GroupPlan g = job.g;
